@@ -1,0 +1,331 @@
+"""ctypes binding of the operators around the convolution layer (include/bltrain.h).
+
+Layer norm, log probabilities and the AdamW step, as plans like ``blconv.Plan``:
+argument marshalling only, every compute step runs in the HIP kernels of
+libblconv.so on the current stream (or the one given).  Buffers are the
+caller's; ``workspace()`` and ``state()`` make those whose size a plan sets.
+"""
+from __future__ import annotations
+
+import ctypes
+
+from . import blconv
+from .blconv import BlError, _check  # noqa: F401  (BlError: what these calls raise)
+
+BL_F32, BL_BF16, BL_F16 = 0, 1, 2
+
+EXPORTED = (
+    "bl_norm_plan_create", "bl_norm_plan_destroy", "bl_norm_workspace_size", "bl_norm_forward", "bl_norm_backward",
+    "bl_logprob_plan_create", "bl_logprob_plan_destroy", "bl_logprob_workspace_size", "bl_logprob_forward",
+    "bl_logprob_backward", "bl_adamw_plan_create", "bl_adamw_plan_destroy", "bl_adamw_state_size",
+    "bl_adamw_state_layout", "bl_adamw_step", "bl_adamw_get_moments", "bl_adamw_set_moments",
+)
+
+_P, _I, _L, _D, _S = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_double, ctypes.c_size_t
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("outer", _L), ("size", _L), ("inner", _L), ("dtype", _I), ("wdtype", _I), ("eps", _D),
+                ("x_stride", _L), ("y_stride", _L)]
+
+
+class LogProbDesc(ctypes.Structure):
+    _fields_ = [("rows", _L), ("classes", _L), ("top", _I), ("dtype", _I), ("stride", _L), ("grad_stride", _L)]
+
+
+class AdamWDesc(ctypes.Structure):
+    _fields_ = [("count", _I), ("sizes", ctypes.POINTER(_L)), ("decay", ctypes.POINTER(ctypes.c_ubyte)),
+                ("param_dtype", _I), ("grad_dtype", _I), ("bits", _I)]
+
+
+class AdamWArgs(ctypes.Structure):
+    _fields_ = [("lr", _D), ("beta1", _D), ("beta2", _D), ("eps", _D), ("weight_decay", _D), ("step", _L),
+                ("seed", ctypes.c_uint), ("grad_scale", _P), ("live", _P)]
+
+
+_lib = None
+
+
+def load():
+    """libblconv.so with this module's calls declared."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    lib = blconv.load()
+    pp = ctypes.POINTER(_P)
+    lib.bl_norm_plan_create.argtypes = [pp, ctypes.POINTER(NormDesc)]
+    lib.bl_norm_workspace_size.argtypes = [_P, ctypes.POINTER(_S)]
+    lib.bl_norm_forward.argtypes = [_P] * 8
+    lib.bl_norm_backward.argtypes = [_P] * 10
+    lib.bl_logprob_plan_create.argtypes = [pp, ctypes.POINTER(LogProbDesc)]
+    lib.bl_logprob_workspace_size.argtypes = [_P, ctypes.POINTER(_S)]
+    lib.bl_logprob_forward.argtypes = [_P] * 9
+    lib.bl_logprob_backward.argtypes = [_P] * 8
+    lib.bl_adamw_plan_create.argtypes = [pp, ctypes.POINTER(AdamWDesc)]
+    lib.bl_adamw_state_size.argtypes = [_P, ctypes.POINTER(_S), ctypes.POINTER(_L), ctypes.POINTER(_L)]
+    lib.bl_adamw_state_layout.argtypes = [_P] + [ctypes.POINTER(_S)] * 4
+    lib.bl_adamw_step.argtypes = [_P, _P, _P, _P, ctypes.POINTER(AdamWArgs), _P]
+    lib.bl_adamw_get_moments.argtypes = [_P] * 5
+    lib.bl_adamw_set_moments.argtypes = [_P] * 5
+    for name in ("bl_norm_plan_destroy", "bl_logprob_plan_destroy", "bl_adamw_plan_destroy"):
+        getattr(lib, name).argtypes = [_P]
+    for name in EXPORTED:
+        getattr(lib, name)  # every declared symbol must be exported
+    _lib = lib
+    return lib
+
+
+def _dtypes():
+    import torch
+    return {torch.float32: BL_F32, torch.bfloat16: BL_BF16, torch.float16: BL_F16}
+
+
+def _dtype_code(dtype, name):
+    code = _dtypes().get(dtype)
+    if code is None:
+        raise ValueError(f"{name} must be torch.float32, torch.bfloat16 or torch.float16, not {dtype}")
+    return code
+
+
+def _stream(stream):
+    import torch
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def _flat(t, dtype, numel, name):
+    """Device pointer of a contiguous tensor of `numel` elements, whatever its shape."""
+    if t is None:
+        return None
+    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on the GPU")
+    if t.numel() != numel:
+        raise ValueError(f"{name} has {t.numel()} elements, expected {numel}")
+    return t.data_ptr()
+
+
+def _sliced(t, dtype, outer, length, stride, name):
+    """Device pointer of `outer` contiguous slices of `length` elements whose
+    starts are `stride` apart: a contiguous tensor where stride = length, else
+    one whose first axis has that stride."""
+    if not (t.is_cuda and t.dtype == dtype):
+        raise ValueError(f"{name} must be a {dtype} tensor on the GPU")
+    if t.numel() != outer * length:
+        raise ValueError(f"{name} has {t.numel()} elements, expected {outer * length}")
+    if stride == length or outer <= 1:
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    elif t.dim() < 2 or t.shape[0] != outer or t.stride(0) != stride or not t[0].is_contiguous():
+        raise ValueError(f"{name} must have {outer} contiguous slices, {stride} elements apart")
+    return t.data_ptr()
+
+
+class _Plan:
+    _destroy = ""
+
+    def __del__(self):
+        h = getattr(self, "_h", None)
+        if h is not None and h.value:
+            getattr(self._lib, self._destroy)(h)
+            self._h = None
+
+    def workspace(self, device="cuda"):
+        import torch
+        return torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
+
+    def _ws(self, ws):
+        if self.workspace_bytes == 0:
+            return None
+        if ws is None or not ws.is_cuda or ws.numel() * ws.element_size() < self.workspace_bytes:
+            raise ValueError("workspace must be a GPU tensor of at least workspace_bytes bytes")
+        return ws.data_ptr()
+
+
+class NormPlan(_Plan):
+    """Layer norm over the middle axis of [outer][size][inner].
+
+    Rows: ``NormPlan(rows, features)``; the channels at each position of the
+    convolution layer's maps: ``NormPlan(N, C, L)`` or ``NormPlan(N, C, H * W)``;
+    whole samples: ``NormPlan(N, C * H * W)``.  Tensors may have any shape of
+    that many elements.  ``x_stride`` and ``y_stride`` (elements between outer
+    slices, 0: dense) are those of x and dx, and of y and dy.
+    """
+
+    _destroy = "bl_norm_plan_destroy"
+
+    def __init__(self, outer, size, inner=1, dtype=None, wdtype=None, eps=1e-5, x_stride=0, y_stride=0):
+        import torch
+        self._lib = load()
+        self.dtype = torch.float32 if dtype is None else dtype
+        self.wdtype = torch.float32 if wdtype is None else wdtype
+        d = NormDesc(outer, size, inner, _dtype_code(self.dtype, "dtype"), _dtype_code(self.wdtype, "wdtype"),
+                     float(eps), x_stride, y_stride)
+        self._h = _P()
+        _check("bl_norm_plan_create", self._lib.bl_norm_plan_create(ctypes.byref(self._h), ctypes.byref(d)))
+        self.outer, self.size, self.inner = outer, size, inner
+        self.x_stride, self.y_stride = x_stride or size * inner, y_stride or size * inner
+        n = _S()
+        _check("bl_norm_workspace_size", self._lib.bl_norm_workspace_size(self._h, ctypes.byref(n)))
+        self.workspace_bytes = n.value
+
+    def stats_shape(self):
+        return (2, self.outer, self.inner)
+
+    def _x(self, t, name):
+        return _sliced(t, self.dtype, self.outer, self.size * self.inner, self.x_stride, name)
+
+    def _y(self, t, name):
+        return _sliced(t, self.dtype, self.outer, self.size * self.inner, self.y_stride, name)
+
+    def _stats(self, t):
+        import torch
+        return _flat(t, torch.float32, 2 * self.outer * self.inner, "stats")
+
+    def forward(self, x, weight, bias, y, stats, ws, stream=None):
+        """y, and mean and 1 / deviation in `stats` (None: not wanted); weight
+        None: 1, bias None: 0."""
+        _check("bl_norm_forward", self._lib.bl_norm_forward(
+            self._h, self._x(x, "x"), _flat(weight, self.wdtype, self.size, "weight"),
+            _flat(bias, self.wdtype, self.size, "bias"), self._y(y, "y"), self._stats(stats), self._ws(ws),
+            _stream(stream)))
+
+    def backward(self, dy, x, weight, stats, dx, dweight, dbias, ws, stream=None):
+        """dx, and the gradients of weight and bias (None: not wanted)."""
+        _check("bl_norm_backward", self._lib.bl_norm_backward(
+            self._h, self._y(dy, "dy"), self._x(x, "x"), _flat(weight, self.wdtype, self.size, "weight"),
+            self._stats(stats), self._x(dx, "dx"), _flat(dweight, self.wdtype, self.size, "dweight"),
+            _flat(dbias, self.wdtype, self.size, "dbias"), self._ws(ws), _stream(stream)))
+
+
+class LogProbPlan(_Plan):
+    """Log probabilities of given classes, entropies and the `top` likeliest
+    classes of rows of logits, and the logits' gradient."""
+
+    _destroy = "bl_logprob_plan_destroy"
+
+    def __init__(self, rows, classes, top=0, dtype=None, stride=0, grad_stride=0):
+        import torch
+        self._lib = load()
+        self.dtype = torch.float32 if dtype is None else dtype
+        d = LogProbDesc(rows, classes, top, _dtype_code(self.dtype, "dtype"), stride, grad_stride)
+        self._h = _P()
+        _check("bl_logprob_plan_create", self._lib.bl_logprob_plan_create(ctypes.byref(self._h), ctypes.byref(d)))
+        self.rows, self.classes, self.top = rows, classes, top
+        self.stride, self.grad_stride = stride or classes, grad_stride or classes
+        n = _S()
+        _check("bl_logprob_workspace_size", self._lib.bl_logprob_workspace_size(self._h, ctypes.byref(n)))
+        self.workspace_bytes = n.value
+
+    def forward(self, logits, targets, logp, stats, top_logp, top_index, ws, stream=None):
+        """logp [rows], stats [3][rows] (largest logit, log of the sum of
+        exponentials over it, entropy), top_logp and top_index [rows][top]."""
+        import torch
+        _check("bl_logprob_forward", self._lib.bl_logprob_forward(
+            self._h, _sliced(logits, self.dtype, self.rows, self.classes, self.stride, "logits"),
+            _flat(targets, torch.int64, self.rows, "targets"), _flat(logp, torch.float32, self.rows, "logp"),
+            _flat(stats, torch.float32, 3 * self.rows, "stats"),
+            _flat(top_logp, torch.float32, self.rows * self.top, "top_logp"),
+            _flat(top_index, torch.int64, self.rows * self.top, "top_index"), self._ws(ws), _stream(stream)))
+
+    def backward(self, logits, targets, stats, g_logp, g_entropy, dlogits, stream=None):
+        """The logits' gradient from those of logp and of the entropy (None: 0)."""
+        import torch
+        _check("bl_logprob_backward", self._lib.bl_logprob_backward(
+            self._h, _sliced(logits, self.dtype, self.rows, self.classes, self.stride, "logits"),
+            _flat(targets, torch.int64, self.rows, "targets"), _flat(stats, torch.float32, 3 * self.rows, "stats"),
+            _flat(g_logp, torch.float32, self.rows, "g_logp"),
+            _flat(g_entropy, torch.float32, self.rows, "g_entropy"),
+            _sliced(dlogits, self.dtype, self.rows, self.classes, self.grad_stride, "dlogits"), _stream(stream)))
+
+
+class AdamWTensors:
+    """The parameters and gradients that an AdamW step goes over: the tensors,
+    which it keeps alive, and the list of their addresses."""
+
+    def __init__(self, plan, params, grads):
+        if len(params) != len(plan.sizes) or len(grads) != len(plan.sizes):
+            raise ValueError(f"expected {len(plan.sizes)} parameters and gradients")
+        self.plan, self.params, self.grads = plan, list(params), list(grads)
+        ptrs = _P * len(plan.sizes)
+        self._p = ptrs(*[_flat(t, plan.param_dtype, n, f"parameter {i}")
+                         for i, (t, n) in enumerate(zip(params, plan.sizes))])
+        self._g = ptrs(*[_flat(t, plan.grad_dtype, n, f"gradient {i}")
+                         for i, (t, n) in enumerate(zip(grads, plan.sizes))])
+
+
+class AdamWPlan(_Plan):
+    """One AdamW step over tensors of the given sizes; `bits`: 32 or 8 for the
+    moments; `decay`: for each tensor whether weight decay applies (None: to all)."""
+
+    _destroy = "bl_adamw_plan_destroy"
+    workspace_bytes = 0
+
+    def __init__(self, sizes, param_dtype=None, grad_dtype=None, bits=32, decay=None):
+        import torch
+        self._lib = load()
+        self.sizes, self.bits = [int(n) for n in sizes], bits
+        self.param_dtype = torch.float32 if param_dtype is None else param_dtype
+        self.grad_dtype = torch.float32 if grad_dtype is None else grad_dtype
+        count = len(self.sizes)
+        if decay is not None and len(decay) != count:
+            raise ValueError("decay must have a value for each tensor")
+        d = AdamWDesc(count, (_L * count)(*self.sizes),
+                      None if decay is None else (ctypes.c_ubyte * count)(*[bool(x) for x in decay]),
+                      _dtype_code(self.param_dtype, "param_dtype"), _dtype_code(self.grad_dtype, "grad_dtype"), bits)
+        self._h = _P()
+        _check("bl_adamw_plan_create", self._lib.bl_adamw_plan_create(ctypes.byref(self._h), ctypes.byref(d)))
+        n, total, start = _S(), _L(), (_L * count)()
+        _check("bl_adamw_state_size", self._lib.bl_adamw_state_size(self._h, ctypes.byref(n), ctypes.byref(total),
+                                                                    start))
+        self.state_bytes, self.total, self.starts = n.value, total.value, list(start)
+
+    def state(self, device="cuda"):
+        """A new state: moments of zero."""
+        import torch
+        return torch.zeros(self.state_bytes, dtype=torch.uint8, device=device)
+
+    def _state(self, state):
+        if not (state.is_cuda and state.is_contiguous()) or state.numel() * state.element_size() != self.state_bytes:
+            raise ValueError("state must be a contiguous GPU tensor of state_bytes bytes")
+        return state.data_ptr()
+
+    def bind(self, params, grads):
+        """The list of tensors that step() takes: contiguous, of the plan's sizes and types."""
+        return AdamWTensors(self, params, grads)
+
+    def step(self, tensors, state, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, step=1, grad_scale=None,
+             seed=0, live=None, stream=None):
+        """One step, in place.  `grad_scale`: a float32 GPU tensor of one element
+        that gradients are multiplied by.  `live`: a float64 GPU tensor (lr, step)
+        that is read in the place of those two when the kernels run."""
+        import torch
+        if tensors.plan is not self:
+            raise ValueError("the tensors were bound to another plan")
+        a = AdamWArgs(lr, betas[0], betas[1], eps, weight_decay, step, seed & 0xFFFFFFFF,
+                      _flat(grad_scale, torch.float32, 1, "grad_scale"), _flat(live, torch.float64, 2, "live"))
+        _check("bl_adamw_step", self._lib.bl_adamw_step(self._h, tensors._p, tensors._g, self._state(state),
+                                                        ctypes.byref(a), _stream(stream)))
+
+    def moments(self, state, m=None, v=None, stream=None):
+        """(m, v), [total] each, tensor i's at starts[i]: of 32 bits as views of
+        the state, of 8 bits as their values in new bfloat16 tensors (or those given)."""
+        import torch
+        if self.bits == 32 and m is None and v is None:
+            both = state.view(torch.float32)
+            return both[:self.total], both[self.total:]
+        dtype = torch.float32 if self.bits == 32 else torch.bfloat16
+        with torch.cuda.stream(stream):  # (None: the current one) memory of the stream that writes it
+            m = torch.empty(self.total, dtype=dtype, device=state.device) if m is None else m
+            v = torch.empty(self.total, dtype=dtype, device=state.device) if v is None else v
+        _check("bl_adamw_get_moments", self._lib.bl_adamw_get_moments(
+            self._h, self._state(state), _flat(m, dtype, self.total, "m"), _flat(v, dtype, self.total, "v"),
+            _stream(stream)))
+        return m, v
+
+    def load_moments(self, state, m, v, stream=None):
+        """Sets the moments from values (converted to float32) in the layout of moments()."""
+        import torch
+        with torch.cuda.stream(stream):
+            m, v = m.float(), v.float()
+        _check("bl_adamw_set_moments", self._lib.bl_adamw_set_moments(
+            self._h, self._state(state), _flat(m, torch.float32, self.total, "m"),
+            _flat(v, torch.float32, self.total, "v"), _stream(stream)))
