@@ -197,7 +197,9 @@ bl_status_t bl_adamw_step(bl_adamw_plan_t plan, void* const* params, const void*
 
 /* The moments as values, m and v [total] each: fp32 with bits = 32, bfloat16 with
  * bits = 8 (which holds every 8-bit value exactly); and from fp32 values, rounded
- * to nearest with bits = 8 (half away from zero). */
+ * to nearest with bits = 8 (half away from zero; S is the largest power of two
+ * below the block's largest magnitude, so that values which bl_adamw_get_moments
+ * gave are held again exactly). */
 bl_status_t bl_adamw_get_moments(bl_adamw_plan_t plan, const void* state, void* m, void* v, void* stream);
 bl_status_t bl_adamw_set_moments(bl_adamw_plan_t plan, void* state, const float* m, const float* v, void* stream);
 

@@ -68,6 +68,13 @@ constexpr float kDownM = 0x1p-113f, kUpM = 0x1p113f, kDownV = 0x1p-97f, kUpV = 0
 __device__ __forceinline__ float power_of(float largest) {
   return fmaxf(__uint_as_float(__float_as_uint(largest) & 0x7F800000u), 0x1p-96f);
 }
+// For moments set from values: half of it where the largest is itself a power of
+// two (which the code above all fractions then holds), so that values which
+// codes stood for are held again as they are, however their block's S was.
+__device__ __forceinline__ float power_below(float largest) {
+  const unsigned u = __float_as_uint(largest);
+  return power_of(__uint_as_float(u ? u - 1 : 0));
+}
 __device__ __forceinline__ unsigned encode(float a, float scale, float down, unsigned d16) {
   return (__float_as_uint(a / scale * down) + (d16 << 4)) >> 20;
 }
@@ -197,7 +204,7 @@ __global__ __launch_bounds__(kT) void k_get8(const StepArgs a, bf16_t* m, bf16_t
 __global__ __launch_bounds__(kT) void k_set8(StepArgs a, const float* m, const float* v) {
   const size_t at = ((size_t)blockIdx.x * kT + threadIdx.x) * 4;
   const Pack<float, 4> mi = load_pack<float, 4>(m + at), vi = load_pack<float, 4>(v + at);
-  const float ms = power_of(block_largest(mi.v)), vs = power_of(block_largest(vi.v));
+  const float ms = power_below(block_largest(mi.v)), vs = power_below(block_largest(vi.v));
   unsigned mc = 0, vc = 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
