@@ -14,7 +14,7 @@ LIB = os.path.join(PKG, "libblconv.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["plan.cpp", "api.hip", "tables.hip", "direct.hip", "bluestein.hip", "fft2d.hip", "mdft.hip", "pgemm.hip", "contract.hip", "thin.hip", "energy.hip", "topk.hip", "small.hip",
-           "norm.hip", "logprob.hip", "adamw.hip"]
+           "norm.hip", "norm_rows.hip", "norm_maps.hip", "logprob.hip", "adamw.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950",

@@ -1,105 +1,64 @@
-// Layer norm over the middle axis of [outer][size][inner]: forward and backward.
+// Layer norm over the middle axis of [outer][size][inner]: plan, dispatch and
+// the last sum of the weights' gradients.
 #include <cmath>
 #include <new>
 
-#include "ops.hpp"
-
-struct bl_norm_plan_s {
-  bl_norm_desc_t d;
-};
+#include "norm.hpp"
 
 namespace blc {
 namespace {
 
-constexpr int kT = 256;
-
-__device__ float block_sum(float x, float* red) {
-  x = wave_sum(x);
+// Sums of partial rows part[parts][2 size] by columns: 64 columns and 16 slices
+// of the rows a block, each slice in order with four loads in flight, then the
+// slices in order.  (One thread a column would wait for `parts` loads in turn.)
+constexpr int kCols = 64, kSlices = 16;
+template <typename T>
+__global__ __launch_bounds__(kCols* kSlices) void k_norm_sum(const float* part, int parts, long size, void* dw,
+                                                             void* db, bool wide) {
+  __shared__ float red[kSlices][kCols];
+  const int col = threadIdx.x % kCols, slice = threadIdx.x / kCols;
+  const long n = 2 * size, c = (long)blockIdx.x * kCols + col;
+  float acc[4] = {};
+  if (c < n) {
+    int r = slice;
+    for (; r + 3 * kSlices < parts; r += 4 * kSlices) {
+      float v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = part[(size_t)(r + k * kSlices) * n + c];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[k] += v[k];
+    }
+    for (int k = 0; r < parts; r += kSlices, ++k) acc[k] += part[(size_t)r * n + c];
+  }
+  red[slice][col] = (acc[0] + acc[1]) + (acc[2] + acc[3]);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-  __syncthreads();
-  float t = 0.f;
-  for (int w = 0; w < kT / 64; ++w) t += red[w];
-  return t;
-}
-
-__device__ float load_w(const void* w, int dtype, long i) {
-  return dtype == BL_F32 ? static_cast<const float*>(w)[i]
-                         : dtype == BL_BF16 ? to_f32(static_cast<const bf16_t*>(w)[i])
-                                            : to_f32(static_cast<const f16_t*>(w)[i]);
-}
-__device__ void store_w(void* w, int dtype, long i, float x) {
-  if (dtype == BL_F32) static_cast<float*>(w)[i] = x;
-  else if (dtype == BL_BF16) static_cast<bf16_t*>(w)[i] = (bf16_t)x;
-  else static_cast<f16_t*>(w)[i] = (f16_t)x;
-}
-
-template <typename T>
-__global__ void k_norm_fwd(const T* x, const void* w, const void* b, T* y, float* stats, bl_norm_desc_t d) {
-  __shared__ float red[kT / 64];
-  const long site = blockIdx.x, o = site / d.inner, i = site % d.inner, sites = d.outer * d.inner;
-  const T* xr = x + o * d.x_stride + i;
-  float s = 0.f;
-  for (long j = threadIdx.x; j < d.size; j += kT) s += to_f32(xr[j * d.inner]);
-  const float mean = block_sum(s, red) / d.size;
-  s = 0.f;
-  for (long j = threadIdx.x; j < d.size; j += kT) {
-    const float c = to_f32(xr[j * d.inner]) - mean;
-    s += c * c;
-  }
-  const float rstd = 1.f / sqrtf(block_sum(s, red) / d.size + (float)d.eps);
-  for (long j = threadIdx.x; j < d.size; j += kT) {
-    const float h = (to_f32(xr[j * d.inner]) - mean) * rstd;
-    y[o * d.y_stride + j * d.inner + i] = (T)(h * (w ? load_w(w, d.wdtype, j) : 1.f) + (b ? load_w(b, d.wdtype, j) : 0.f));
-  }
-  if (stats && threadIdx.x == 0) {
-    stats[site] = mean;
-    stats[sites + site] = rstd;
-  }
-}
-
-template <typename T>
-__global__ void k_norm_dx(const T* dy, const T* x, const void* w, const float* stats, T* dx, bl_norm_desc_t d) {
-  __shared__ float red[kT / 64];
-  const long site = blockIdx.x, o = site / d.inner, i = site % d.inner, sites = d.outer * d.inner;
-  const float mean = stats[site], rstd = stats[sites + site];
-  float s1 = 0.f, s2 = 0.f;
-  for (long j = threadIdx.x; j < d.size; j += kT) {
-    const float h = (to_f32(x[o * d.x_stride + j * d.inner + i]) - mean) * rstd;
-    const float u = to_f32(dy[o * d.y_stride + j * d.inner + i]) * (w ? load_w(w, d.wdtype, j) : 1.f);
-    s1 += u;
-    s2 += u * h;
-  }
-  s1 = block_sum(s1, red) / d.size;
-  s2 = block_sum(s2, red) / d.size;
-  for (long j = threadIdx.x; j < d.size; j += kT) {
-    const float h = (to_f32(x[o * d.x_stride + j * d.inner + i]) - mean) * rstd;
-    const float u = to_f32(dy[o * d.y_stride + j * d.inner + i]) * (w ? load_w(w, d.wdtype, j) : 1.f);
-    dx[o * d.x_stride + j * d.inner + i] = (T)(rstd * (u - s1 - h * s2));
-  }
-}
-
-template <typename T>
-__global__ void k_norm_dw(const T* dy, const T* x, const float* stats, void* dw, void* db, bl_norm_desc_t d) {
-  __shared__ float red[kT / 64];
-  const long j = blockIdx.x, sites = d.outer * d.inner;
-  float s1 = 0.f, s2 = 0.f;
-  for (long site = threadIdx.x; site < sites; site += kT) {
-    const long o = site / d.inner, i = site % d.inner;
-    const float h = (to_f32(x[o * d.x_stride + j * d.inner + i]) - stats[site]) * stats[sites + site];
-    const float g = to_f32(dy[o * d.y_stride + j * d.inner + i]);
-    s1 += g * h;
-    s2 += g;
-  }
-  s1 = block_sum(s1, red);
-  s2 = block_sum(s2, red);
-  if (threadIdx.x == 0) {
-    if (dw) store_w(dw, d.wdtype, j, s1);
-    if (db) store_w(db, d.wdtype, j, s2);
-  }
+  if (slice || c >= n) return;
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < kSlices; ++k) sum += red[k][col];
+  void* out = c < size ? dw : db;
+  const long i = c < size ? c : c - size;
+  if (!out) return;
+  if (wide) static_cast<float*>(out)[i] = sum;
+  else static_cast<T*>(out)[i] = (T)sum;
 }
 
 }  // namespace
+
+bl_status_t norm_sum_parts(const bl_norm_plan_s* p, const NormPtrs& a, int parts, hipStream_t s) {
+  if (!a.dw && !a.db) return BL_OK;
+  const unsigned blocks = (unsigned)((2 * p->d.size + kCols - 1) / kCols);
+  const bool wide = p->d.wdtype == BL_F32;
+  return timed_launch("norm_sum", 8.0 * parts * p->d.size, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    if (p->d.dtype == BL_BF16)
+      hipExtLaunchKernelGGL(k_norm_sum<bf16_t>, dim3(blocks), dim3(kCols * kSlices), 0, s, e0, e1, 0, a.part, parts,
+                            (long)p->d.size, a.dw, a.db, wide);
+    else
+      hipExtLaunchKernelGGL(k_norm_sum<f16_t>, dim3(blocks), dim3(kCols * kSlices), 0, s, e0, e1, 0, a.part, parts,
+                            (long)p->d.size, a.dw, a.db, wide);
+  });
+}
+
 }  // namespace blc
 
 using namespace blc;
@@ -118,8 +77,14 @@ extern "C" bl_status_t bl_norm_plan_create(bl_norm_plan_t* out, const bl_norm_de
   if (!d.x_stride) d.x_stride = d.size * d.inner;
   if (!d.y_stride) d.y_stride = d.size * d.inner;
   if (d.outer > 1 && (d.x_stride < d.size * d.inner || d.y_stride < d.size * d.inner)) return BL_ERR_INVALID_ARG;
-  bl_norm_plan_s* p = new (std::nothrow) bl_norm_plan_s{d};
+  bl_norm_plan_s* p = new (std::nothrow) bl_norm_plan_s{};
   if (!p) return BL_ERR_OOM;
+  p->d = d;
+  const bl_status_t st = !d.outer ? BL_OK : d.inner == 1 ? norm_rows_plan(p) : norm_maps_plan(p);
+  if (st != BL_OK) {
+    delete p;
+    return st;
+  }
   *out = p;
   return BL_OK;
 }
@@ -132,59 +97,39 @@ extern "C" bl_status_t bl_norm_plan_destroy(bl_norm_plan_t p) {
 
 extern "C" bl_status_t bl_norm_workspace_size(bl_norm_plan_t p, size_t* bytes) {
   if (!p || !bytes) return BL_ERR_INVALID_ARG;
-  *bytes = 0;
+  *bytes = p->bytes;
   return BL_OK;
 }
 
-namespace {
-template <typename T>
-bl_status_t forward(const bl_norm_plan_s* p, const void* x, const void* w, const void* b, void* y, float* stats,
-                    hipStream_t s) {
-  const bl_norm_desc_t& d = p->d;
-  const double n = (double)d.outer * d.size * d.inner;
-  if (!d.outer) return BL_OK;
-  return timed_launch("norm_fwd", 2 * n * sizeof(T), 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-    hipExtLaunchKernelGGL(k_norm_fwd<T>, dim3((unsigned)(d.outer * d.inner)), dim3(kT), 0, s, e0, e1, 0,
-                          static_cast<const T*>(x), w, b, static_cast<T*>(y), stats, d);
-  });
-}
-template <typename T>
-bl_status_t backward(const bl_norm_plan_s* p, const void* dy, const void* x, const void* w, const float* stats,
-                     void* dx, void* dw, void* db, hipStream_t s) {
-  const bl_norm_desc_t& d = p->d;
-  const double n = (double)d.outer * d.size * d.inner;
-  const T* dyt = static_cast<const T*>(dy);
-  const T* xt = static_cast<const T*>(x);
-  if (dw || db) {
-    const bl_status_t st = timed_launch("norm_dw", 2 * n * sizeof(T), 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-      hipExtLaunchKernelGGL(k_norm_dw<T>, dim3((unsigned)d.size), dim3(kT), 0, s, e0, e1, 0, dyt, xt, stats, dw, db, d);
-    });
-    if (st != BL_OK) return st;
-  }
-  if (!d.outer) return BL_OK;
-  return timed_launch("norm_dx", 3 * n * sizeof(T), 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-    hipExtLaunchKernelGGL(k_norm_dx<T>, dim3((unsigned)(d.outer * d.inner)), dim3(kT), 0, s, e0, e1, 0, dyt, xt, w,
-                          stats, static_cast<T*>(dx), d);
-  });
-}
-}  // namespace
-
 extern "C" bl_status_t bl_norm_forward(bl_norm_plan_t p, const void* x, const void* w, const void* b, void* y,
                                        float* stats, void* ws, void* stream) {
-  if (!p || (p->d.outer && (!x || !y))) return BL_ERR_INVALID_ARG;
-  (void)ws;
+  if (!p || (p->d.outer && (!x || !y || (p->bytes && !ws)))) return BL_ERR_INVALID_ARG;
+  if (!p->d.outer) return BL_OK;
+  NormPtrs a{};
+  a.x = x;
+  a.w = w;
+  a.b = b;
+  a.y = y;
+  a.stats = stats;
+  a.sums = reinterpret_cast<float*>(static_cast<char*>(ws) + p->off_sums);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (p->d.dtype == BL_F32) return forward<float>(p, x, w, b, y, stats, s);
-  if (p->d.dtype == BL_BF16) return forward<bf16_t>(p, x, w, b, y, stats, s);
-  return forward<f16_t>(p, x, w, b, y, stats, s);
+  return p->d.inner == 1 ? norm_rows_forward(p, a, s) : norm_maps_forward(p, a, s);
 }
 
 extern "C" bl_status_t bl_norm_backward(bl_norm_plan_t p, const void* dy, const void* x, const void* w,
                                         const float* stats, void* dx, void* dw, void* db, void* ws, void* stream) {
-  if (!p || (p->d.outer && (!dy || !x || !stats || !dx))) return BL_ERR_INVALID_ARG;
-  (void)ws;
+  if (!p || (p->d.outer && (!dy || !x || !stats || !dx || (p->bytes && !ws)))) return BL_ERR_INVALID_ARG;
+  NormPtrs a{};
+  a.x = x;
+  a.dy = dy;
+  a.w = w;
+  a.dx = dx;
+  a.dw = dw;
+  a.db = db;
+  a.stats = const_cast<float*>(stats);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + p->off_part);
+  a.sums = reinterpret_cast<float*>(static_cast<char*>(ws) + p->off_sums);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (p->d.dtype == BL_F32) return backward<float>(p, dy, x, w, stats, dx, dw, db, s);
-  if (p->d.dtype == BL_BF16) return backward<bf16_t>(p, dy, x, w, stats, dx, dw, db, s);
-  return backward<f16_t>(p, dy, x, w, stats, dx, dw, db, s);
+  if (!p->d.outer) return norm_sum_parts(p, a, 0, s);
+  return p->d.inner == 1 ? norm_rows_backward(p, a, s) : norm_maps_backward(p, a, s);
 }

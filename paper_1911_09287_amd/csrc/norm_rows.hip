@@ -1,0 +1,536 @@
+// Layer norm of rows (inner = 1).
+//
+// A row stays in the registers of the lanes that hold it: it is read once, its
+// mean and then the squares of what differs from the mean are summed over the
+// lanes, and it is written once (backward: x and dy are read once, the two sums
+// of u and u h taken together).  Bound by HBM.  Short rows lie on 1 to 64 lanes
+// of a wave, long ones on a block; rows that a block's registers do not hold, or
+// that are too few to fill the GPU, are cut in chunks over many blocks, in two
+// launches: partial statistics, then the result.
+#include <algorithm>
+
+#include "norm.hpp"
+
+namespace blc {
+namespace {
+
+constexpr int kT = kNormThreads;
+constexpr int kMostThreads = 1024;
+constexpr int kTargetBlocks = 512;  // two a compute unit
+
+// ---- sums over the lanes of a row ---------------------------------------------
+// BLOCK: over the block, by way of LDS; `red` alternates between two arrays from
+// one sum to the next, so that one barrier a sum is enough.
+template <bool BLOCK, int N>
+__device__ __forceinline__ void row_sum(float (&x)[N], int lanes, float (*red)[kMostThreads / kWave]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i], BLOCK ? kWave : lanes);
+  if (!BLOCK) return;
+  const int wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+  if (threadIdx.x % kWave == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) red[i][wave] = x[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    x[i] = red[i][0];
+    for (int k = 1; k < waves; ++k) x[i] += red[i][k];
+  }
+}
+
+// E vectors of 16 bytes a lane.  Weights of few are kept over a block's rows.
+template <typename T, int E, bool BLOCK>
+__global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_fwd(NormPtrs a, bl_norm_desc_t d, int lanes) {
+  constexpr int V = 16 / sizeof(T);
+  __shared__ float red[2][1][kMostThreads / kWave];
+  const int in = BLOCK ? threadIdx.x : threadIdx.x % lanes, step = BLOCK ? blockDim.x : lanes;
+  const long rows = d.outer, M = d.size;
+  const long each = BLOCK ? 1 : kT / lanes;
+  const bool wide = d.wdtype == BL_F32;
+  constexpr bool keep = E * V <= 16;
+  float w[keep ? E : 1][V], b[keep ? E : 1][V];
+  if (keep)
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      const long i = (long)(in + k * step) * V;
+      load_weights<T, V>(a.w, wide, i, M - i, 1.f, w[k]);
+      load_weights<T, V>(a.b, wide, i, M - i, 0.f, b[k]);
+    }
+  for (long row = blockIdx.x * each + (BLOCK ? 0 : threadIdx.x / lanes); row < rows; row += gridDim.x * each) {
+    const T* x = static_cast<const T*>(a.x) + row * d.x_stride;
+    T* y = static_cast<T*>(a.y) + row * d.y_stride;
+    Held<T, V> v[E];
+    float s[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      const long i = (long)(in + k * step) * V;
+      v[k].load(x + i, M - i);
+    }
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[0] += v[k][j];
+      v[k].refresh();
+    }
+    row_sum<BLOCK>(s, lanes, red[0]);
+    const float mean = s[0] / (float)M;
+    s[0] = 0.f;
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float c = v[k][j] - mean;
+        s[0] += (long)(in + k * step) * V + j < M ? c * c : 0.f;
+      }
+      v[k].refresh();
+    }
+    row_sum<BLOCK>(s, lanes, red[1]);
+    const float rstd = 1.f / sqrtf(s[0] / (float)M + (float)d.eps);
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      const long i = (long)(in + k * step) * V;
+      const int at = keep ? k : 0;
+      if (!keep) {
+        load_weights<T, V>(a.w, wide, i, M - i, 1.f, w[0]);
+        load_weights<T, V>(a.b, wide, i, M - i, 0.f, b[0]);
+      }
+      Pack<T, V> o;
+#pragma unroll
+      for (int j = 0; j < V; ++j) o.v[j] = (T)fmaf((v[k][j] - mean) * rstd, w[at][j], b[at][j]);
+      store_part<T, V>(y + i, M - i, o);
+    }
+    if (a.stats && in == 0) {
+      a.stats[row] = mean;
+      a.stats[rows + row] = rstd;
+    }
+  }
+}
+
+// dx; and where part is given this block's sums of dy h and dy by column, [block][2][M].
+template <typename T, int E, bool BLOCK>
+__global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_bwd(NormPtrs a, bl_norm_desc_t d, int lanes,
+                                                                        bool sums) {
+  constexpr int V = 16 / sizeof(T);
+  __shared__ float red[2][2][kMostThreads / kWave];
+  __shared__ float comb[BLOCK ? 1 : 2 * kWave * E * V];
+  const int in = BLOCK ? threadIdx.x : threadIdx.x % lanes, step = BLOCK ? blockDim.x : lanes;
+  const long rows = d.outer, M = d.size;
+  const long each = BLOCK ? 1 : kT / lanes;
+  const float inv = 1.f / (float)M;
+  float w[E][V], aw[E][V] = {}, ab[E][V] = {};
+#pragma unroll
+  for (int k = 0; k < E; ++k) {
+    const long i = (long)(in + k * step) * V;
+    load_weights<T, V>(a.w, d.wdtype == BL_F32, i, M - i, 1.f, w[k]);
+  }
+  int turn = 0;
+  for (long row = blockIdx.x * each + (BLOCK ? 0 : threadIdx.x / lanes); row < rows; row += gridDim.x * each) {
+    const T* x = static_cast<const T*>(a.x) + row * d.x_stride;
+    const T* dy = static_cast<const T*>(a.dy) + row * d.y_stride;
+    T* dx = static_cast<T*>(a.dx) + row * d.x_stride;
+    Held<T, V> v[E], g[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      const long i = (long)(in + k * step) * V;
+      v[k].load(x + i, M - i);
+      g[k].load(dy + i, M - i);
+    }
+    const float mean = a.stats[row], rstd = a.stats[rows + row];
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {  // (past the row dy is 0)
+        const float h = (v[k][j] - mean) * rstd, dyj = g[k][j], u = dyj * w[k][j];
+        s[0] += u;
+        s[1] = fmaf(u, h, s[1]);
+        aw[k][j] = fmaf(dyj, h, aw[k][j]);
+        ab[k][j] += dyj;
+      }
+      v[k].refresh();
+      g[k].refresh();
+    }
+    row_sum<BLOCK>(s, lanes, red[turn]);
+    turn ^= 1;
+    const float c1 = s[0] * inv, c2 = s[1] * inv;
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      const long i = (long)(in + k * step) * V;
+      Pack<T, V> o;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float h = (v[k][j] - mean) * rstd;
+        o.v[j] = (T)(rstd * (fmaf(g[k][j], w[k][j], -c1) - h * c2));
+      }
+      store_part<T, V>(dx + i, M - i, o);
+    }
+  }
+  if (!sums) return;
+  float* part = a.part + (size_t)blockIdx.x * 2 * M;
+  if (BLOCK) {
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      const long i = (long)(in + k * step) * V;
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (i + j < M) {
+          part[i + j] = aw[k][j];
+          part[M + i + j] = ab[k][j];
+        }
+    }
+    return;
+  }
+  // the rows of a wave, then the waves in order
+#pragma unroll
+  for (int k = 0; k < E; ++k)
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      for (int o = lanes; o < kWave; o <<= 1) {
+        aw[k][j] += __shfl_xor(aw[k][j], o);
+        ab[k][j] += __shfl_xor(ab[k][j], o);
+      }
+  const int width = lanes * E * V;  // >= M
+  for (int wave = 0; wave < kT / kWave; ++wave) {
+    if ((int)threadIdx.x / kWave == wave && (int)(threadIdx.x % kWave) < lanes)
+#pragma unroll
+      for (int k = 0; k < E; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          float* c = comb + (in + k * step) * V + j;
+          c[0] = aw[k][j] + (wave ? c[0] : 0.f);
+          c[width] = ab[k][j] + (wave ? c[width] : 0.f);
+        }
+    __syncthreads();
+  }
+  for (int i = threadIdx.x; i < M; i += kT) {
+    part[i] = comb[i];
+    part[M + i] = comb[width + i];
+  }
+}
+
+// ---- rows over several blocks ---------------------------------------------------
+constexpr int kTileVecs = 4;  // vectors of a thread that are in flight together
+
+// Sum over a block of kT threads, for every thread.
+template <int N>
+__device__ __forceinline__ void block_sum(float (&x)[N], float (*red)[kT / kWave]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
+  __syncthreads();
+  if (threadIdx.x % kWave == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) red[i][threadIdx.x / kWave] = x[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    x[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kT / kWave; ++k) x[i] += red[i][k];
+  }
+}
+
+// Forward: mean and sum of squared differences from it of one chunk of one row.
+// A tile's are exact to fp32 (the mean first), tiles are joined by the sums'
+// update for two sets: n, mean and M2 of both give n, mean and M2 of the union.
+template <typename T>
+__global__ __launch_bounds__(kT) void k_split_stats(NormPtrs a, bl_norm_desc_t d, long chunk, int chunks) {
+  constexpr int V = 16 / sizeof(T), tile = kT * V * kTileVecs;
+  __shared__ float red[1][kT / kWave];
+  const long row = blockIdx.x / (unsigned)chunks, piece = blockIdx.x % (unsigned)chunks;
+  const long from = piece * chunk, to = min((long)d.size, from + chunk);
+  const T* x = static_cast<const T*>(a.x) + row * d.x_stride;
+  float n = 0.f, mean = 0.f, m2 = 0.f;
+  for (long at = from; at < to; at += tile) {
+    Pack<T, V> v[kTileVecs];
+    float s[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < kTileVecs; ++k) {
+      const long i = at + (long)(threadIdx.x + k * kT) * V;
+      v[k] = load_part<T, V>(x + i, to - i, (T)0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < kTileVecs; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[0] += to_f32(v[k].v[j]);
+    block_sum(s, red);
+    const float nt = (float)min((long)tile, to - at), mt = s[0] / nt;
+    s[0] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kTileVecs; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float c = to_f32(v[k].v[j]) - mt;
+        s[0] += at + (long)(threadIdx.x + k * kT) * V + j < to ? c * c : 0.f;
+      }
+    block_sum(s, red);
+    const float all = n + nt, diff = mt - mean;
+    mean += diff * (nt / all);
+    m2 += s[0] + diff * diff * (n * nt / all);
+    n = all;
+  }
+  if (threadIdx.x == 0) {
+    float* o = a.sums + (size_t)blockIdx.x * 2;
+    o[0] = mean;
+    o[1] = m2;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kT) void k_split_fwd(NormPtrs a, bl_norm_desc_t d, long chunk, int chunks) {
+  constexpr int V = 16 / sizeof(T);
+  __shared__ float red[1][kT / kWave];
+  const long row = blockIdx.x / (unsigned)chunks, piece = blockIdx.x % (unsigned)chunks;
+  const long from = piece * chunk, to = min((long)d.size, from + chunk);
+  const float* sums = a.sums + (size_t)row * chunks * 2;
+  const bool mine = (int)threadIdx.x < chunks;
+  const float nc = mine ? (float)min(chunk, (long)d.size - (long)threadIdx.x * chunk) : 0.f;
+  const float mc = mine ? sums[2 * threadIdx.x] : 0.f, m2 = mine ? sums[2 * threadIdx.x + 1] : 0.f;
+  float s[1] = {nc * mc};
+  block_sum(s, red);
+  const float mean = s[0] / (float)d.size;
+  s[0] = m2 + nc * (mc - mean) * (mc - mean);
+  block_sum(s, red);
+  const float rstd = 1.f / sqrtf(s[0] / (float)d.size + (float)d.eps);
+  if (a.stats && piece == 0 && threadIdx.x == 0) {
+    a.stats[row] = mean;
+    a.stats[d.outer + row] = rstd;
+  }
+  const T* x = static_cast<const T*>(a.x) + row * d.x_stride;
+  T* y = static_cast<T*>(a.y) + row * d.y_stride;
+  const bool wide = d.wdtype == BL_F32;
+  for (long at = from; at < to; at += (long)kT * V * kTileVecs) {
+    Pack<T, V> v[kTileVecs];
+#pragma unroll
+    for (int k = 0; k < kTileVecs; ++k) {
+      const long i = at + (long)(threadIdx.x + k * kT) * V;
+      v[k] = load_part<T, V>(x + i, to - i, (T)0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < kTileVecs; ++k) {
+      const long i = at + (long)(threadIdx.x + k * kT) * V;
+      float w[V], b[V];
+      load_weights<T, V>(a.w, wide, i, to - i, 1.f, w);
+      load_weights<T, V>(a.b, wide, i, to - i, 0.f, b);
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[k].v[j] = (T)fmaf((to_f32(v[k].v[j]) - mean) * rstd, w[j], b[j]);
+      store_part<T, V>(y + i, to - i, v[k]);
+    }
+  }
+}
+
+// Backward: sums of u and u h of one chunk of one row.
+template <typename T>
+__global__ __launch_bounds__(kT) void k_split_sums(NormPtrs a, bl_norm_desc_t d, long chunk, int chunks) {
+  constexpr int V = 16 / sizeof(T);
+  __shared__ float red[2][kT / kWave];
+  const long row = blockIdx.x / (unsigned)chunks, piece = blockIdx.x % (unsigned)chunks;
+  const long from = piece * chunk, to = min((long)d.size, from + chunk);
+  const T* x = static_cast<const T*>(a.x) + row * d.x_stride;
+  const T* dy = static_cast<const T*>(a.dy) + row * d.y_stride;
+  const float mean = a.stats[row], rstd = a.stats[d.outer + row];
+  float s[2] = {0.f, 0.f};
+  for (long at = from; at < to; at += (long)kT * V * kTileVecs) {
+    Pack<T, V> v[kTileVecs], g[kTileVecs];
+#pragma unroll
+    for (int k = 0; k < kTileVecs; ++k) {
+      const long i = at + (long)(threadIdx.x + k * kT) * V;
+      v[k] = load_part<T, V>(x + i, to - i, (T)0.f);
+      g[k] = load_part<T, V>(dy + i, to - i, (T)0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < kTileVecs; ++k) {
+      const long i = at + (long)(threadIdx.x + k * kT) * V;
+      float w[V];
+      load_weights<T, V>(a.w, d.wdtype == BL_F32, i, to - i, 1.f, w);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float h = (to_f32(v[k].v[j]) - mean) * rstd, u = to_f32(g[k].v[j]) * w[j];
+        s[0] += u;
+        s[1] = fmaf(u, h, s[1]);
+      }
+    }
+  }
+  block_sum(s, red);
+  if (threadIdx.x == 0) {
+    float* o = a.sums + (size_t)blockIdx.x * 2;
+    o[0] = s[0];
+    o[1] = s[1];
+  }
+}
+
+// dx of one chunk of every groups-th row, and this block's sums by column,
+// [group][2][M].  One vector a thread, so that the sums stay in registers.
+template <typename T>
+__global__ __launch_bounds__(kT) void k_split_bwd(NormPtrs a, bl_norm_desc_t d, long chunk, int chunks,
+                                                  int groups, bool sums) {
+  constexpr int V = 16 / sizeof(T);
+  __shared__ float red[2][kT / kWave];
+  const long first = blockIdx.x / (unsigned)chunks, from = blockIdx.x % (unsigned)chunks * chunk;
+  const long to = min((long)d.size, from + chunk), M = d.size;
+  const float inv = 1.f / (float)M;
+  for (long at = from; at < to; at += (long)kT * V) {
+    const long i = at + (long)threadIdx.x * V;
+    float w[V], aw[V] = {}, ab[V] = {};
+    load_weights<T, V>(a.w, d.wdtype == BL_F32, i, to - i, 1.f, w);
+    for (long row = first; row < d.outer; row += groups) {
+      const Pack<T, V> v = load_part<T, V>(static_cast<const T*>(a.x) + row * d.x_stride + i, to - i, (T)0.f);
+      const Pack<T, V> g = load_part<T, V>(static_cast<const T*>(a.dy) + row * d.y_stride + i, to - i, (T)0.f);
+      const float* all = a.sums + (size_t)row * chunks * 2;
+      float s[2] = {0.f, 0.f};
+      if ((int)threadIdx.x < chunks) s[0] = all[2 * threadIdx.x], s[1] = all[2 * threadIdx.x + 1];
+      block_sum(s, red);
+      const float mean = a.stats[row], rstd = a.stats[d.outer + row], c1 = s[0] * inv, c2 = s[1] * inv;
+      Pack<T, V> o;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float h = (to_f32(v.v[j]) - mean) * rstd, dyj = to_f32(g.v[j]);
+        aw[j] = fmaf(dyj, h, aw[j]);
+        ab[j] += dyj;
+        o.v[j] = (T)(rstd * (fmaf(dyj, w[j], -c1) - h * c2));
+      }
+      store_part<T, V>(static_cast<T*>(a.dx) + row * d.x_stride + i, to - i, o);
+    }
+    if (!sums) continue;
+    float* part = a.part + (size_t)first * 2 * M;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (i + j < to) {
+        part[i + j] = aw[j];
+        part[M + i + j] = ab[j];
+      }
+  }
+}
+
+// How a row of nv vectors lies on lanes, `most` vectors on one at most.
+bl_norm_rows rows_shape(long nv, int most, bool backward) {
+  bl_norm_rows r{};
+  const int wave_each = backward ? 2 : 4;  // (backward: and two sums for each of a lane's values)
+  if (nv <= (long)kWave * wave_each) {
+    r.each = nv <= kWave ? 1 : nv <= 2 * kWave ? 2 : 4;
+    r.threads = 1;
+    while ((long)r.threads * r.each < nv) r.threads *= 2;
+    return r;
+  }
+  r.block = true;
+  r.each = backward ? 1 : 2;
+  r.threads = 256;
+  while ((long)r.threads * r.each < nv) {
+    if (r.each < (backward ? 2 : 4)) r.each *= 2;
+    else if (r.threads < kMostThreads) r.threads *= 2;
+    else if (r.each < most) r.each *= 2;
+    else return bl_norm_rows{true, 0, 0};  // does not fit
+  }
+  return r;
+}
+
+template <typename T, bool BLOCK>
+bl_status_t launch_fwd(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s) {
+  const bl_norm_rows& r = p->fwd;
+  const long each = BLOCK ? 1 : kT / r.threads;
+  const unsigned blocks = (unsigned)std::min<long>((p->d.outer + each - 1) / each, BLOCK ? 2 * kTargetBlocks : 4 * kTargetBlocks);
+  const double bytes = 2.0 * p->d.outer * p->d.size * sizeof(T);
+  return timed_launch("norm_fwd", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    auto go = [&](auto kernel) {
+      hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(BLOCK ? r.threads : kT), 0, s, e0, e1, 0, a, p->d, r.threads);
+    };
+    if (r.each == 1) go(k_rows_fwd<T, 1, BLOCK>);
+    else if (r.each == 2) go(k_rows_fwd<T, 2, BLOCK>);
+    else if (r.each == 4) go(k_rows_fwd<T, 4, BLOCK>);
+    else go(k_rows_fwd<T, 8, true>);
+  });
+}
+
+template <typename T, bool BLOCK>
+bl_status_t launch_bwd(const bl_norm_plan_s* p, const NormPtrs& a, bool sums, hipStream_t s) {
+  const bl_norm_rows& r = p->bwd;
+  const double bytes = 3.0 * p->d.outer * p->d.size * sizeof(T);
+  return timed_launch("norm_bwd", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    auto go = [&](auto kernel) {
+      hipExtLaunchKernelGGL(kernel, dim3(p->parts), dim3(BLOCK ? r.threads : kT), 0, s, e0, e1, 0, a, p->d, r.threads,
+                            sums);
+    };
+    if (r.each == 1) go(k_rows_bwd<T, 1, BLOCK>);
+    else if (r.each == 2) go(k_rows_bwd<T, 2, BLOCK>);
+    else go(k_rows_bwd<float, 4, true>);
+  });
+}
+
+template <typename T>
+bl_status_t forward(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s) {
+  if (!p->fwd_split) return p->fwd.block ? launch_fwd<T, true>(p, a, s) : launch_fwd<T, false>(p, a, s);
+  const dim3 grid((unsigned)(p->chunks * p->d.outer));
+  const double bytes = (double)p->d.outer * p->d.size * sizeof(T);
+  const bl_status_t st = timed_launch("norm_stats", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    hipExtLaunchKernelGGL(k_split_stats<T>, grid, dim3(kT), 0, s, e0, e1, 0, a, p->d, p->chunk, p->chunks);
+  });
+  if (st != BL_OK) return st;
+  return timed_launch("norm_fwd", 2 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    hipExtLaunchKernelGGL(k_split_fwd<T>, grid, dim3(kT), 0, s, e0, e1, 0, a, p->d, p->chunk, p->chunks);
+  });
+}
+
+template <typename T>
+bl_status_t backward(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s) {
+  const bool sums = a.dw || a.db;
+  bl_status_t st;
+  if (!p->bwd_split) {
+    st = p->bwd.block ? launch_bwd<T, true>(p, a, sums, s) : launch_bwd<T, false>(p, a, sums, s);
+  } else {
+    const double bytes = (double)p->d.outer * p->d.size * sizeof(T);
+    st = timed_launch("norm_sums", 2 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+      hipExtLaunchKernelGGL(k_split_sums<T>, dim3((unsigned)(p->chunks * p->d.outer)), dim3(kT), 0, s, e0, e1, 0, a,
+                            p->d, p->chunk, p->chunks);
+    });
+    if (st != BL_OK) return st;
+    st = timed_launch("norm_bwd", 3 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+      hipExtLaunchKernelGGL(k_split_bwd<T>, dim3((unsigned)(p->chunks * p->row_groups)), dim3(kT), 0, s, e0, e1, 0, a,
+                            p->d, p->chunk, p->chunks, p->row_groups, sums);
+    });
+  }
+  return st == BL_OK && sums ? norm_sum_parts(p, a, p->parts, s) : st;
+}
+
+}  // namespace
+
+bl_status_t norm_rows_plan(bl_norm_plan_s* p) {
+  const long rows = p->d.outer, M = p->d.size, V = 16 / dtype_bytes(p->d.dtype), nv = (M + V - 1) / V;
+  // fp32 values of x, dy, w and two sums of 32 16-bit values a lane would not fit a
+  // block of 1024's registers
+  p->fwd = rows_shape(nv, 8, false);
+  p->bwd = rows_shape(nv, p->d.dtype == BL_F32 ? 4 : 2, true);
+  p->fwd_split = !p->fwd.threads;
+  p->bwd_split = !p->bwd.threads;
+  if (p->fwd_split || p->bwd_split) {
+    const long tile = (long)kT * V * kTileVecs;
+    const long chunks = std::min<long>(kT, (M + tile - 1) / tile);
+    p->chunk = ((M + chunks - 1) / chunks + tile - 1) / tile * tile;
+    p->chunks = (int)((M + p->chunk - 1) / p->chunk);
+    if (rows * p->chunks >= kMostBlocks) return BL_ERR_UNSUPPORTED;
+    p->off_sums = 0;
+    p->bytes = round_up((size_t)rows * p->chunks * 2 * sizeof(float), 256);
+  }
+  p->off_part = p->bytes;
+  if (p->bwd_split) {
+    p->row_groups = (int)std::min<long>(rows, std::max<long>(1, kTargetBlocks / p->chunks));
+    p->parts = p->row_groups;
+  } else {
+    const long each = p->bwd.block ? 1 : kT / p->bwd.threads;
+    p->parts = (int)std::min<long>((rows + each - 1) / each, p->bwd.block && p->bwd.threads > 512 ? kTargetBlocks / 2 : kTargetBlocks);
+  }
+  p->bytes += (size_t)p->parts * 2 * M * sizeof(float);
+  return BL_OK;
+}
+
+bl_status_t norm_rows_forward(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s) {
+  if (p->d.dtype == BL_F32) return forward<float>(p, a, s);
+  if (p->d.dtype == BL_BF16) return forward<bf16_t>(p, a, s);
+  return forward<f16_t>(p, a, s);
+}
+
+bl_status_t norm_rows_backward(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s) {
+  if (p->d.dtype == BL_F32) return backward<float>(p, a, s);
+  if (p->d.dtype == BL_BF16) return backward<bf16_t>(p, a, s);
+  return backward<f16_t>(p, a, s);
+}
+
+}  // namespace blc

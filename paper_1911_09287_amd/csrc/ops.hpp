@@ -2,6 +2,8 @@
 // adamw.hip): element types, vector loads of any alignment, wave reductions.
 #pragma once
 
+#include <type_traits>
+
 #include "bltrain.h"
 #include "common.hpp"
 
@@ -52,6 +54,30 @@ __device__ __forceinline__ void store_part(T* p, long n, const Pack<T, N>& r) {
   for (int j = 0; j < N; ++j)
     if (j < n) p[j] = r.v[j];
 }
+
+// N elements as they were loaded, in 32-bit words, for kernels that keep many:
+// refresh() makes the compiler convert them again at the next use instead of
+// keeping fp32 copies in registers.
+template <typename T, int N>
+struct Held {
+  static constexpr int kWords = (N * (int)sizeof(T) + 3) / 4;
+  unsigned w[kWords];
+
+  __device__ __forceinline__ void load(const T* p, long n) {
+    const Pack<T, N> r = load_part<T, N>(p, n, (T)0.f);
+    if (N * sizeof(T) % 4) w[kWords - 1] = 0;
+    __builtin_memcpy(w, &r, sizeof(r));
+  }
+  __device__ __forceinline__ float operator[](int j) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
+    else if constexpr (std::is_same_v<T, bf16_t>) return __uint_as_float(j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+    else return (float)__builtin_bit_cast(f16_t, (unsigned short)(j & 1 ? w[j / 2] >> 16 : w[j / 2]));
+  }
+  __device__ __forceinline__ void refresh() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) asm volatile("" : "+v"(w[i]));
+  }
+};
 
 __device__ __forceinline__ float wave_sum(float x, int width = kWave) {
   for (int o = width / 2; o > 0; o >>= 1) x += __shfl_xor(x, o);
