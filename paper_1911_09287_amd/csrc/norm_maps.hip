@@ -35,9 +35,10 @@ __device__ __forceinline__ Place place_of(long tile, const bl_norm_desc_t& d, un
 template <int N, int LANES, int THREADS>
 __device__ __forceinline__ void channel_sum(float (&x)[N], float (*red)[LANES * N]) {
 #pragma unroll
-  for (int j = 0; j < N; ++j)
-#pragma unroll
-    for (int o = LANES; o < kWave; o <<= 1) x[j] += __shfl_xor(x[j], o);
+  for (int j = 0; j < N; ++j) {
+    if (LANES == 16) x[j] = add16(x[j]);
+    if (LANES <= 32) x[j] = add32(x[j]);
+  }
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % LANES, waves = THREADS / kWave;
   if ((int)(threadIdx.x % kWave) < LANES)
 #pragma unroll
@@ -68,9 +69,9 @@ __global__ __launch_bounds__(THREADS) void k_maps_fwd(NormPtrs a, bl_norm_desc_t
     float s[VEC] = {};
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
+      v[k].refresh();
 #pragma unroll
       for (int j = 0; j < VEC; ++j) s[j] += v[k][j];
-      v[k].refresh();
     }
     channel_sum<VEC, LANES, THREADS>(s, red[0]);
     float mean[VEC];
@@ -82,6 +83,7 @@ __global__ __launch_bounds__(THREADS) void k_maps_fwd(NormPtrs a, bl_norm_desc_t
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
       const bool there = group + k * groups < d.size;
+      v[k].refresh();
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const float c = there ? v[k][j] - mean[j] : 0.f;
@@ -147,6 +149,8 @@ __global__ __launch_bounds__(THREADS) void k_maps_bwd(NormPtrs a, bl_norm_desc_t
       const int c = group + k * groups;
       float w[1];
       load_weights<T, 1>(a.w, wide, c, c < d.size, 1.f, w);
+      v[k].refresh();
+      g[k].refresh();
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {  // (where there is no value dy is 0)
         const float h = (v[k][j] - mean.v[j]) * rstd.v[j], dyj = g[k][j], u = dyj * w[0];
@@ -181,11 +185,8 @@ __global__ __launch_bounds__(THREADS) void k_maps_bwd(NormPtrs a, bl_norm_desc_t
   for (int k = 0; k < EACH; ++k) {
     const int c = group + k * groups;
     if (c >= d.size) break;
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) {
-      aw[k] += __shfl_xor(aw[k], o);
-      ab[k] += __shfl_xor(ab[k], o);
-    }
+    aw[k] = wave_sum(aw[k], LANES);
+    ab[k] = wave_sum(ab[k], LANES);
     if (threadIdx.x % LANES == 0) {
       part[c] = aw[k];
       part[d.size + c] = ab[k];

@@ -26,15 +26,18 @@ __device__ __forceinline__ void row_sum(float (&x)[N], int lanes, float (*red)[k
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i], BLOCK ? kWave : lanes);
   if (!BLOCK) return;
-  const int wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+  const int wave = threadIdx.x / kWave, waves = blockDim.x / kWave;  // a multiple of 4
   if (threadIdx.x % kWave == 0)
 #pragma unroll
     for (int i = 0; i < N; ++i) red[i][wave] = x[i];
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    x[i] = red[i][0];
-    for (int k = 1; k < waves; ++k) x[i] += red[i][k];
+    x[i] = 0.f;
+    for (int k = 0; k < waves; k += 4) {
+      const float4 r = *reinterpret_cast<const float4*>(&red[i][k]);
+      x[i] += (r.x + r.y) + (r.z + r.w);
+    }
   }
 }
 
@@ -42,7 +45,7 @@ __device__ __forceinline__ void row_sum(float (&x)[N], int lanes, float (*red)[k
 template <typename T, int E, bool BLOCK>
 __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_fwd(NormPtrs a, bl_norm_desc_t d, int lanes) {
   constexpr int V = 16 / sizeof(T);
-  __shared__ float red[2][1][kMostThreads / kWave];
+  __shared__ __align__(16) float red[2][1][kMostThreads / kWave];
   const int in = BLOCK ? threadIdx.x : threadIdx.x % lanes, step = BLOCK ? blockDim.x : lanes;
   const long rows = d.outer, M = d.size;
   const long each = BLOCK ? 1 : kT / lanes;
@@ -68,15 +71,16 @@ __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_fwd(NormPtrs
     }
 #pragma unroll
     for (int k = 0; k < E; ++k) {
+      v[k].refresh();
 #pragma unroll
       for (int j = 0; j < V; ++j) s[0] += v[k][j];
-      v[k].refresh();
     }
     row_sum<BLOCK>(s, lanes, red[0]);
     const float mean = s[0] / (float)M;
     s[0] = 0.f;
 #pragma unroll
     for (int k = 0; k < E; ++k) {
+      v[k].refresh();
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float c = v[k][j] - mean;
@@ -111,7 +115,7 @@ template <typename T, int E, bool BLOCK>
 __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_bwd(NormPtrs a, bl_norm_desc_t d, int lanes,
                                                                         bool sums) {
   constexpr int V = 16 / sizeof(T);
-  __shared__ float red[2][2][kMostThreads / kWave];
+  __shared__ __align__(16) float red[2][2][kMostThreads / kWave];
   __shared__ float comb[BLOCK ? 1 : 2 * kWave * E * V];
   const int in = BLOCK ? threadIdx.x : threadIdx.x % lanes, step = BLOCK ? blockDim.x : lanes;
   const long rows = d.outer, M = d.size;
@@ -139,6 +143,8 @@ __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_bwd(NormPtrs
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < E; ++k) {
+      v[k].refresh();
+      g[k].refresh();
 #pragma unroll
       for (int j = 0; j < V; ++j) {  // (past the row dy is 0)
         const float h = (v[k][j] - mean) * rstd, dyj = g[k][j], u = dyj * w[k][j];
@@ -241,17 +247,19 @@ __global__ __launch_bounds__(kT) void k_split_stats(NormPtrs a, bl_norm_desc_t d
   const T* x = static_cast<const T*>(a.x) + row * d.x_stride;
   float n = 0.f, mean = 0.f, m2 = 0.f;
   for (long at = from; at < to; at += tile) {
-    Pack<T, V> v[kTileVecs];
+    Held<T, V> v[kTileVecs];
     float s[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k) {
       const long i = at + (long)(threadIdx.x + k * kT) * V;
-      v[k] = load_part<T, V>(x + i, to - i, (T)0.f);
+      v[k].load(x + i, to - i);
     }
 #pragma unroll
-    for (int k = 0; k < kTileVecs; ++k)
+    for (int k = 0; k < kTileVecs; ++k) {
+      v[k].refresh();
 #pragma unroll
-      for (int j = 0; j < V; ++j) s[0] += to_f32(v[k].v[j]);
+      for (int j = 0; j < V; ++j) s[0] += v[k][j];
+    }
     block_sum(s, red);
     const float nt = (float)min((long)tile, to - at), mt = s[0] / nt;
     s[0] = 0.f;
@@ -259,7 +267,7 @@ __global__ __launch_bounds__(kT) void k_split_stats(NormPtrs a, bl_norm_desc_t d
     for (int k = 0; k < kTileVecs; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float c = to_f32(v[k].v[j]) - mt;
+        const float c = v[k][j] - mt;
         s[0] += at + (long)(threadIdx.x + k * kT) * V + j < to ? c * c : 0.f;
       }
     block_sum(s, red);
@@ -299,11 +307,11 @@ __global__ __launch_bounds__(kT) void k_split_fwd(NormPtrs a, bl_norm_desc_t d, 
   T* y = static_cast<T*>(a.y) + row * d.y_stride;
   const bool wide = d.wdtype == BL_F32;
   for (long at = from; at < to; at += (long)kT * V * kTileVecs) {
-    Pack<T, V> v[kTileVecs];
+    Held<T, V> v[kTileVecs];
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k) {
       const long i = at + (long)(threadIdx.x + k * kT) * V;
-      v[k] = load_part<T, V>(x + i, to - i, (T)0.f);
+      v[k].load(x + i, to - i);
     }
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k) {
@@ -311,9 +319,11 @@ __global__ __launch_bounds__(kT) void k_split_fwd(NormPtrs a, bl_norm_desc_t d, 
       float w[V], b[V];
       load_weights<T, V>(a.w, wide, i, to - i, 1.f, w);
       load_weights<T, V>(a.b, wide, i, to - i, 0.f, b);
+      v[k].refresh();
+      Pack<T, V> o;
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[k].v[j] = (T)fmaf((to_f32(v[k].v[j]) - mean) * rstd, w[j], b[j]);
-      store_part<T, V>(y + i, to - i, v[k]);
+      for (int j = 0; j < V; ++j) o.v[j] = (T)fmaf((v[k][j] - mean) * rstd, w[j], b[j]);
+      store_part<T, V>(y + i, to - i, o);
     }
   }
 }
@@ -330,21 +340,23 @@ __global__ __launch_bounds__(kT) void k_split_sums(NormPtrs a, bl_norm_desc_t d,
   const float mean = a.stats[row], rstd = a.stats[d.outer + row];
   float s[2] = {0.f, 0.f};
   for (long at = from; at < to; at += (long)kT * V * kTileVecs) {
-    Pack<T, V> v[kTileVecs], g[kTileVecs];
+    Held<T, V> v[kTileVecs], g[kTileVecs];
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k) {
       const long i = at + (long)(threadIdx.x + k * kT) * V;
-      v[k] = load_part<T, V>(x + i, to - i, (T)0.f);
-      g[k] = load_part<T, V>(dy + i, to - i, (T)0.f);
+      v[k].load(x + i, to - i);
+      g[k].load(dy + i, to - i);
     }
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k) {
       const long i = at + (long)(threadIdx.x + k * kT) * V;
       float w[V];
       load_weights<T, V>(a.w, d.wdtype == BL_F32, i, to - i, 1.f, w);
+      v[k].refresh();
+      g[k].refresh();
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float h = (to_f32(v[k].v[j]) - mean) * rstd, u = to_f32(g[k].v[j]) * w[j];
+        const float h = (v[k][j] - mean) * rstd, u = g[k][j] * w[j];
         s[0] += u;
         s[1] = fmaf(u, h, s[1]);
       }
@@ -373,17 +385,20 @@ __global__ __launch_bounds__(kT) void k_split_bwd(NormPtrs a, bl_norm_desc_t d, 
     float w[V], aw[V] = {}, ab[V] = {};
     load_weights<T, V>(a.w, d.wdtype == BL_F32, i, to - i, 1.f, w);
     for (long row = first; row < d.outer; row += groups) {
-      const Pack<T, V> v = load_part<T, V>(static_cast<const T*>(a.x) + row * d.x_stride + i, to - i, (T)0.f);
-      const Pack<T, V> g = load_part<T, V>(static_cast<const T*>(a.dy) + row * d.y_stride + i, to - i, (T)0.f);
+      Held<T, V> v, g;
+      v.load(static_cast<const T*>(a.x) + row * d.x_stride + i, to - i);
+      g.load(static_cast<const T*>(a.dy) + row * d.y_stride + i, to - i);
       const float* all = a.sums + (size_t)row * chunks * 2;
       float s[2] = {0.f, 0.f};
       if ((int)threadIdx.x < chunks) s[0] = all[2 * threadIdx.x], s[1] = all[2 * threadIdx.x + 1];
       block_sum(s, red);
       const float mean = a.stats[row], rstd = a.stats[d.outer + row], c1 = s[0] * inv, c2 = s[1] * inv;
+      v.refresh();
+      g.refresh();
       Pack<T, V> o;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float h = (to_f32(v.v[j]) - mean) * rstd, dyj = to_f32(g.v[j]);
+        const float h = (v[j] - mean) * rstd, dyj = g[j];
         aw[j] = fmaf(dyj, h, aw[j]);
         ab[j] += dyj;
         o.v[j] = (T)(rstd * (fmaf(dyj, w[j], -c1) - h * c2));
@@ -404,7 +419,7 @@ __global__ __launch_bounds__(kT) void k_split_bwd(NormPtrs a, bl_norm_desc_t d, 
 // How a row of nv vectors lies on lanes, `most` vectors on one at most.
 bl_norm_rows rows_shape(long nv, int most, bool backward) {
   bl_norm_rows r{};
-  const int wave_each = backward ? 2 : 4;  // (backward: and two sums for each of a lane's values)
+  const int wave_each = 4;
   if (nv <= (long)kWave * wave_each) {
     r.each = nv <= kWave ? 1 : nv <= 2 * kWave ? 2 : 4;
     r.threads = 1;
@@ -451,7 +466,8 @@ bl_status_t launch_bwd(const bl_norm_plan_s* p, const NormPtrs& a, bool sums, hi
     };
     if (r.each == 1) go(k_rows_bwd<T, 1, BLOCK>);
     else if (r.each == 2) go(k_rows_bwd<T, 2, BLOCK>);
-    else go(k_rows_bwd<float, 4, true>);
+    else if (BLOCK) go(k_rows_bwd<float, 4, true>);
+    else go(k_rows_bwd<T, 4, false>);
   });
 }
 

@@ -55,18 +55,30 @@ __device__ __forceinline__ void store_part(T* p, long n, const Pack<T, N>& r) {
     if (j < n) p[j] = r.v[j];
 }
 
-// N elements as they were loaded, in 32-bit words, for kernels that keep many:
-// refresh() makes the compiler convert them again at the next use instead of
-// keeping fp32 copies in registers.
+// N elements as they were loaded, in 32-bit words, for kernels that hold many.
+// refresh() after the loads keeps conversions (and the wait for a load) out of
+// the branch that loads, so that all loads of a lane are in flight together;
+// later it makes the compiler convert again instead of keeping fp32 copies.
 template <typename T, int N>
 struct Held {
   static constexpr int kWords = (N * (int)sizeof(T) + 3) / 4;
   unsigned w[kWords];
 
+  // The first n elements at p (n <= 0: none; the others are 0).
   __device__ __forceinline__ void load(const T* p, long n) {
-    const Pack<T, N> r = load_part<T, N>(p, n, (T)0.f);
-    if (N * sizeof(T) % 4) w[kWords - 1] = 0;
-    __builtin_memcpy(w, &r, sizeof(r));
+    if (n >= N) {
+      if (N * sizeof(T) % 4) w[kWords - 1] = 0;
+      __builtin_memcpy(w, p, N * sizeof(T));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = 0;
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < n) {
+          if constexpr (sizeof(T) == 4) w[j] = __builtin_bit_cast(unsigned, p[j]);
+          else w[j / 2] |= (unsigned)__builtin_bit_cast(unsigned short, p[j]) << (16 * (j & 1));
+        }
+    }
   }
   __device__ __forceinline__ float operator[](int j) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
@@ -79,12 +91,31 @@ struct Held {
   }
 };
 
-__device__ __forceinline__ float wave_sum(float x, int width = kWave) {
-  for (int o = width / 2; o > 0; o >>= 1) x += __shfl_xor(x, o);
-  return x;
+// ---- sums over lanes ------------------------------------------------------------
+// x of the lane that DPP control CTRL names.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xF, 0xF, false));
 }
-__device__ __forceinline__ float wave_max(float x, int width = kWave) {
-  for (int o = width / 2; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+// x + x of the lane 16 (32) further or back: two copies that exchange their odd
+// and even rows of 16 (upper and lower halves of 32).
+__device__ __forceinline__ float add16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float add32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// Sum over groups of `lanes` neighbouring lanes (a power of two, the same for the
+// whole wave; every lane of a group active), for each of them.
+__device__ __forceinline__ float wave_sum(float x, int lanes = kWave) {
+  if (lanes > 1) x += dpp<0xB1>(x);   // quad_perm 1 0 3 2
+  if (lanes > 2) x += dpp<0x4E>(x);   // quad_perm 2 3 0 1
+  if (lanes > 4) x += dpp<0x141>(x);  // row_half_mirror: the other four of eight
+  if (lanes > 8) x += dpp<0x140>(x);  // row_mirror: the other eight of sixteen
+  if (lanes > 16) x = add16(x);
+  if (lanes > 32) x = add32(x);
   return x;
 }
 
