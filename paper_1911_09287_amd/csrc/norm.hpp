@@ -38,20 +38,35 @@ struct NormPtrs {
   float *part, *sums;  // workspace
 };
 
-// n weights from index i on as fp32 (`one`: without weights), fp32 or of the activations' type.
-template <typename T, int N>
-__device__ __forceinline__ void load_weights(const void* w, bool wide, long i, long n, float one, float (&out)[N]) {
+// E vectors of N weights at from, from + step, ... of M, as fp32 (`one`: without
+// weights); w holds fp32 (wide) or the activations' type.  All loads are in flight
+// before the first is waited for.
+template <typename T, int N, int E>
+__device__ __forceinline__ void load_weights(const void* w, bool wide, long from, long step, long M, float one,
+                                             float (&out)[E][N]) {
+  if (!w) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) out[j] = one;
-  if (!w) return;
-  if (wide) {
-    const Pack<float, N> p = load_part<float, N>(static_cast<const float*>(w) + i, n, 0.f);
+    for (int k = 0; k < E; ++k)
 #pragma unroll
-    for (int j = 0; j < N; ++j) out[j] = p.v[j];
+      for (int j = 0; j < N; ++j) out[k][j] = one;
+  } else if (wide) {
+    Held<float, N> r[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) r[k].load(static_cast<const float*>(w) + from + k * step, M - from - k * step);
+#pragma unroll
+    for (int k = 0; k < E; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j) out[k][j] = r[k][j];
   } else {
-    const Pack<T, N> p = load_part<T, N>(static_cast<const T*>(w) + i, n, (T)0.f);
+    Held<T, N> r[E];
 #pragma unroll
-    for (int j = 0; j < N; ++j) out[j] = to_f32(p.v[j]);
+    for (int k = 0; k < E; ++k) r[k].load(static_cast<const T*>(w) + from + k * step, M - from - k * step);
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      r[k].refresh();
+#pragma unroll
+      for (int j = 0; j < N; ++j) out[k][j] = r[k][j];
+    }
   }
 }
 

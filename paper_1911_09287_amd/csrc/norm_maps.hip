@@ -66,6 +66,9 @@ __global__ __launch_bounds__(THREADS) void k_maps_fwd(NormPtrs a, bl_norm_desc_t
     Held<T, VEC> v[EACH];
 #pragma unroll
     for (int k = 0; k < EACH; ++k, x += step) v[k].load(x, group + k * groups < d.size ? p.n : 0);
+    float w[EACH][1], b[EACH][1];
+    load_weights<T, 1, EACH>(a.w, wide, group, groups, d.size, 1.f, w);
+    load_weights<T, 1, EACH>(a.b, wide, group, groups, d.size, 0.f, b);
     float s[VEC] = {};
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
@@ -98,12 +101,9 @@ __global__ __launch_bounds__(THREADS) void k_maps_fwd(NormPtrs a, bl_norm_desc_t
     for (int k = 0; k < EACH; ++k, y += step) {
       const int c = group + k * groups;
       if (c >= d.size) break;
-      float w[1], b[1];
-      load_weights<T, 1>(a.w, wide, c, 1, 1.f, w);
-      load_weights<T, 1>(a.b, wide, c, 1, 0.f, b);
       Pack<T, VEC> o;
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) o.v[j] = (T)fmaf((v[k][j] - mean[j]) * s[j], w[0], b[0]);
+      for (int j = 0; j < VEC; ++j) o.v[j] = (T)fmaf((v[k][j] - mean[j]) * s[j], w[k][0], b[k][0]);
       store_part<T, VEC>(y, p.n, o);
     }
     if (a.stats && group == 0)
@@ -126,7 +126,8 @@ __global__ __launch_bounds__(THREADS) void k_maps_bwd(NormPtrs a, bl_norm_desc_t
   const bool wide = d.wdtype == BL_F32;
   const long sites = d.outer * d.inner, step = groups * d.inner;
   const float inv = 1.f / (float)d.size;
-  float aw[EACH] = {}, ab[EACH] = {};
+  float w[EACH][1], aw[EACH] = {}, ab[EACH] = {};
+  load_weights<T, 1, EACH>(a.w, wide, group, groups, d.size, 1.f, w);
   int turn = 0;
   for (long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const Place p = place_of<VEC, LANES>(tile, d, per_slice);
@@ -146,14 +147,11 @@ __global__ __launch_bounds__(THREADS) void k_maps_bwd(NormPtrs a, bl_norm_desc_t
     float s[2 * VEC] = {};
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
-      const int c = group + k * groups;
-      float w[1];
-      load_weights<T, 1>(a.w, wide, c, c < d.size, 1.f, w);
       v[k].refresh();
       g[k].refresh();
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {  // (where there is no value dy is 0)
-        const float h = (v[k][j] - mean.v[j]) * rstd.v[j], dyj = g[k][j], u = dyj * w[0];
+        const float h = (v[k][j] - mean.v[j]) * rstd.v[j], dyj = g[k][j], u = dyj * w[k][0];
         s[2 * j] += u;
         s[2 * j + 1] = fmaf(u, h, s[2 * j + 1]);
         aw[k] = fmaf(dyj, h, aw[k]);
@@ -168,13 +166,11 @@ __global__ __launch_bounds__(THREADS) void k_maps_bwd(NormPtrs a, bl_norm_desc_t
     for (int k = 0; k < EACH; ++k, dx += step) {
       const int c = group + k * groups;
       if (c >= d.size) break;
-      float w[1];
-      load_weights<T, 1>(a.w, wide, c, 1, 1.f, w);
       Pack<T, VEC> o;
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const float h = (v[k][j] - mean.v[j]) * rstd.v[j];
-        o.v[j] = (T)(rstd.v[j] * (fmaf(g[k][j], w[0], -s[2 * j] * inv) - h * (s[2 * j + 1] * inv)));
+        o.v[j] = (T)(rstd.v[j] * (fmaf(g[k][j], w[k][0], -s[2 * j] * inv) - h * (s[2 * j + 1] * inv)));
       }
       store_part<T, VEC>(dx, p.n, o);
     }
@@ -224,10 +220,10 @@ __global__ __launch_bounds__(kStreamThreads) void k_maps_fwd_stream(NormPtrs a, 
     const float rstd = 1.f / sqrtf(s[0] / (float)d.size + (float)d.eps);
     if (!p.n) continue;
     for (long c = group; c < d.size; c += groups) {
-      float w[1], b[1];
-      load_weights<T, 1>(a.w, wide, c, 1, 1.f, w);
-      load_weights<T, 1>(a.b, wide, c, 1, 0.f, b);
-      y[c * d.inner] = (T)fmaf((to_f32(x[c * d.inner]) - mean) * rstd, w[0], b[0]);
+      float w[1][1], b[1][1];
+      load_weights<T, 1, 1>(a.w, wide, c, 0, d.size, 1.f, w);
+      load_weights<T, 1, 1>(a.b, wide, c, 0, d.size, 0.f, b);
+      y[c * d.inner] = (T)fmaf((to_f32(x[c * d.inner]) - mean) * rstd, w[0][0], b[0][0]);
     }
     if (a.stats && group == 0) {
       a.stats[p.outer * d.inner + p.at] = mean;
@@ -255,9 +251,9 @@ __global__ __launch_bounds__(kStreamThreads) void k_maps_bwd_stream(NormPtrs a, 
     float s[2] = {};
     if (p.n)
       for (long c = group; c < d.size; c += groups) {
-        float w[1];
-        load_weights<T, 1>(a.w, wide, c, 1, 1.f, w);
-        const float u = to_f32(dy[c * d.inner]) * w[0];
+        float w[1][1];
+        load_weights<T, 1, 1>(a.w, wide, c, 0, d.size, 1.f, w);
+        const float u = to_f32(dy[c * d.inner]) * w[0][0];
         s[0] += u;
         s[1] = fmaf(u, (to_f32(x[c * d.inner]) - mean) * rstd, s[1]);
       }
@@ -265,12 +261,12 @@ __global__ __launch_bounds__(kStreamThreads) void k_maps_bwd_stream(NormPtrs a, 
     turn ^= 1;
     const float c1 = s[0] / (float)d.size, c2 = s[1] / (float)d.size;
     for (long c = group; c < d.size; c += groups) {
-      float w[1], h = 0.f, g = 0.f;
-      load_weights<T, 1>(a.w, wide, c, 1, 1.f, w);
+      float w[1][1], h = 0.f, g = 0.f;
+      load_weights<T, 1, 1>(a.w, wide, c, 0, d.size, 1.f, w);
       if (p.n) {
         h = (to_f32(x[c * d.inner]) - mean) * rstd;
         g = to_f32(dy[c * d.inner]);
-        dx[c * d.inner] = (T)(rstd * (fmaf(g, w[0], -c1) - h * c2));
+        dx[c * d.inner] = (T)(rstd * (fmaf(g, w[0][0], -c1) - h * c2));
       }
       if (!sums) continue;
       const float dw = wave_sum(g * h), db = wave_sum(g);
@@ -312,7 +308,7 @@ long tiles_of(const bl_norm_desc_t& d, int vec, int lanes, unsigned* per_slice) 
 
 template <typename T, bool BACKWARD, typename Go>
 bl_status_t dispatch(const bl_norm_plan_s* p, Go&& go) {
-  constexpr int full = (BACKWARD ? 8 : 16) / sizeof(T), lanes = BACKWARD ? 32 : 16;
+  constexpr int full = (BACKWARD ? 8 : 16) / sizeof(T), lanes = 16;
   const int vec = p->map_vec[BACKWARD], on = p->map_lanes[BACKWARD], each = p->map_each[BACKWARD];
   const int threads = p->map_threads[BACKWARD];
 #define BL_MAPS(V, L, E, N)                                            \
@@ -328,7 +324,6 @@ bl_status_t dispatch(const bl_norm_plan_s* p, Go&& go) {
   BL_MAPS5(full, lanes);
   BL_MAPS5(1, 64);
   BL_MAPS(1, 16, 16, 1024);
-  if constexpr (BACKWARD) { BL_MAPS(full, 16, 16, 1024); }
 #undef BL_MAPS5
 #undef BL_MAPS
   return BL_ERR_INVALID_ARG;
@@ -378,7 +373,7 @@ bl_status_t backward(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s) 
 
 bl_status_t norm_maps_plan(bl_norm_plan_s* p) {
   const int wide = dtype_bytes(p->d.dtype);
-  const Shape f = maps_shape(p->d, 16 / wide, 16), b = maps_shape(p->d, 8 / wide, 32);
+  const Shape f = maps_shape(p->d, 16 / wide, 16), b = maps_shape(p->d, 8 / wide, 16);
   const Shape both[2] = {f, b};
   for (int i = 0; i < 2; ++i) {
     p->map_threads[i] = both[i].threads;

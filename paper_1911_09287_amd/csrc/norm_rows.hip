@@ -50,15 +50,12 @@ __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_fwd(NormPtrs
   const long rows = d.outer, M = d.size;
   const long each = BLOCK ? 1 : kT / lanes;
   const bool wide = d.wdtype == BL_F32;
-  constexpr bool keep = E * V <= 16;
+  constexpr bool keep = E * V <= 32;
   float w[keep ? E : 1][V], b[keep ? E : 1][V];
-  if (keep)
-#pragma unroll
-    for (int k = 0; k < E; ++k) {
-      const long i = (long)(in + k * step) * V;
-      load_weights<T, V>(a.w, wide, i, M - i, 1.f, w[k]);
-      load_weights<T, V>(a.b, wide, i, M - i, 0.f, b[k]);
-    }
+  if constexpr (keep) {
+    load_weights<T, V, E>(a.w, wide, (long)in * V, (long)step * V, M, 1.f, w);
+    load_weights<T, V, E>(a.b, wide, (long)in * V, (long)step * V, M, 0.f, b);
+  }
   for (long row = blockIdx.x * each + (BLOCK ? 0 : threadIdx.x / lanes); row < rows; row += gridDim.x * each) {
     const T* x = static_cast<const T*>(a.x) + row * d.x_stride;
     T* y = static_cast<T*>(a.y) + row * d.y_stride;
@@ -94,9 +91,9 @@ __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_fwd(NormPtrs
     for (int k = 0; k < E; ++k) {
       const long i = (long)(in + k * step) * V;
       const int at = keep ? k : 0;
-      if (!keep) {
-        load_weights<T, V>(a.w, wide, i, M - i, 1.f, w[0]);
-        load_weights<T, V>(a.b, wide, i, M - i, 0.f, b[0]);
+      if constexpr (!keep) {
+        load_weights<T, V, 1>(a.w, wide, i, 0, M, 1.f, w);
+        load_weights<T, V, 1>(a.b, wide, i, 0, M, 0.f, b);
       }
       Pack<T, V> o;
 #pragma unroll
@@ -122,11 +119,7 @@ __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_bwd(NormPtrs
   const long each = BLOCK ? 1 : kT / lanes;
   const float inv = 1.f / (float)M;
   float w[E][V], aw[E][V] = {}, ab[E][V] = {};
-#pragma unroll
-  for (int k = 0; k < E; ++k) {
-    const long i = (long)(in + k * step) * V;
-    load_weights<T, V>(a.w, d.wdtype == BL_F32, i, M - i, 1.f, w[k]);
-  }
+  load_weights<T, V, E>(a.w, d.wdtype == BL_F32, (long)in * V, (long)step * V, M, 1.f, w);
   int turn = 0;
   for (long row = blockIdx.x * each + (BLOCK ? 0 : threadIdx.x / lanes); row < rows; row += gridDim.x * each) {
     const T* x = static_cast<const T*>(a.x) + row * d.x_stride;
@@ -313,16 +306,16 @@ __global__ __launch_bounds__(kT) void k_split_fwd(NormPtrs a, bl_norm_desc_t d, 
       const long i = at + (long)(threadIdx.x + k * kT) * V;
       v[k].load(x + i, to - i);
     }
+    float w[kTileVecs][V], b[kTileVecs][V];
+    load_weights<T, V, kTileVecs>(a.w, wide, at + (long)threadIdx.x * V, kT * V, to, 1.f, w);
+    load_weights<T, V, kTileVecs>(a.b, wide, at + (long)threadIdx.x * V, kT * V, to, 0.f, b);
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k) {
       const long i = at + (long)(threadIdx.x + k * kT) * V;
-      float w[V], b[V];
-      load_weights<T, V>(a.w, wide, i, to - i, 1.f, w);
-      load_weights<T, V>(a.b, wide, i, to - i, 0.f, b);
       v[k].refresh();
       Pack<T, V> o;
 #pragma unroll
-      for (int j = 0; j < V; ++j) o.v[j] = (T)fmaf((v[k][j] - mean) * rstd, w[j], b[j]);
+      for (int j = 0; j < V; ++j) o.v[j] = (T)fmaf((v[k][j] - mean) * rstd, w[k][j], b[k][j]);
       store_part<T, V>(y + i, to - i, o);
     }
   }
@@ -347,16 +340,15 @@ __global__ __launch_bounds__(kT) void k_split_sums(NormPtrs a, bl_norm_desc_t d,
       v[k].load(x + i, to - i);
       g[k].load(dy + i, to - i);
     }
+    float w[kTileVecs][V];
+    load_weights<T, V, kTileVecs>(a.w, d.wdtype == BL_F32, at + (long)threadIdx.x * V, kT * V, to, 1.f, w);
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k) {
-      const long i = at + (long)(threadIdx.x + k * kT) * V;
-      float w[V];
-      load_weights<T, V>(a.w, d.wdtype == BL_F32, i, to - i, 1.f, w);
       v[k].refresh();
       g[k].refresh();
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float h = (v[k][j] - mean) * rstd, u = g[k][j] * w[j];
+        const float h = (v[k][j] - mean) * rstd, u = g[k][j] * w[k][j];
         s[0] += u;
         s[1] = fmaf(u, h, s[1]);
       }
@@ -382,8 +374,8 @@ __global__ __launch_bounds__(kT) void k_split_bwd(NormPtrs a, bl_norm_desc_t d, 
   const float inv = 1.f / (float)M;
   for (long at = from; at < to; at += (long)kT * V) {
     const long i = at + (long)threadIdx.x * V;
-    float w[V], aw[V] = {}, ab[V] = {};
-    load_weights<T, V>(a.w, d.wdtype == BL_F32, i, to - i, 1.f, w);
+    float w[1][V], aw[V] = {}, ab[V] = {};
+    load_weights<T, V, 1>(a.w, d.wdtype == BL_F32, i, 0, to, 1.f, w);
     for (long row = first; row < d.outer; row += groups) {
       Held<T, V> v, g;
       v.load(static_cast<const T*>(a.x) + row * d.x_stride + i, to - i);
@@ -401,7 +393,7 @@ __global__ __launch_bounds__(kT) void k_split_bwd(NormPtrs a, bl_norm_desc_t d, 
         const float h = (v[j] - mean) * rstd, dyj = g[j];
         aw[j] = fmaf(dyj, h, aw[j]);
         ab[j] += dyj;
-        o.v[j] = (T)(rstd * (fmaf(dyj, w[j], -c1) - h * c2));
+        o.v[j] = (T)(rstd * (fmaf(dyj, w[0][j], -c1) - h * c2));
       }
       store_part<T, V>(static_cast<T*>(a.dx) + row * d.x_stride + i, to - i, o);
     }
