@@ -18,10 +18,9 @@ struct bl_norm_plan_s {
   int chunks;                // split: blocks a row
   long chunk;                // split: elements of one, a multiple of its tile
   int row_groups;            // split backward: blocks a chunk, over rows
-  int map_threads[2];        // inner > 1, forward and backward: threads of a block,
-  int map_vec[2];            //   positions of a thread, lanes along positions and
-  int map_lanes[2];          //   channels of a thread (0: the channels are read again
-  int map_each[2];           //   for every use)
+  // inner > 1, forward and backward: threads of a block, positions of a thread,
+  // lanes along positions and channels of a thread (0: read again for every use)
+  int map_threads[2], map_vec[2], map_lanes[2], map_each[2];
   int parts;                 // backward: partial sums of dw and db, [parts][2][size]
   size_t off_part, off_sums, bytes;
 };

@@ -80,6 +80,13 @@ struct Held {
         }
     }
   }
+  // All of them at `bytes` from a pointer that the whole wave shares (one address
+  // register), or zeros.
+  __device__ __forceinline__ void load_at(const T* p, unsigned bytes, bool there) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+    if (there) __builtin_memcpy(w, reinterpret_cast<const char*>(p) + (size_t)bytes, N * sizeof(T));
+  }
   __device__ __forceinline__ float operator[](int j) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
     else if constexpr (std::is_same_v<T, bf16_t>) return __uint_as_float(j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);

@@ -54,7 +54,9 @@ ROWS = [(1, 1, 1), (3, 1, 1), (3, 5, 1), (5, 7, 1), (2, 63, 1), (2, 64, 1), (9, 
         (3, 255, 1), (4, 257, 1), (3, 1000, 1), (2, 1025, 1), (7, 2047, 1), (3, 4099, 1), (2, 8192, 1), (3, 16385, 1),
         (2, 33000, 1), (1, 65537, 1), (2, 200704, 1), (1, 262144, 1), (600, 768, 1), (4000, 64, 1), (513, 2050, 1)]
 MAPS = [(2, 3, 2), (4, 1, 33), (3, 5, 7), (2, 33, 49), (2, 128, 16), (1, 256, 270), (3, 512, 16), (2, 64, 56 * 56),
-        (2, 1024, 9), (1, 1500, 6), (1, 2100, 40), (5, 17, 3), (70, 128, 4), (2, 130, 513), (64, 100, 25)]
+        (2, 1024, 9), (1, 1500, 6), (1, 2100, 40), (5, 17, 3), (70, 128, 4), (2, 130, 513), (64, 100, 25),
+        (2, 300, 9), (1, 513, 5), (1, 300, 6), (2, 700, 6), (1, 270, 130), (1, 600, 4), (2, 1024, 12), (3, 65, 35),
+        (1, 40, 7)]
 
 
 def norm_reference(x, w, b, dy, eps):
