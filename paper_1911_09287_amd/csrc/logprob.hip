@@ -1,101 +1,416 @@
 // Log probabilities of given classes, entropies and likeliest classes of rows of
 // logits, and the gradient of the logits.
+//
+// Forward: a row of up to 2048 classes lies in the registers of a wave, a longer one
+// is cut in pieces of up to 8192, each in the registers of a block; the logits are
+// read once.  A lane takes its own largest logit m and sums a = sum e^(z - m) and
+// b = sum e^(z - m) (z - m); two such triples over sets of classes join to one
+// (m' = max, a' = a e^(m - m'), b' = e^(m - m') (b + (m - m') a), added), over lanes,
+// waves and pieces, in an order that sizes alone decide.  log q_t = z_t - m - log a and
+// the entropy log a - b / a come from the row's.  Bound by HBM, in 16 bits nearly by
+// the exponentials.
+//
+// The `top` likeliest: a value and its class make one key of 64 bits whose order is
+// the wanted one.  Of the lanes' largest values (of 64 groups of lanes) the top-th
+// bounds the answer from below, so that few values are left; these go to LDS and one
+// wave sorts them, 64 keys on its lanes, by a bitonic network.  Where more are left
+// than there is room for (many equal values), or the row holds NaN, the waves take
+// 64 keys after another and join them to a sorted list.  Pieces leave their `top` keys
+// for a second launch that joins them.
+#include <algorithm>
 #include <new>
 
 #include "ops.hpp"
 
 struct bl_logprob_plan_s {
   bl_logprob_desc_t d;
+  int each;          // vectors of 16 bytes of a lane: 1, 2, 4 or 8
+  bool block;        // a piece by a block (else a row by a wave)
+  int pieces;        // of a row
+  long piece;        // classes of one
+  size_t off_sums, bytes;  // workspace: keys of the pieces, then their (m, a, b)
 };
 
 namespace blc {
 namespace {
 
 constexpr int kT = 256;
+constexpr int kWaves = kT / kWave;
+constexpr int kRoom = 512;  // keys that are left after the bound, for which LDS has room
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
+using u64 = unsigned long long;
 
-// A value and its class as one number: larger values first, then lower classes;
-// -0 as 0, NaN above every number.
-__device__ unsigned long long order_key(float z, unsigned j) {
-  z += 0.f;
-  unsigned u = __float_as_uint(z);
-  u = z != z ? 0xFFFFFFFFu : u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
-  return ((unsigned long long)u << 32) | (0xFFFFFFFFu - j);
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// ---- keys -----------------------------------------------------------------------
+// A value as a number of the same order: -0 as 0, NaN above all others.
+__device__ __forceinline__ unsigned order_of(float z) {
+  const unsigned u = __float_as_uint(z + 0.f);
+  return z != z ? 0xFFFFFFFFu : u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(unsigned o) {
+  return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu));  // (all ones is a NaN)
+}
+// Larger values first, then lower classes.  No key is 0.
+__device__ __forceinline__ u64 key_of(float z, unsigned j) { return (u64)order_of(z) << 32 | (0xFFFFFFFFu - j); }
+
+// x of the lane whose number differs in bit J.
+template <int J>
+__device__ __forceinline__ unsigned lane_xor(unsigned x) {
+  if constexpr (J == 1) return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, false);
+  if constexpr (J == 2) return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, false);
+  if constexpr (J == 4) {  // reversed within eights, then within fours
+    const int r = __builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, false);
+    return (unsigned)__builtin_amdgcn_update_dpp(0, r, 0x1B, 0xF, 0xF, false);
+  }
+  if constexpr (J == 8) return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, false);
+  if constexpr (J == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  }
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return threadIdx.x & 32 ? r[0] : r[1];
+}
+template <int J>
+__device__ __forceinline__ u64 lane_xor(u64 x) {
+  return (u64)lane_xor<J>((unsigned)(x >> 32)) << 32 | lane_xor<J>((unsigned)x);
+}
+// One step of a bitonic network: lanes that differ in bit J exchange; the larger
+// goes to the lower one where `falling`.
+template <int J, typename K>
+__device__ __forceinline__ K exchange(K x, bool falling) {
+  const K y = lane_xor<J>(x);
+  const bool lower = !(threadIdx.x & J);
+  return (lower == falling) == (y > x) ? y : x;
+}
+// Falling order over the wave of values that rise and then fall (or the reverse).
+template <typename K>
+__device__ __forceinline__ K merge64(K x) {
+  x = exchange<32>(x, true);
+  x = exchange<16>(x, true);
+  x = exchange<8>(x, true);
+  x = exchange<4>(x, true);
+  x = exchange<2>(x, true);
+  return exchange<1>(x, true);
+}
+// Falling order over the wave.
+template <typename K>
+__device__ __forceinline__ K sort64(K x) {
+  const unsigned l = threadIdx.x;
+  x = exchange<1>(x, !(l & 2));
+  x = exchange<2>(x, !(l & 4));
+  x = exchange<1>(x, !(l & 4));
+  x = exchange<4>(x, !(l & 8));
+  x = exchange<2>(x, !(l & 8));
+  x = exchange<1>(x, !(l & 8));
+  x = exchange<8>(x, !(l & 16));
+  x = exchange<4>(x, !(l & 16));
+  x = exchange<2>(x, !(l & 16));
+  x = exchange<1>(x, !(l & 16));
+  x = exchange<16>(x, !(l & 32));
+  x = exchange<8>(x, !(l & 32));
+  x = exchange<4>(x, !(l & 32));
+  x = exchange<2>(x, !(l & 32));
+  x = exchange<1>(x, !(l & 32));
+  return merge64(x);
+}
+// The 64 largest of two lists in falling order, in falling order.
+__device__ __forceinline__ u64 join64(u64 a, u64 b) {
+  b = lane_xor<1>(lane_xor<2>(lane_xor<4>(lane_xor<8>(lane_xor<16>(lane_xor<32>(b))))));  // reversed
+  return merge64(a > b ? a : b);
+}
+__device__ __forceinline__ u64 lane_value(u64 x, int lane) {
+  return (u64)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 |
+         (unsigned)__builtin_amdgcn_readlane((int)(unsigned)x, lane);
+}
+// Joins 64 keys in any order (0: none) to a list whose top-th is `last`.
+__device__ __forceinline__ void take64(u64 x, int top, u64& list, u64& last) {
+  if (!__ballot(x > last)) return;
+  list = join64(list, sort64(x));
+  last = lane_value(list, top - 1);
 }
 
-template <typename V, typename Op>
-__device__ V block_reduce(V x, V* red, Op op) {
-  for (int o = 32; o > 0; o >>= 1) x = op(x, __shfl_xor(x, o));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = red[0];
-  for (int w = 1; w < kT / 64; ++w) x = op(x, red[w]);
-  return x;
+// ---- softmax statistics -----------------------------------------------------------
+// Largest value m, a = sum 2^t and b = sum 2^t t with t = (z - m) log2 e.
+struct Sums {
+  float m, a, b;
+};
+// The same sums relative to m2 >= m.
+__device__ __forceinline__ Sums rebased(Sums s, float m2) {
+  if (s.m == m2) return s;
+  // (bounded: of values that far below 2^t is 0, and 0 times infinity is not)
+  const float t = fmaxf((s.m - m2) * kLog2e, -1000.f), f = exp2_(t);
+  return Sums{m2, s.a * f, f * fmaf(t, s.a, s.b)};
+}
+__device__ __forceinline__ Sums over_wave(Sums s) {
+  s = rebased(s, wave_max(s.m));
+  return Sums{s.m, wave_sum(s.a), wave_sum(s.b)};
+}
+__device__ __forceinline__ Sums joined(Sums p, Sums q) {
+  const float m = fmaxf(p.m, q.m);
+  p = rebased(p, m);
+  q = rebased(q, m);
+  return Sums{m, p.a + q.a, p.b + q.b};
+}
+
+// What a row's results follow from.
+struct Row {
+  float base, log_sum;  // log q_j = z_j - base - log_sum
+  bool none;            // every class is ruled out
+  __device__ Row(const Sums& s) {
+    none = s.m == -INFINITY && s.a == 0.f;  // (a is NaN where there is a NaN)
+    base = s.m == -INFINITY ? 0.f : s.m;
+    log_sum = logf(s.a);
+  }
+};
+
+struct Ptrs {
+  const void* logits;
+  const long long* targets;
+  float *logp, *stats, *top_logp;
+  long long* top_index;
+  u64* keys;    // [row][piece][top]
+  float* sums;  // [row][piece][3]
+};
+
+// One lane writes a row's logp and stats.
+template <typename T>
+__device__ __forceinline__ void write_row(const Ptrs& a, const bl_logprob_desc_t& d, long row, const Sums& s,
+                                          const Row& r) {
+  const long long t = a.targets ? a.targets[row] : -1;
+  if (a.logp) {
+    float x = 0.f;
+    if (t >= 0 && t < d.classes)
+      x = r.none ? -INFINITY : to_f32(static_cast<const T*>(a.logits)[row * d.stride + t]) - r.base - r.log_sum;
+    a.logp[row] = x;
+  }
+  if (a.stats) {
+    a.stats[row] = s.m;
+    a.stats[d.rows + row] = r.log_sum;
+    a.stats[2 * d.rows + row] = r.none ? 0.f : r.log_sum - s.b * kLn2 / s.a;
+  }
+}
+// A wave writes a row's likeliest classes from its list.
+__device__ __forceinline__ void write_top(const Ptrs& a, const bl_logprob_desc_t& d, long row, const Row& r, u64 list) {
+  const int i = threadIdx.x % kWave;
+  if (i >= d.top) return;
+  const long at = row * d.top + i;
+  a.top_index[at] = list ? (long long)(0xFFFFFFFFu - (unsigned)list) : -1;
+  a.top_logp[at] = !list || r.none ? -INFINITY : value_of((unsigned)(list >> 32)) - r.base - r.log_sum;
 }
 
 template <typename T>
-__global__ void k_logprob_fwd(const T* logits, const long long* targets, float* logp, float* stats, float* top_logp,
-                              long long* top_index, bl_logprob_desc_t d) {
-  __shared__ float redf[kT / 64];
-  __shared__ unsigned long long redk[kT / 64];
-  const long row = blockIdx.x;
-  const T* z = logits + row * d.stride;
-  auto add = [](float a, float b) { return a + b; };
-  auto large = [](float a, float b) { return fmaxf(a, b); };
-  float m = -INFINITY;
-  for (long j = threadIdx.x; j < d.classes; j += kT) m = fmaxf(m, to_f32(z[j]));
-  m = block_reduce(m, redf, large);
-  const float base = m == -INFINITY ? 0.f : m;
-  float a = 0.f, b = 0.f;
-  for (long j = threadIdx.x; j < d.classes; j += kT) {
-    const float t = to_f32(z[j]) - base, e = expf(t);
-    a += e;
-    if (e != 0.f) b += e * t;
-  }
-  a = block_reduce(a, redf, add);
-  b = block_reduce(b, redf, add);
-  const bool none = m == -INFINITY && a == 0.f;  // (a NaN beside it is not ruled out)
-  const float log_sum = logf(a);
-  if (threadIdx.x == 0) {
-    const long long t = targets ? targets[row] : -1;
-    const bool there = t >= 0 && t < d.classes;
-    if (logp) logp[row] = !there ? 0.f : none ? -INFINITY : to_f32(z[t]) - base - log_sum;
-    if (stats) {
-      stats[row] = m;
-      stats[d.rows + row] = log_sum;
-      stats[2 * d.rows + row] = none ? 0.f : log_sum - b / a;
+constexpr unsigned kMinusInf = sizeof(T) == 4 ? 0xFF800000u : std::is_same_v<T, bf16_t> ? 0xFF80FF80u : 0xFC00FC00u;
+
+template <int WAVES>
+__device__ __forceinline__ void part_sync() {  // over the waves that work on one piece
+  if (WAVES == 1) wave_sync();
+  else __syncthreads();
+}
+
+// Pieces of rows (WAVES = 1: whole rows), E vectors a lane.  With `pieces` > 1 each
+// leaves its sums and keys, else it gives the row's results.
+template <typename T, int E, int WAVES, bool TOP>
+__global__ __launch_bounds__(kT) void k_logprob_fwd(Ptrs a, bl_logprob_desc_t d, int pieces, long piece) {
+  constexpr int V = 16 / sizeof(T), kParts = kWaves / WAVES;  // pieces of a block at a time
+  __shared__ u64 room[kParts][TOP ? (WAVES == 1 ? kRoom / 2 : kRoom) : 1];
+  __shared__ unsigned largest[kParts][TOP ? WAVES * kWave : 1];
+  __shared__ int left[kParts];
+  __shared__ Sums wave_sums[WAVES];
+  const int part = WAVES == 1 ? threadIdx.x / kWave : 0, in = WAVES == 1 ? threadIdx.x % kWave : threadIdx.x;
+  const int lane = threadIdx.x % kWave, wave = in / kWave;
+  const unsigned long long count = (unsigned long long)d.rows * pieces;
+  for (unsigned long long q = (unsigned long long)blockIdx.x * kParts + part; q < count;
+       q += (unsigned long long)gridDim.x * kParts) {
+    const long row = pieces == 1 ? (long)q : (long)(q / (unsigned)pieces);
+    const long from = pieces == 1 ? 0 : (long)(q % (unsigned)pieces) * piece;
+    const int len = (int)min(piece, (long)d.classes - from);
+    const T* z = static_cast<const T*>(a.logits) + row * d.stride + from;
+    Held<T, V> v[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      const int i = (in + k * WAVES * kWave) * V;
+      v[k].load(z + i, len - i, kMinusInf<T>);
     }
-  }
-  auto larger = [](unsigned long long a, unsigned long long b) { return a > b ? a : b; };
-  unsigned long long last = ~0ull;
-  for (int k = 0; k < d.top; ++k) {
-    unsigned long long best = 0;
-    for (long j = threadIdx.x; j < d.classes; j += kT) {
-      const unsigned long long key = order_key(to_f32(z[j]), (unsigned)j);
-      if (key < last && key > best) best = key;
+    Sums s{-INFINITY, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      v[k].refresh();
+#pragma unroll
+      for (int j = 0; j < V; ++j) s.m = fmaxf(s.m, v[k][j]);
     }
-    last = block_reduce(best, redk, larger);
-    if (threadIdx.x == 0) {
-      const long j = last ? (long)(0xFFFFFFFFu - (unsigned)last) : -1;
-      top_index[row * d.top + k] = j;
-      top_logp[row * d.top + k] = j < 0 || none ? -INFINITY : to_f32(z[j]) - base - log_sum;
+    if (TOP) {
+      largest[part][in] = order_of(s.m);
+      if (in == 0) left[part] = 0;
     }
+    const float base = s.m == -INFINITY ? 0.f : s.m;
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      v[k].refresh();
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float t = (v[k][j] - base) * kLog2e, e = exp2_(t);
+        s.a += e;
+        s.b = fmaf(e, fmaxf(t, -1000.f), s.b);  // (t = -infinity: e is 0)
+      }
+    }
+    s = over_wave(s);
+    if (WAVES > 1 && lane == 0) wave_sums[wave] = s;
+    part_sync<WAVES>();
+    if (WAVES > 1) {
+      s = wave_sums[0];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) s = joined(s, wave_sums[w]);
+    }
+    const Row r(s);
+    u64 list = 0, last = 0;
+    if (TOP) {
+      // the top-th of 64 groups' largest values is a bound from below
+      unsigned o = largest[part][lane];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) o = max(o, largest[part][lane + w * kWave]);
+      const float bound = value_of((unsigned)__builtin_amdgcn_readlane((int)sort64(o), d.top - 1));
+      constexpr int kMost = WAVES == 1 ? kRoom / 2 : kRoom;
+      bool whole = s.a == s.a;  // no NaN
+      if (whole) {
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+          v[k].refresh();
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const float zj = v[k][j];
+            const int i = (in + k * WAVES * kWave) * V + j;
+            const u64 pass = __ballot(zj >= bound && i < len);
+            if (pass) {
+              int at = 0;
+              if (lane == 0) at = atomicAdd(&left[part], __popcll(pass));
+              at = __builtin_amdgcn_readfirstlane(at) +
+                   __builtin_amdgcn_mbcnt_hi((unsigned)(pass >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)pass, 0));
+              if ((pass >> lane & 1) && at < kMost) room[part][at] = key_of(zj, (unsigned)(from + i));
+            }
+          }
+        }
+      }
+      part_sync<WAVES>();
+      const int n = left[part];
+      whole = whole && n <= kMost;
+      if (whole) {
+        if (wave == 0)
+          for (int i = lane; i - lane < n; i += kWave) take64(i < n ? room[part][i] : 0, d.top, list, last);
+      } else {  // 64 by 64, the waves in turn; then their lists
+        for (int i = in; i - lane < len; i += 4 * WAVES * kWave) {
+          float zi[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) zi[u] = i + u * WAVES * kWave < len ? to_f32(z[i + u * WAVES * kWave]) : 0.f;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int iu = i + u * WAVES * kWave;
+            take64(iu < len ? key_of(zi[u], (unsigned)(from + iu)) : 0, d.top, list, last);
+          }
+        }
+        if (WAVES > 1) {
+          __syncthreads();  // `left` has been read
+          room[0][in] = list;
+          __syncthreads();
+          if (wave == 0)
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) list = join64(list, room[0][w * kWave + lane]);
+        }
+      }
+    }
+    if (wave == 0) {
+      if (pieces == 1) {
+        if (lane == 0) write_row<T>(a, d, row, s, r);
+        if (TOP) write_top(a, d, row, r, list);
+      } else {
+        if (lane < 3) a.sums[q * 3 + lane] = lane == 0 ? s.m : lane == 1 ? s.a : s.b;
+        if (TOP && lane < d.top) a.keys[q * d.top + lane] = list;
+      }
+    }
+    part_sync<WAVES>();  // before LDS is written again
   }
 }
 
-template <typename T>
-__global__ void k_logprob_bwd(const T* logits, const long long* targets, const float* stats, const float* g_logp,
-                              const float* g_entropy, T* dlogits, bl_logprob_desc_t d) {
-  const long row = blockIdx.x;
-  const float m = stats[row], log_sum = stats[d.rows + row], entropy = stats[2 * d.rows + row];
-  const long long t = targets ? targets[row] : -1;
-  const bool none = m == -INFINITY && log_sum == -INFINITY;
-  const float g = g_logp && t >= 0 && t < d.classes ? g_logp[row] : 0.f, ge = g_entropy ? g_entropy[row] : 0.f;
-  for (long j = threadIdx.x; j < d.classes; j += kT) {
-    const float lq = to_f32(logits[row * d.stride + j]) - m - log_sum, q = expf(lq);
-    float dz = (j == t ? g : 0.f) - g * q;
-    if (g_entropy && q != 0.f) dz -= ge * q * (lq + entropy);
-    dlogits[row * d.grad_stride + j] = (T)(none ? 0.f : dz);
+// Rows of pieces: a block joins a row's sums and keys.
+template <typename T, bool TOP>
+__global__ __launch_bounds__(kT) void k_logprob_join(Ptrs a, bl_logprob_desc_t d, int pieces) {
+  __shared__ u64 lists[kT];
+  __shared__ Sums wave_sums[kWaves];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  for (long row = blockIdx.x; row < d.rows; row += gridDim.x) {
+    const float* sums = a.sums + (size_t)row * pieces * 3;
+    Sums s{-INFINITY, 0.f, 0.f};
+    for (int p = threadIdx.x; p < pieces; p += kT) s = joined(s, Sums{sums[3 * p], sums[3 * p + 1], sums[3 * p + 2]});
+    s = over_wave(s);
+    if (lane == 0) wave_sums[wave] = s;
+    u64 list = 0, last = 0;
+    if (TOP) {
+      const u64* keys = a.keys + (size_t)row * pieces * d.top;
+      const long n = (long)pieces * d.top;
+      for (long i = threadIdx.x; i - lane < n; i += kT) take64(i < n ? keys[i] : 0, d.top, list, last);
+      lists[threadIdx.x] = list;
+    }
+    __syncthreads();
+    s = wave_sums[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) s = joined(s, wave_sums[w]);
+    const Row r(s);
+    if (threadIdx.x == 0) write_row<T>(a, d, row, s, r);
+    if (TOP && wave == 0) {
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) list = join64(list, lists[w * kWave + lane]);
+      write_top(a, d, row, r, list);
+    }
+    __syncthreads();
+  }
+}
+
+// Gradient: E vectors of a piece a lane (WAVES = 1: a row by a wave), read and
+// written once.  Bound by HBM.
+struct GradPtrs {
+  const void* logits;
+  const long long* targets;
+  const float *stats, *g_logp, *g_entropy;
+  void* dlogits;
+};
+template <typename T, int E, int WAVES, bool ENTROPY>
+__global__ __launch_bounds__(kT) void k_logprob_bwd(GradPtrs a, bl_logprob_desc_t d, int pieces, long piece) {
+  constexpr int V = 16 / sizeof(T), kParts = kWaves / WAVES;
+  const int part = WAVES == 1 ? threadIdx.x / kWave : 0, in = WAVES == 1 ? threadIdx.x % kWave : threadIdx.x;
+  const unsigned long long count = (unsigned long long)d.rows * pieces;
+  for (unsigned long long q = (unsigned long long)blockIdx.x * kParts + part; q < count;
+       q += (unsigned long long)gridDim.x * kParts) {
+    const long row = pieces == 1 ? (long)q : (long)(q / (unsigned)pieces);
+    const long from = pieces == 1 ? 0 : (long)(q % (unsigned)pieces) * piece;
+    const int len = (int)min(piece, (long)d.classes - from);
+    const T* z = static_cast<const T*>(a.logits) + row * d.stride + from;
+    T* dz = static_cast<T*>(a.dlogits) + row * d.grad_stride + from;
+    Held<T, V> v[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      const int i = (in + k * WAVES * kWave) * V;
+      v[k].load(z + i, len - i);
+    }
+    const float m = a.stats[row], log_sum = a.stats[d.rows + row];
+    const float entropy = ENTROPY ? a.stats[2 * d.rows + row] : 0.f, ge = ENTROPY ? a.g_entropy[row] : 0.f;
+    const long long t = a.targets ? a.targets[row] : -1;
+    const float g = a.g_logp && t >= 0 && t < d.classes ? a.g_logp[row] : 0.f;
+    const bool none = m == -INFINITY && log_sum == -INFINITY;
+    const int at = t >= from && t < from + len ? (int)(t - from) : -1;  // the target in this piece
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      const int i = (in + k * WAVES * kWave) * V;
+      v[k].refresh();
+      Pack<T, V> o;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float lq = v[k][j] - m - log_sum, p = exp2_(lq * kLog2e);
+        float x = i + j == at ? g - g * p : -(g * p);
+        if (ENTROPY) x -= ge * p * fmaxf(lq + entropy, -1000.f);  // (a class ruled out: p is 0)
+        o.v[j] = (T)(none ? 0.f : x);
+      }
+      store_part<T, V>(dz + i, len - i, o);
+    }
   }
 }
 
@@ -103,6 +418,75 @@ __global__ void k_logprob_bwd(const T* logits, const long long* targets, const f
 }  // namespace blc
 
 using namespace blc;
+
+namespace {
+constexpr long kWaveClasses = 2048;   // rows up to so many lie on one wave
+constexpr long kPieceClasses = 8192;  // and pieces of longer ones on a block
+constexpr unsigned kGrid = 1u << 20;  // blocks of a launch, which go on with what is left
+
+// Vectors of a lane, of those that kernels are compiled for, for `n` classes on `threads` lanes.
+int vectors_of(long n, int threads, int wide) {
+  const long per = (long)threads * (16 / wide);
+  int each = 1;
+  while (each * per < n) each *= 2;
+  return each;
+}
+
+template <typename T, int WAVES, bool TOP>
+bl_status_t forward(const bl_logprob_plan_s* p, const Ptrs& a, hipStream_t s) {
+  const bl_logprob_desc_t& d = p->d;
+  const unsigned long long work = ((unsigned long long)d.rows * p->pieces + kWaves / WAVES - 1) / (kWaves / WAVES);
+  const unsigned blocks = (unsigned)std::min<unsigned long long>(work, kGrid);
+  const double bytes = (double)d.rows * d.classes * sizeof(T);
+  bl_status_t st = timed_launch("logprob_fwd", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    auto go = [&](auto kernel) {
+      hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(kT), 0, s, e0, e1, 0, a, d, p->pieces, p->piece);
+    };
+    if (p->each == 1) go(k_logprob_fwd<T, 1, WAVES, TOP>);
+    else if (p->each == 2) go(k_logprob_fwd<T, 2, WAVES, TOP>);
+    else if (p->each == 4 || sizeof(T) == 2) go(k_logprob_fwd<T, 4, WAVES, TOP>);
+    else go(k_logprob_fwd<float, 8, WAVES, TOP>);
+  });
+  if (st != BL_OK || p->pieces == 1) return st;
+  const double left = (double)d.rows * p->pieces * (12 + 8 * d.top);
+  return timed_launch("logprob_join", left, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    hipExtLaunchKernelGGL((k_logprob_join<T, TOP>), dim3((unsigned)std::min<long long>(d.rows, kGrid)), dim3(kT), 0, s,
+                          e0, e1, 0, a, d, p->pieces);
+  });
+}
+
+template <typename T>
+bl_status_t forward(const bl_logprob_plan_s* p, const Ptrs& a, hipStream_t s) {
+  if (p->block) return p->d.top ? forward<T, kWaves, true>(p, a, s) : forward<T, kWaves, false>(p, a, s);
+  return p->d.top ? forward<T, 1, true>(p, a, s) : forward<T, 1, false>(p, a, s);
+}
+
+template <typename T, int WAVES, bool ENTROPY>
+bl_status_t backward(const bl_logprob_plan_s* p, const GradPtrs& a, hipStream_t s) {
+  const bl_logprob_desc_t& d = p->d;
+  const long most = 4L * kT * (16 / (long)sizeof(T));  // of a piece: four vectors a lane
+  const int pieces = WAVES == 1 ? 1 : (int)((d.classes + most - 1) / most);
+  const long piece = ((d.classes + pieces - 1) / pieces + 15) / 16 * 16;
+  const int each = vectors_of(piece < d.classes ? piece : (long)d.classes, WAVES * kWave, (int)sizeof(T));
+  const unsigned long long work = ((unsigned long long)d.rows * pieces + kWaves / WAVES - 1) / (kWaves / WAVES);
+  const unsigned blocks = (unsigned)std::min<unsigned long long>(work, kGrid);
+  return timed_launch("logprob_bwd", 2.0 * d.rows * d.classes * sizeof(T), 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    auto go = [&](auto kernel) {
+      hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(kT), 0, s, e0, e1, 0, a, d, pieces, piece);
+    };
+    if (each == 1) go(k_logprob_bwd<T, 1, WAVES, ENTROPY>);
+    else if (each == 2) go(k_logprob_bwd<T, 2, WAVES, ENTROPY>);
+    else if (each == 4 || WAVES > 1 || sizeof(T) == 2) go(k_logprob_bwd<T, 4, WAVES, ENTROPY>);
+    else go(k_logprob_bwd<float, 8, 1, ENTROPY>);
+  });
+}
+
+template <typename T>
+bl_status_t backward(const bl_logprob_plan_s* p, const GradPtrs& a, hipStream_t s) {
+  if (p->d.classes > kWaveClasses) return a.g_entropy ? backward<T, kWaves, true>(p, a, s) : backward<T, kWaves, false>(p, a, s);
+  return a.g_entropy ? backward<T, 1, true>(p, a, s) : backward<T, 1, false>(p, a, s);
+}
+}  // namespace
 
 extern "C" bl_status_t bl_logprob_plan_create(bl_logprob_plan_t* out, const bl_logprob_desc_t* desc) {
   if (!out || !desc) return BL_ERR_INVALID_ARG;
@@ -115,8 +499,17 @@ extern "C" bl_status_t bl_logprob_plan_create(bl_logprob_plan_t* out, const bl_l
   if (d.rows > 1 && (d.stride < d.classes || d.grad_stride < d.classes)) return BL_ERR_INVALID_ARG;
   const long long most = (1LL << 31) - 1;
   if (d.top > 64 || d.classes > most || d.rows > most) return BL_ERR_UNSUPPORTED;
-  bl_logprob_plan_s* p = new (std::nothrow) bl_logprob_plan_s{d};
+  bl_logprob_plan_s* p = new (std::nothrow) bl_logprob_plan_s{};
   if (!p) return BL_ERR_OOM;
+  p->d = d;
+  p->block = d.classes > kWaveClasses;
+  p->pieces = p->block ? (int)((d.classes + kPieceClasses - 1) / kPieceClasses) : 1;
+  p->piece = p->pieces == 1 ? (long)d.classes : ((d.classes + p->pieces - 1) / p->pieces + 15) / 16 * 16;
+  p->each = vectors_of(p->piece, p->block ? kT : kWave, dtype_bytes(d.dtype));
+  if (p->pieces > 1) {
+    p->off_sums = (size_t)d.rows * p->pieces * d.top * sizeof(u64);
+    p->bytes = p->off_sums + (size_t)d.rows * p->pieces * 3 * sizeof(float);
+  }
   *out = p;
   return BL_OK;
 }
@@ -129,43 +522,22 @@ extern "C" bl_status_t bl_logprob_plan_destroy(bl_logprob_plan_t p) {
 
 extern "C" bl_status_t bl_logprob_workspace_size(bl_logprob_plan_t p, size_t* bytes) {
   if (!p || !bytes) return BL_ERR_INVALID_ARG;
-  *bytes = 0;
+  *bytes = p->bytes;
   return BL_OK;
 }
-
-namespace {
-template <typename T>
-bl_status_t forward(const bl_logprob_plan_s* p, const void* logits, const long long* targets, float* logp,
-                    float* stats, float* top_logp, long long* top_index, hipStream_t s) {
-  const bl_logprob_desc_t& d = p->d;
-  return timed_launch("logprob_fwd", (double)d.rows * d.classes * sizeof(T), 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-    hipExtLaunchKernelGGL(k_logprob_fwd<T>, dim3((unsigned)d.rows), dim3(kT), 0, s, e0, e1, 0,
-                          static_cast<const T*>(logits), targets, logp, stats, top_logp, top_index, d);
-  });
-}
-template <typename T>
-bl_status_t backward(const bl_logprob_plan_s* p, const void* logits, const long long* targets, const float* stats,
-                     const float* g_logp, const float* g_entropy, void* dlogits, hipStream_t s) {
-  const bl_logprob_desc_t& d = p->d;
-  return timed_launch("logprob_bwd", 2.0 * d.rows * d.classes * sizeof(T), 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-    hipExtLaunchKernelGGL(k_logprob_bwd<T>, dim3((unsigned)d.rows), dim3(kT), 0, s, e0, e1, 0,
-                          static_cast<const T*>(logits), targets, stats, g_logp, g_entropy,
-                          static_cast<T*>(dlogits), d);
-  });
-}
-}  // namespace
 
 extern "C" bl_status_t bl_logprob_forward(bl_logprob_plan_t p, const void* logits, const long long* targets,
                                           float* logp, float* stats, float* top_logp, long long* top_index, void* ws,
                                           void* stream) {
   if (!p) return BL_ERR_INVALID_ARG;
   if (!p->d.rows) return BL_OK;
-  if (!logits || (p->d.top && (!top_logp || !top_index))) return BL_ERR_INVALID_ARG;
-  (void)ws;
+  if (!logits || (p->d.top && (!top_logp || !top_index)) || (p->bytes && !ws)) return BL_ERR_INVALID_ARG;
+  const Ptrs a{logits, targets, logp, stats, top_logp, top_index, static_cast<u64*>(ws),
+               reinterpret_cast<float*>(static_cast<char*>(ws) + p->off_sums)};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (p->d.dtype == BL_F32) return forward<float>(p, logits, targets, logp, stats, top_logp, top_index, s);
-  if (p->d.dtype == BL_BF16) return forward<bf16_t>(p, logits, targets, logp, stats, top_logp, top_index, s);
-  return forward<f16_t>(p, logits, targets, logp, stats, top_logp, top_index, s);
+  if (p->d.dtype == BL_F32) return forward<float>(p, a, s);
+  if (p->d.dtype == BL_BF16) return forward<bf16_t>(p, a, s);
+  return forward<f16_t>(p, a, s);
 }
 
 extern "C" bl_status_t bl_logprob_backward(bl_logprob_plan_t p, const void* logits, const long long* targets,
@@ -174,8 +546,9 @@ extern "C" bl_status_t bl_logprob_backward(bl_logprob_plan_t p, const void* logi
   if (!p) return BL_ERR_INVALID_ARG;
   if (!p->d.rows) return BL_OK;
   if (!logits || !stats || !dlogits) return BL_ERR_INVALID_ARG;
+  const GradPtrs a{logits, targets, stats, g_logp, g_entropy, dlogits};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (p->d.dtype == BL_F32) return backward<float>(p, logits, targets, stats, g_logp, g_entropy, dlogits, s);
-  if (p->d.dtype == BL_BF16) return backward<bf16_t>(p, logits, targets, stats, g_logp, g_entropy, dlogits, s);
-  return backward<f16_t>(p, logits, targets, stats, g_logp, g_entropy, dlogits, s);
+  if (p->d.dtype == BL_F32) return backward<float>(p, a, s);
+  if (p->d.dtype == BL_BF16) return backward<bf16_t>(p, a, s);
+  return backward<f16_t>(p, a, s);
 }

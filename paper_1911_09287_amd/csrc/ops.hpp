@@ -64,19 +64,20 @@ struct Held {
   static constexpr int kWords = (N * (int)sizeof(T) + 3) / 4;
   unsigned w[kWords];
 
-  // The first n elements at p (n <= 0: none; the others are 0).
-  __device__ __forceinline__ void load(const T* p, long n) {
+  // The first n elements at p (n <= 0: none; the others are `fill`, a word's bits).
+  __device__ __forceinline__ void load(const T* p, long n, unsigned fill = 0) {
     if (n >= N) {
       if (N * sizeof(T) % 4) w[kWords - 1] = 0;
       __builtin_memcpy(w, p, N * sizeof(T));
     } else {
 #pragma unroll
-      for (int i = 0; i < kWords; ++i) w[i] = 0;
+      for (int i = 0; i < kWords; ++i) w[i] = fill;
 #pragma unroll
       for (int j = 0; j < N; ++j)
         if (j < n) {
           if constexpr (sizeof(T) == 4) w[j] = __builtin_bit_cast(unsigned, p[j]);
-          else w[j / 2] |= (unsigned)__builtin_bit_cast(unsigned short, p[j]) << (16 * (j & 1));
+          else w[j / 2] = (w[j / 2] & (j & 1 ? 0xFFFFu : 0xFFFF0000u)) |
+                          (unsigned)__builtin_bit_cast(unsigned short, p[j]) << (16 * (j & 1));
         }
     }
   }
@@ -113,6 +114,21 @@ __device__ __forceinline__ float add16(float x) {
 __device__ __forceinline__ float add32(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float max16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, dpp<0xB1>(x));
+  x = fmaxf(x, dpp<0x4E>(x));
+  x = fmaxf(x, dpp<0x141>(x));
+  x = fmaxf(x, dpp<0x140>(x));
+  return max32(max16(x));
 }
 // Sum over groups of `lanes` neighbouring lanes (a power of two, the same for the
 // whole wave; every lane of a group active), for each of them.
