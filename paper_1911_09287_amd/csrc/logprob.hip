@@ -11,11 +11,10 @@
 // the exponentials.
 //
 // The `top` likeliest: a value and its class make one key of 64 bits whose order is
-// the wanted one.  Of the lanes' largest values (of 64 groups of lanes) the top-th
-// bounds the answer from below, so that few values are left; these go to LDS and one
-// wave sorts them, 64 keys on its lanes, by a bitonic network.  Where more are left
-// than there is room for (many equal values), or the row holds NaN, the waves take
-// 64 keys after another and join them to a sorted list.  Pieces leave their `top` keys
+// the wanted one.  The top-th of the largest values on each lane bounds the answer
+// from below, so that few values are left; these go to LDS and one wave sorts them, 64 keys on its lanes, by a
+// bitonic network.  Where more are left than there is room for (many equal values), or
+// the row holds NaN, the waves take 64 keys after another and join them to a sorted list.  Pieces leave their `top` keys
 // for a second launch that joins them.
 #include <algorithm>
 #include <new>
@@ -37,6 +36,12 @@ namespace {
 constexpr int kT = 256;
 constexpr int kWaves = kT / kWave;
 constexpr int kRoom = 512;  // keys that are left after the bound, for which LDS has room
+// `top` up to which a block's bound is the top-th of the largest values on each lane
+// over the waves; beyond, each wave's ceil(top / 4)-th of its lanes', and the least of
+// the waves.  The first is nearer where few are wanted (4096 rows of 32000 bfloat16
+// logits, top 8: 92 us against 99), the second where most lanes hold one (32000 fp32,
+// top 64: 286 against 170).
+constexpr int kFewTop = 24;
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 using u64 = unsigned long long;
 
@@ -75,43 +80,45 @@ template <int J>
 __device__ __forceinline__ u64 lane_xor(u64 x) {
   return (u64)lane_xor<J>((unsigned)(x >> 32)) << 32 | lane_xor<J>((unsigned)x);
 }
-// One step of a bitonic network: lanes that differ in bit J exchange; the larger
-// goes to the lower one where `falling`.
-template <int J, typename K>
-__device__ __forceinline__ K exchange(K x, bool falling) {
-  const K y = lane_xor<J>(x);
-  const bool lower = !(threadIdx.x & J);
-  return (lower == falling) == (y > x) ? y : x;
+// One step of a bitonic network: lanes that differ in bit J exchange.  Stretches of
+// K lanes fall and rise in turn (K = 64: all fall); where they fall the larger goes
+// to the lower lane.  The lanes that keep the larger are known beforehand.
+constexpr u64 larger_lanes(int J, int K) {
+  u64 m = 0;
+  for (int l = 0; l < kWave; ++l)
+    if (((l & J) == 0) == (K == kWave || (l & K) == 0)) m |= 1ull << l;
+  return m;
+}
+template <int J, int K>
+__device__ __forceinline__ unsigned exchange(unsigned x) {
+  const unsigned y = lane_xor<J>(x);
+  return __builtin_amdgcn_inverse_ballot_w64(larger_lanes(J, K)) ? max(x, y) : min(x, y);
+}
+template <int J, int K>
+__device__ __forceinline__ u64 exchange(u64 x) {
+  const u64 y = lane_xor<J>(x);
+  return __builtin_amdgcn_inverse_ballot_w64(larger_lanes(J, K) ^ __ballot(y < x)) ? y : x;
+}
+// Steps J, J / 2, ... 1.
+template <int J, int K, typename X>
+__device__ __forceinline__ X merge_stretches(X x) {
+  x = exchange<J, K>(x);
+  if constexpr (J > 1) x = merge_stretches<J / 2, K>(x);
+  return x;
 }
 // Falling order over the wave of values that rise and then fall (or the reverse).
-template <typename K>
-__device__ __forceinline__ K merge64(K x) {
-  x = exchange<32>(x, true);
-  x = exchange<16>(x, true);
-  x = exchange<8>(x, true);
-  x = exchange<4>(x, true);
-  x = exchange<2>(x, true);
-  return exchange<1>(x, true);
+template <typename X>
+__device__ __forceinline__ X merge64(X x) {
+  return merge_stretches<32, 64>(x);
 }
 // Falling order over the wave.
-template <typename K>
-__device__ __forceinline__ K sort64(K x) {
-  const unsigned l = threadIdx.x;
-  x = exchange<1>(x, !(l & 2));
-  x = exchange<2>(x, !(l & 4));
-  x = exchange<1>(x, !(l & 4));
-  x = exchange<4>(x, !(l & 8));
-  x = exchange<2>(x, !(l & 8));
-  x = exchange<1>(x, !(l & 8));
-  x = exchange<8>(x, !(l & 16));
-  x = exchange<4>(x, !(l & 16));
-  x = exchange<2>(x, !(l & 16));
-  x = exchange<1>(x, !(l & 16));
-  x = exchange<16>(x, !(l & 32));
-  x = exchange<8>(x, !(l & 32));
-  x = exchange<4>(x, !(l & 32));
-  x = exchange<2>(x, !(l & 32));
-  x = exchange<1>(x, !(l & 32));
+template <typename X>
+__device__ __forceinline__ X sort64(X x) {
+  x = merge_stretches<1, 2>(x);
+  x = merge_stretches<2, 4>(x);
+  x = merge_stretches<4, 8>(x);
+  x = merge_stretches<8, 16>(x);
+  x = merge_stretches<16, 32>(x);
   return merge64(x);
 }
 // The 64 largest of two lists in falling order, in falling order.
@@ -126,7 +133,8 @@ __device__ __forceinline__ u64 lane_value(u64 x, int lane) {
 // Joins 64 keys in any order (0: none) to a list whose top-th is `last`.
 __device__ __forceinline__ void take64(u64 x, int top, u64& list, u64& last) {
   if (!__ballot(x > last)) return;
-  list = join64(list, sort64(x));
+  x = sort64(x);
+  list = lane_value(list, 0) ? join64(list, x) : x;
   last = lane_value(list, top - 1);
 }
 
@@ -208,20 +216,35 @@ __device__ __forceinline__ void part_sync() {  // over the waves that work on on
   else __syncthreads();
 }
 
+// Adds 2^t and 2^t t of all values to a lane's sums.
+template <typename T, int V, int E, typename Exponent>
+__device__ __forceinline__ void add_terms(Held<T, V> (&v)[E], Sums& s, Exponent&& exponent) {
+#pragma unroll
+  for (int k = 0; k < E; ++k) {
+    v[k].refresh();
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float t = exponent(v[k][j]), e = exp2_(t);
+      s.a += e;
+      s.b = fmaf(e, fmaxf(t, -1000.f), s.b);  // (t = -infinity: e is 0)
+    }
+  }
+}
+
 // Pieces of rows (WAVES = 1: whole rows), E vectors a lane.  With `pieces` > 1 each
 // leaves its sums and keys, else it gives the row's results.
 template <typename T, int E, int WAVES, bool TOP>
 __global__ __launch_bounds__(kT) void k_logprob_fwd(Ptrs a, bl_logprob_desc_t d, int pieces, long piece) {
   constexpr int V = 16 / sizeof(T), kParts = kWaves / WAVES;  // pieces of a block at a time
-  __shared__ u64 room[kParts][TOP ? (WAVES == 1 ? kRoom / 2 : kRoom) : 1];
-  __shared__ unsigned largest[kParts][TOP ? WAVES * kWave : 1];
+  __shared__ u64 room[kParts][TOP ? kRoom : 1];
+  __shared__ unsigned largest[TOP ? WAVES * kWave : 1];
   __shared__ int left[kParts];
   __shared__ Sums wave_sums[WAVES];
   const int part = WAVES == 1 ? threadIdx.x / kWave : 0, in = WAVES == 1 ? threadIdx.x % kWave : threadIdx.x;
   const int lane = threadIdx.x % kWave, wave = in / kWave;
   const unsigned long long count = (unsigned long long)d.rows * pieces;
-  for (unsigned long long q = (unsigned long long)blockIdx.x * kParts + part; q < count;
-       q += (unsigned long long)gridDim.x * kParts) {
+  const unsigned long long stride = (unsigned long long)gridDim.x * kParts;
+  for (unsigned long long q = (unsigned long long)blockIdx.x * kParts + part; q < count; q += stride) {
     const long row = pieces == 1 ? (long)q : (long)(q / (unsigned)pieces);
     const long from = pieces == 1 ? 0 : (long)(q % (unsigned)pieces) * piece;
     const int len = (int)min(piece, (long)d.classes - from);
@@ -233,27 +256,35 @@ __global__ __launch_bounds__(kT) void k_logprob_fwd(Ptrs a, bl_logprob_desc_t d,
       v[k].load(z + i, len - i, kMinusInf<T>);
     }
     Sums s{-INFINITY, 0.f, 0.f};
+    float most[E];  // of each vector
 #pragma unroll
     for (int k = 0; k < E; ++k) {
       v[k].refresh();
+      most[k] = v[k][0];
 #pragma unroll
-      for (int j = 0; j < V; ++j) s.m = fmaxf(s.m, v[k][j]);
+      for (int j = 1; j < V; ++j) most[k] = fmaxf(most[k], v[k][j]);
+      s.m = fmaxf(s.m, most[k]);
     }
+    unsigned bound = 0;
+    const bool by_lanes = WAVES == 1 || d.top <= kFewTop;
     if (TOP) {
-      largest[part][in] = order_of(s.m);
+      bound = order_of(s.m);
+      if (!by_lanes) bound = (unsigned)__builtin_amdgcn_readlane((int)sort64(bound), (d.top + WAVES - 1) / WAVES - 1);
+      if (WAVES > 1) largest[in] = bound;
       if (in == 0) left[part] = 0;
     }
     const float base = s.m == -INFINITY ? 0.f : s.m;
-#pragma unroll
-    for (int k = 0; k < E; ++k) {
-      v[k].refresh();
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float t = (v[k][j] - base) * kLog2e, e = exp2_(t);
-        s.a += e;
-        s.b = fmaf(e, fmaxf(t, -1000.f), s.b);  // (t = -infinity: e is 0)
-      }
+    if (!__ballot(fabsf(base) > 1e38f)) {
+      // t = z log2 e + c with c rounded once: all terms are 2^r too large, r what the
+      // rounding left, which is taken out of the sums
+      const float c = -(base * kLog2e), left_over = fmaf(base, kLog2e, c), f = exp2_(-left_over);
+      add_terms<T, V, E>(v, s, [&](float z) { return fmaf(z, kLog2e, c); });
+      s.b = fmaf(-left_over, s.a, s.b) * f;
+      s.a *= f;
+    } else {  // (there the product would overflow)
+      add_terms<T, V, E>(v, s, [&](float z) { return (z - base) * kLog2e; });
     }
+    if (!(s.a < INFINITY)) s.a = NAN;  // (infinite only beside an infinite logit)
     s = over_wave(s);
     if (WAVES > 1 && lane == 0) wave_sums[wave] = s;
     part_sync<WAVES>();
@@ -265,35 +296,47 @@ __global__ __launch_bounds__(kT) void k_logprob_fwd(Ptrs a, bl_logprob_desc_t d,
     const Row r(s);
     u64 list = 0, last = 0;
     if (TOP) {
-      // the top-th of 64 groups' largest values is a bound from below
-      unsigned o = largest[part][lane];
 #pragma unroll
-      for (int w = 1; w < WAVES; ++w) o = max(o, largest[part][lane + w * kWave]);
-      const float bound = value_of((unsigned)__builtin_amdgcn_readlane((int)sort64(o), d.top - 1));
-      constexpr int kMost = WAVES == 1 ? kRoom / 2 : kRoom;
+      for (int w = 0; w < (WAVES > 1 ? WAVES : 0); ++w) {
+        const unsigned o = largest[lane + w * kWave];
+        bound = w == 0 ? o : by_lanes ? max(bound, o) : min(bound, o);
+      }
+      if (by_lanes) bound = (unsigned)__builtin_amdgcn_readlane((int)sort64(bound), d.top - 1);
+      const float least = value_of(bound);
       bool whole = s.a == s.a;  // no NaN
       if (whole) {
+        // each lane's vectors that hold such a value (mostly none, seldom two), read again
+        unsigned hits = 0;
 #pragma unroll
-        for (int k = 0; k < E; ++k) {
-          v[k].refresh();
+        for (int k = 0; k < E; ++k) hits |= most[k] >= least ? 1u << k : 0u;
+        while (__ballot(hits != 0)) {
+          const int i = hits ? (in + __builtin_ctz(hits) * WAVES * kWave) * V : len;
+          hits &= hits - 1;
+          Held<T, V> u;
+          u.load(z + i, len - i, kMinusInf<T>);
+          u.refresh();
+          u64 pass[V];
+          int n = 0;
 #pragma unroll
           for (int j = 0; j < V; ++j) {
-            const float zj = v[k][j];
-            const int i = (in + k * WAVES * kWave) * V + j;
-            const u64 pass = __ballot(zj >= bound && i < len);
-            if (pass) {
-              int at = 0;
-              if (lane == 0) at = atomicAdd(&left[part], __popcll(pass));
-              at = __builtin_amdgcn_readfirstlane(at) +
-                   __builtin_amdgcn_mbcnt_hi((unsigned)(pass >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)pass, 0));
-              if ((pass >> lane & 1) && at < kMost) room[part][at] = key_of(zj, (unsigned)(from + i));
-            }
+            pass[j] = __ballot(u[j] >= least && i + j < len);
+            n += __popcll(pass[j]);
+          }
+          int at = 0;
+          if (lane == 0) at = atomicAdd(&left[part], n);
+          at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const int to = at + __builtin_amdgcn_mbcnt_hi((unsigned)(pass[j] >> 32),
+                                                          __builtin_amdgcn_mbcnt_lo((unsigned)pass[j], 0));
+            if ((pass[j] >> lane & 1) && to < kRoom) room[part][to] = key_of(u[j], (unsigned)(from + i + j));
+            at += __popcll(pass[j]);
           }
         }
       }
       part_sync<WAVES>();
       const int n = left[part];
-      whole = whole && n <= kMost;
+      whole = whole && n <= kRoom;
       if (whole) {
         if (wave == 0)
           for (int i = lane; i - lane < n; i += kWave) take64(i < n ? room[part][i] : 0, d.top, list, last);
@@ -327,7 +370,7 @@ __global__ __launch_bounds__(kT) void k_logprob_fwd(Ptrs a, bl_logprob_desc_t d,
         if (TOP && lane < d.top) a.keys[q * d.top + lane] = list;
       }
     }
-    part_sync<WAVES>();  // before LDS is written again
+    if (q + stride < count) part_sync<WAVES>();  // before LDS is written again
   }
 }
 
@@ -421,7 +464,7 @@ using namespace blc;
 
 namespace {
 constexpr long kWaveClasses = 2048;   // rows up to so many lie on one wave
-constexpr long kPieceClasses = 8192;  // and pieces of longer ones on a block
+constexpr long kPieceVectors = 8 * kT; // and pieces of longer ones on a block, 8 vectors a lane
 constexpr unsigned kGrid = 1u << 20;  // blocks of a launch, which go on with what is left
 
 // Vectors of a lane, of those that kernels are compiled for, for `n` classes on `threads` lanes.
@@ -444,8 +487,8 @@ bl_status_t forward(const bl_logprob_plan_s* p, const Ptrs& a, hipStream_t s) {
     };
     if (p->each == 1) go(k_logprob_fwd<T, 1, WAVES, TOP>);
     else if (p->each == 2) go(k_logprob_fwd<T, 2, WAVES, TOP>);
-    else if (p->each == 4 || sizeof(T) == 2) go(k_logprob_fwd<T, 4, WAVES, TOP>);
-    else go(k_logprob_fwd<float, 8, WAVES, TOP>);
+    else if (p->each == 4) go(k_logprob_fwd<T, 4, WAVES, TOP>);
+    else go(k_logprob_fwd<T, 8, WAVES, TOP>);
   });
   if (st != BL_OK || p->pieces == 1) return st;
   const double left = (double)d.rows * p->pieces * (12 + 8 * d.top);
@@ -497,13 +540,14 @@ extern "C" bl_status_t bl_logprob_plan_create(bl_logprob_plan_t* out, const bl_l
   if (!d.stride) d.stride = d.classes;
   if (!d.grad_stride) d.grad_stride = d.classes;
   if (d.rows > 1 && (d.stride < d.classes || d.grad_stride < d.classes)) return BL_ERR_INVALID_ARG;
-  const long long most = (1LL << 31) - 1;
-  if (d.top > 64 || d.classes > most || d.rows > most) return BL_ERR_UNSUPPORTED;
+  const long long limit = (1LL << 31) - 1;
+  if (d.top > 64 || d.classes > limit || d.rows > limit) return BL_ERR_UNSUPPORTED;
   bl_logprob_plan_s* p = new (std::nothrow) bl_logprob_plan_s{};
   if (!p) return BL_ERR_OOM;
   p->d = d;
   p->block = d.classes > kWaveClasses;
-  p->pieces = p->block ? (int)((d.classes + kPieceClasses - 1) / kPieceClasses) : 1;
+  const long most = kPieceVectors * (16 / dtype_bytes(d.dtype));
+  p->pieces = p->block ? (int)((d.classes + most - 1) / most) : 1;
   p->piece = p->pieces == 1 ? (long)d.classes : ((d.classes + p->pieces - 1) / p->pieces + 15) / 16 * 16;
   p->each = vectors_of(p->piece, p->block ? kT : kWave, dtype_bytes(d.dtype));
   if (p->pieces > 1) {
