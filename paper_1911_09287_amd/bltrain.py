@@ -9,6 +9,8 @@ from __future__ import annotations
 
 import ctypes
 
+import torch
+
 from . import blconv
 from .blconv import BlError, _check  # noqa: F401  (BlError: what these calls raise)
 
@@ -75,21 +77,19 @@ def load():
     return lib
 
 
-def _dtypes():
-    import torch
-    return {torch.float32: BL_F32, torch.bfloat16: BL_BF16, torch.float16: BL_F16}
+_DTYPES = {torch.float32: BL_F32, torch.bfloat16: BL_BF16, torch.float16: BL_F16}
 
 
 def _dtype_code(dtype, name):
-    code = _dtypes().get(dtype)
+    code = _DTYPES.get(dtype)
     if code is None:
         raise ValueError(f"{name} must be torch.float32, torch.bfloat16 or torch.float16, not {dtype}")
     return code
 
 
-def _stream(stream):
-    import torch
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+def _stream(stream, t):
+    """The HIP stream: the given one, or the current one of the device of tensor t."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def _flat(t, dtype, numel, name):
@@ -129,13 +129,12 @@ class _Plan:
             self._h = None
 
     def workspace(self, device="cuda"):
-        import torch
         return torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
 
     def _ws(self, ws):
         if self.workspace_bytes == 0:
             return None
-        if ws is None or not ws.is_cuda or ws.numel() * ws.element_size() < self.workspace_bytes:
+        if ws is None or not ws.is_cuda or ws.nbytes < self.workspace_bytes:
             raise ValueError("workspace must be a GPU tensor of at least workspace_bytes bytes")
         return ws.data_ptr()
 
@@ -153,7 +152,6 @@ class NormPlan(_Plan):
     _destroy = "bl_norm_plan_destroy"
 
     def __init__(self, outer, size, inner=1, dtype=None, wdtype=None, eps=1e-5, x_stride=0, y_stride=0):
-        import torch
         self._lib = load()
         self.dtype = torch.float32 if dtype is None else dtype
         self.wdtype = torch.float32 if wdtype is None else wdtype
@@ -177,7 +175,6 @@ class NormPlan(_Plan):
         return _sliced(t, self.dtype, self.outer, self.size * self.inner, self.y_stride, name)
 
     def _stats(self, t):
-        import torch
         return _flat(t, torch.float32, 2 * self.outer * self.inner, "stats")
 
     def forward(self, x, weight, bias, y, stats, ws, stream=None):
@@ -186,14 +183,14 @@ class NormPlan(_Plan):
         _check("bl_norm_forward", self._lib.bl_norm_forward(
             self._h, self._x(x, "x"), _flat(weight, self.wdtype, self.size, "weight"),
             _flat(bias, self.wdtype, self.size, "bias"), self._y(y, "y"), self._stats(stats), self._ws(ws),
-            _stream(stream)))
+            _stream(stream, x)))
 
     def backward(self, dy, x, weight, stats, dx, dweight, dbias, ws, stream=None):
         """dx, and the gradients of weight and bias (None: not wanted)."""
         _check("bl_norm_backward", self._lib.bl_norm_backward(
             self._h, self._y(dy, "dy"), self._x(x, "x"), _flat(weight, self.wdtype, self.size, "weight"),
             self._stats(stats), self._x(dx, "dx"), _flat(dweight, self.wdtype, self.size, "dweight"),
-            _flat(dbias, self.wdtype, self.size, "dbias"), self._ws(ws), _stream(stream)))
+            _flat(dbias, self.wdtype, self.size, "dbias"), self._ws(ws), _stream(stream, x)))
 
 
 class LogProbPlan(_Plan):
@@ -203,7 +200,6 @@ class LogProbPlan(_Plan):
     _destroy = "bl_logprob_plan_destroy"
 
     def __init__(self, rows, classes, top=0, dtype=None, stride=0, grad_stride=0):
-        import torch
         self._lib = load()
         self.dtype = torch.float32 if dtype is None else dtype
         d = LogProbDesc(rows, classes, top, _dtype_code(self.dtype, "dtype"), stride, grad_stride)
@@ -218,23 +214,22 @@ class LogProbPlan(_Plan):
     def forward(self, logits, targets, logp, stats, top_logp, top_index, ws, stream=None):
         """logp [rows], stats [3][rows] (largest logit, log of the sum of
         exponentials over it, entropy), top_logp and top_index [rows][top]."""
-        import torch
         _check("bl_logprob_forward", self._lib.bl_logprob_forward(
             self._h, _sliced(logits, self.dtype, self.rows, self.classes, self.stride, "logits"),
             _flat(targets, torch.int64, self.rows, "targets"), _flat(logp, torch.float32, self.rows, "logp"),
             _flat(stats, torch.float32, 3 * self.rows, "stats"),
             _flat(top_logp, torch.float32, self.rows * self.top, "top_logp"),
-            _flat(top_index, torch.int64, self.rows * self.top, "top_index"), self._ws(ws), _stream(stream)))
+            _flat(top_index, torch.int64, self.rows * self.top, "top_index"), self._ws(ws), _stream(stream, logits)))
 
     def backward(self, logits, targets, stats, g_logp, g_entropy, dlogits, stream=None):
         """The logits' gradient from those of logp and of the entropy (None: 0)."""
-        import torch
         _check("bl_logprob_backward", self._lib.bl_logprob_backward(
             self._h, _sliced(logits, self.dtype, self.rows, self.classes, self.stride, "logits"),
             _flat(targets, torch.int64, self.rows, "targets"), _flat(stats, torch.float32, 3 * self.rows, "stats"),
             _flat(g_logp, torch.float32, self.rows, "g_logp"),
             _flat(g_entropy, torch.float32, self.rows, "g_entropy"),
-            _sliced(dlogits, self.dtype, self.rows, self.classes, self.grad_stride, "dlogits"), _stream(stream)))
+            _sliced(dlogits, self.dtype, self.rows, self.classes, self.grad_stride, "dlogits"),
+            _stream(stream, logits)))
 
 
 class AdamWTensors:
@@ -260,7 +255,6 @@ class AdamWPlan(_Plan):
     workspace_bytes = 0
 
     def __init__(self, sizes, param_dtype=None, grad_dtype=None, bits=32, decay=None):
-        import torch
         self._lib = load()
         self.sizes, self.bits = [int(n) for n in sizes], bits
         self.param_dtype = torch.float32 if param_dtype is None else param_dtype
@@ -280,11 +274,10 @@ class AdamWPlan(_Plan):
 
     def state(self, device="cuda"):
         """A new state: moments of zero."""
-        import torch
         return torch.zeros(self.state_bytes, dtype=torch.uint8, device=device)
 
     def _state(self, state):
-        if not (state.is_cuda and state.is_contiguous()) or state.numel() * state.element_size() != self.state_bytes:
+        if not (state.is_cuda and state.is_contiguous()) or state.nbytes != self.state_bytes:
             raise ValueError("state must be a contiguous GPU tensor of state_bytes bytes")
         return state.data_ptr()
 
@@ -297,18 +290,16 @@ class AdamWPlan(_Plan):
         """One step, in place.  `grad_scale`: a float32 GPU tensor of one element
         that gradients are multiplied by.  `live`: a float64 GPU tensor (lr, step)
         that is read in the place of those two when the kernels run."""
-        import torch
         if tensors.plan is not self:
             raise ValueError("the tensors were bound to another plan")
         a = AdamWArgs(lr, betas[0], betas[1], eps, weight_decay, step, seed & 0xFFFFFFFF,
                       _flat(grad_scale, torch.float32, 1, "grad_scale"), _flat(live, torch.float64, 2, "live"))
         _check("bl_adamw_step", self._lib.bl_adamw_step(self._h, tensors._p, tensors._g, self._state(state),
-                                                        ctypes.byref(a), _stream(stream)))
+                                                        ctypes.byref(a), _stream(stream, state)))
 
     def moments(self, state, m=None, v=None, stream=None):
         """(m, v), [total] each, tensor i's at starts[i]: of 32 bits as views of
         the state, of 8 bits as their values in new bfloat16 tensors (or those given)."""
-        import torch
         if self.bits == 32 and m is None and v is None:
             both = state.view(torch.float32)
             return both[:self.total], both[self.total:]
@@ -318,14 +309,13 @@ class AdamWPlan(_Plan):
             v = torch.empty(self.total, dtype=dtype, device=state.device) if v is None else v
         _check("bl_adamw_get_moments", self._lib.bl_adamw_get_moments(
             self._h, self._state(state), _flat(m, dtype, self.total, "m"), _flat(v, dtype, self.total, "v"),
-            _stream(stream)))
+            _stream(stream, state)))
         return m, v
 
     def load_moments(self, state, m, v, stream=None):
         """Sets the moments from values (converted to float32) in the layout of moments()."""
-        import torch
         with torch.cuda.stream(stream):
             m, v = m.float(), v.float()
         _check("bl_adamw_set_moments", self._lib.bl_adamw_set_moments(
             self._h, self._state(state), _flat(m, torch.float32, self.total, "m"),
-            _flat(v, torch.float32, self.total, "v"), _stream(stream)))
+            _flat(v, torch.float32, self.total, "v"), _stream(stream, state)))

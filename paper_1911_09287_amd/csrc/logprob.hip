@@ -374,37 +374,41 @@ __global__ __launch_bounds__(kT) void k_logprob_fwd(Ptrs a, bl_logprob_desc_t d,
   }
 }
 
-// Rows of pieces: a block joins a row's sums and keys.
-template <typename T, bool TOP>
+// Rows of pieces: a block, or a wave where there are few keys, joins a row's sums
+// and keys.
+template <typename T, int WAVES, bool TOP>
 __global__ __launch_bounds__(kT) void k_logprob_join(Ptrs a, bl_logprob_desc_t d, int pieces) {
-  __shared__ u64 lists[kT];
-  __shared__ Sums wave_sums[kWaves];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  for (long row = blockIdx.x; row < d.rows; row += gridDim.x) {
+  constexpr int kRows = kWaves / WAVES, threads = WAVES * kWave;
+  __shared__ u64 lists[WAVES > 1 && TOP ? kT : 1];
+  __shared__ Sums wave_sums[WAVES];
+  const int lane = threadIdx.x % kWave, in = threadIdx.x % threads, wave = in / kWave;
+  for (long row = (long)blockIdx.x * kRows + threadIdx.x / threads; row < d.rows; row += (long)gridDim.x * kRows) {
     const float* sums = a.sums + (size_t)row * pieces * 3;
     Sums s{-INFINITY, 0.f, 0.f};
-    for (int p = threadIdx.x; p < pieces; p += kT) s = joined(s, Sums{sums[3 * p], sums[3 * p + 1], sums[3 * p + 2]});
+    for (int p = in; p < pieces; p += threads) s = joined(s, Sums{sums[3 * p], sums[3 * p + 1], sums[3 * p + 2]});
     s = over_wave(s);
-    if (lane == 0) wave_sums[wave] = s;
     u64 list = 0, last = 0;
     if (TOP) {
       const u64* keys = a.keys + (size_t)row * pieces * d.top;
       const long n = (long)pieces * d.top;
-      for (long i = threadIdx.x; i - lane < n; i += kT) take64(i < n ? keys[i] : 0, d.top, list, last);
-      lists[threadIdx.x] = list;
+      for (long i = in; i - lane < n; i += threads) take64(i < n ? keys[i] : 0, d.top, list, last);
     }
-    __syncthreads();
-    s = wave_sums[0];
+    if (WAVES > 1) {
+      if (lane == 0) wave_sums[wave] = s;
+      if (TOP) lists[in] = list;
+      __syncthreads();
+      s = wave_sums[0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) s = joined(s, wave_sums[w]);
+      for (int w = 1; w < WAVES; ++w) s = joined(s, wave_sums[w]);
+    }
     const Row r(s);
-    if (threadIdx.x == 0) write_row<T>(a, d, row, s, r);
+    if (in == 0) write_row<T>(a, d, row, s, r);
     if (TOP && wave == 0) {
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) list = join64(list, lists[w * kWave + lane]);
+      for (int w = 1; w < WAVES; ++w) list = join64(list, lists[w * kWave + lane]);
       write_top(a, d, row, r, list);
     }
-    __syncthreads();
+    if (WAVES > 1) __syncthreads();
   }
 }
 
@@ -492,9 +496,14 @@ bl_status_t forward(const bl_logprob_plan_s* p, const Ptrs& a, hipStream_t s) {
   });
   if (st != BL_OK || p->pieces == 1) return st;
   const double left = (double)d.rows * p->pieces * (12 + 8 * d.top);
+  const bool by_waves = p->pieces <= kWave && (long)p->pieces * d.top <= 2 * kWave;
+  const long long join = by_waves ? (d.rows + kWaves - 1) / kWaves : d.rows;
   return timed_launch("logprob_join", left, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-    hipExtLaunchKernelGGL((k_logprob_join<T, TOP>), dim3((unsigned)std::min<long long>(d.rows, kGrid)), dim3(kT), 0, s,
-                          e0, e1, 0, a, d, p->pieces);
+    auto go = [&](auto kernel) {
+      hipExtLaunchKernelGGL(kernel, dim3((unsigned)std::min<long long>(join, kGrid)), dim3(kT), 0, s, e0, e1, 0, a, d,
+                            p->pieces);
+    };
+    by_waves ? go(k_logprob_join<T, 1, TOP>) : go(k_logprob_join<T, kWaves, TOP>);
   });
 }
 
@@ -546,7 +555,9 @@ extern "C" bl_status_t bl_logprob_plan_create(bl_logprob_plan_t* out, const bl_l
   if (!p) return BL_ERR_OOM;
   p->d = d;
   p->block = d.classes > kWaveClasses;
-  const long most = kPieceVectors * (16 / dtype_bytes(d.dtype));
+  long most = kPieceVectors * (16 / dtype_bytes(d.dtype));
+  // few rows in pieces anyway: smaller ones, until there is one for each compute unit
+  while (d.classes > kPieceVectors * (16 / dtype_bytes(d.dtype)) && most > kWaveClasses && d.rows * ((d.classes + most - 1) / most) < 256) most /= 2;
   p->pieces = p->block ? (int)((d.classes + most - 1) / most) : 1;
   p->piece = p->pieces == 1 ? (long)d.classes : ((d.classes + p->pieces - 1) / p->pieces + 15) / 16 * 16;
   p->each = vectors_of(p->piece, p->block ? kT : kWave, dtype_bytes(d.dtype));
