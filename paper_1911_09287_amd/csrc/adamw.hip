@@ -22,6 +22,7 @@ constexpr int kWaves = kT / kWave;
 constexpr int kChunk = 1024;    // tensors start at multiples of this many elements of the layout
 constexpr int kBlock = 128;     // elements that share a power of two: four on each of 32 lanes
 constexpr int kTensors = 128;   // of one launch: their list is part of the kernel's arguments (4 KB at most)
+constexpr int kFewTensors = 16; // 3 KB of arguments cost 1.7 us a launch: few tensors go in a short list
 
 constexpr long long kMostChunks = (1LL << 26) - 1;  // of one launch, which has fewer than 2^32 threads
 constexpr long long kMostBlocks = (1LL << 24) - 1;  // likewise, in blocks of kT threads
@@ -29,11 +30,12 @@ constexpr long long kMostBlocks = (1LL << 24) - 1;  // likewise, in blocks of kT
 // The tensors of a launch; tensor i has chunks first[i] ... first[i + 1] - 1 of
 // the layout (all ones past the last), |tail| elements in the last one, weight
 // decay where tail < 0.
+template <int N>
 struct TensorList {
-  void* p[kTensors];
-  const void* g[kTensors];
-  unsigned first[kTensors + 1];
-  short tail[kTensors];
+  void* p[N];
+  const void* g[N];
+  unsigned first[N + 1];
+  short tail[N];
   unsigned chunks;
 };
 
@@ -152,8 +154,8 @@ __device__ __forceinline__ bf16_t round_param<bf16_t>(float x, unsigned h) {
 // sqrt and reciprocal are the vector unit's, off by an ulp each.  Bound by HBM:
 // 126 million values with moments of 8 bits, gradients in bfloat16: 327 us,
 // 5.4 TB/s (a large copy reaches 5.0).
-template <typename P, typename G, int BITS, int V, bool LIVE>
-__global__ __launch_bounds__(kT) void k_adamw(const TensorList list, StepArgs a) {
+template <typename P, typename G, int BITS, int V, bool LIVE, int N>
+__global__ __launch_bounds__(kT) void k_adamw(const TensorList<N> list, StepArgs a) {
   constexpr int kParts = kChunk / (256 * V);
   const unsigned lane = threadIdx.x & 63;
   const unsigned wave = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + (threadIdx.x >> 6));
@@ -178,8 +180,9 @@ __global__ __launch_bounds__(kT) void k_adamw(const TensorList list, StepArgs a)
     }
   }
   // the tensor: how many start at or before this chunk, less one
-  const unsigned t = __builtin_amdgcn_readfirstlane(__popcll(__ballot(list.first[1 + lane] <= chunk)) +
-                                                    __popcll(__ballot(list.first[65 + lane] <= chunk)));
+  int before = __popcll(__ballot((int)lane < N && list.first[1 + (lane < N ? lane : 0)] <= chunk));
+  if (N > kWave) before += __popcll(__ballot(list.first[1 + (N > kWave ? kWave : 0) + lane] <= chunk));
+  const unsigned t = __builtin_amdgcn_readfirstlane(before);
   const int tail = list.tail[t];
   const int n = (chunk + 1 == list.first[t + 1] ? abs(tail) : kChunk) - (int)from;  // from this lane's first on
   const size_t off = (size_t)(chunk - list.first[t]) * kChunk + from;               // in the tensor
@@ -287,6 +290,16 @@ StepArgs state_of(const bl_adamw_plan_s* p, const void* state) {
   return a;
 }
 
+TensorList<kFewTensors> few_of(const TensorList<kTensors>& l) {
+  TensorList<kFewTensors> f;
+  std::copy_n(l.p, kFewTensors, f.p);
+  std::copy_n(l.g, kFewTensors, f.g);
+  std::copy_n(l.first, kFewTensors + 1, f.first);
+  std::copy_n(l.tail, kFewTensors, f.tail);
+  f.chunks = l.chunks;
+  return f;
+}
+
 // Chunks from which on a wave takes a whole chunk: fewer are spread thinner.
 constexpr unsigned kWholeChunks = 4096;
 
@@ -295,7 +308,7 @@ bl_status_t step(const bl_adamw_plan_s* p, void* const* params, const void* cons
                  hipStream_t s) {
   const int count = (int)p->sizes.size();
   for (int at = 0; at < count;) {
-    TensorList list;
+    TensorList<kTensors> list{};
     int n = 0;
     double values = 0;
     for (; at < count && n < kTensors; ++at) {
@@ -317,9 +330,13 @@ bl_status_t step(const bl_adamw_plan_s* p, void* const* params, const void* cons
     const bool whole = list.chunks >= kWholeChunks;
     const unsigned blocks = (unsigned)(((size_t)list.chunks * (whole ? 1 : 4) + kWaves - 1) / kWaves);
     const bl_status_t st = timed_launch("adamw", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-      auto go = [&](auto kernel) { hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(kT), 0, s, e0, e1, 0, list, a); };
-      if (a.live) whole ? go(k_adamw<P, G, BITS, 4, true>) : go(k_adamw<P, G, BITS, 1, true>);
-      else whole ? go(k_adamw<P, G, BITS, 4, false>) : go(k_adamw<P, G, BITS, 1, false>);
+      auto go = [&](auto kernel, const auto& l) {
+        hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(kT), 0, s, e0, e1, 0, l, a);
+      };
+      if (a.live) whole ? go(k_adamw<P, G, BITS, 4, true, kTensors>, list) : go(k_adamw<P, G, BITS, 1, true, kTensors>, list);
+      else if (whole) go(k_adamw<P, G, BITS, 4, false, kTensors>, list);
+      else if (n > kFewTensors) go(k_adamw<P, G, BITS, 1, false, kTensors>, list);
+      else go(k_adamw<P, G, BITS, 1, false, kFewTensors>, few_of(list));
     });
     if (st != BL_OK) return st;
   }

@@ -8,34 +8,39 @@
 namespace blc {
 namespace {
 
-// Sums of partial rows part[parts][2 size] by columns: 64 columns and 16 slices
+// Sums of partial rows part[parts][2 size] by columns: 64 columns and SLICES slices
 // of the rows a block, each slice in order with four loads in flight, then the
-// slices in order.  (One thread a column would wait for `parts` loads in turn.)
-constexpr int kCols = 64, kSlices = 16;
-template <typename T>
-__global__ __launch_bounds__(kCols* kSlices) void k_norm_sum(const float* part, int parts, long size, void* dw,
-                                                             void* db, bool wide) {
-  __shared__ float red[kSlices][kCols];
+// slices in order.  (One thread a column would wait for many parts in turn; few
+// parts leave slices without work.)
+constexpr int kCols = 64;
+template <typename T, int SLICES>
+__global__ __launch_bounds__(kCols* SLICES) void k_norm_sum(const float* part, int parts, long size, void* dw,
+                                                            void* db, bool wide) {
+  __shared__ float red[SLICES][kCols];
   const int col = threadIdx.x % kCols, slice = threadIdx.x / kCols;
   const long n = 2 * size, c = (long)blockIdx.x * kCols + col;
   float acc[4] = {};
   if (c < n) {
     int r = slice;
-    for (; r + 3 * kSlices < parts; r += 4 * kSlices) {
+    for (; r + 3 * SLICES < parts; r += 4 * SLICES) {
       float v[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = part[(size_t)(r + k * kSlices) * n + c];
+      for (int k = 0; k < 4; ++k) v[k] = part[(size_t)(r + k * SLICES) * n + c];
 #pragma unroll
       for (int k = 0; k < 4; ++k) acc[k] += v[k];
     }
-    for (int k = 0; r < parts; r += kSlices, ++k) acc[k] += part[(size_t)r * n + c];
+    for (int k = 0; r < parts; r += SLICES, ++k) acc[k] += part[(size_t)r * n + c];
   }
-  red[slice][col] = (acc[0] + acc[1]) + (acc[2] + acc[3]);
-  __syncthreads();
-  if (slice || c >= n) return;
-  float sum = 0.f;
+  float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+  if (SLICES > 1) {
+    red[slice][col] = sum;
+    __syncthreads();
+    if (slice) return;
+    sum = 0.f;
 #pragma unroll
-  for (int k = 0; k < kSlices; ++k) sum += red[k][col];
+    for (int k = 0; k < SLICES; ++k) sum += red[k][col];
+  }
+  if (c >= n) return;
   void* out = c < size ? dw : db;
   const long i = c < size ? c : c - size;
   if (!out) return;
@@ -48,14 +53,14 @@ __global__ __launch_bounds__(kCols* kSlices) void k_norm_sum(const float* part, 
 bl_status_t norm_sum_parts(const bl_norm_plan_s* p, const NormPtrs& a, int parts, hipStream_t s) {
   if (!a.dw && !a.db) return BL_OK;
   const unsigned blocks = (unsigned)((2 * p->d.size + kCols - 1) / kCols);
-  const bool wide = p->d.wdtype == BL_F32;
+  const bool wide = p->d.wdtype == BL_F32, few = parts <= 16;
   return timed_launch("norm_sum", 8.0 * parts * p->d.size, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-    if (p->d.dtype == BL_BF16)
-      hipExtLaunchKernelGGL(k_norm_sum<bf16_t>, dim3(blocks), dim3(kCols * kSlices), 0, s, e0, e1, 0, a.part, parts,
+    auto go = [&](auto kernel, int slices) {
+      hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(kCols * slices), 0, s, e0, e1, 0, a.part, parts,
                             (long)p->d.size, a.dw, a.db, wide);
-    else
-      hipExtLaunchKernelGGL(k_norm_sum<f16_t>, dim3(blocks), dim3(kCols * kSlices), 0, s, e0, e1, 0, a.part, parts,
-                            (long)p->d.size, a.dw, a.db, wide);
+    };
+    if (p->d.dtype == BL_F16) few ? go(k_norm_sum<f16_t, 1>, 1) : go(k_norm_sum<f16_t, 16>, 16);
+    else few ? go(k_norm_sum<bf16_t, 1>, 1) : go(k_norm_sum<bf16_t, 16>, 16);
   });
 }
 

@@ -15,8 +15,8 @@ struct bl_norm_plan_s {
   bl_norm_desc_t d;
   bl_norm_rows fwd, bwd;     // inner = 1, not split
   bool fwd_split, bwd_split; // inner = 1: each row by several blocks, in two launches
-  int chunks;                // split: blocks a row
-  long chunk;                // split: elements of one, a multiple of its tile
+  int pieces;                // split: waves a row, four of a block
+  long piece;                // split: elements of one, a multiple of its tile
   int row_groups;            // split backward: blocks a chunk, over rows
   // inner > 1, forward and backward: threads of a block, positions of a thread,
   // lanes along positions and channels of a thread (0: read again for every use)

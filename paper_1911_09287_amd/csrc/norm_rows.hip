@@ -208,91 +208,89 @@ __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_bwd(NormPtrs
 }
 
 // ---- rows over several blocks ---------------------------------------------------
-constexpr int kTileVecs = 4;  // vectors of a thread that are in flight together
+// A block takes a chunk of a row, each of its waves a piece of that, in tiles of
+// four vectors a lane that are in flight together.  The first launch leaves two sums
+// for each piece; no wave waits for another.
+constexpr int kTileVecs = 4;
+constexpr int kBlockWaves = kT / kWave;
+constexpr int kMostChunks = kT / kBlockWaves;  // so that a block joins a row's pieces, one a thread
 
-// Sum over a block of kT threads, for every thread.
-template <int N>
-__device__ __forceinline__ void block_sum(float (&x)[N], float (*red)[kT / kWave]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
-  __syncthreads();
-  if (threadIdx.x % kWave == 0)
-#pragma unroll
-    for (int i = 0; i < N; ++i) red[i][threadIdx.x / kWave] = x[i];
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    x[i] = 0.f;
-#pragma unroll
-    for (int k = 0; k < kT / kWave; ++k) x[i] += red[i][k];
-  }
+struct Split {
+  long piece;   // elements of a wave, a multiple of its tile
+  int pieces;   // of a row, kBlockWaves a block
+};
+template <typename T>
+__device__ __forceinline__ long wave_tile() {
+  return (long)kWave * (16 / (int)sizeof(T)) * kTileVecs;
 }
 
-// Forward: mean and sum of squared differences from it of one chunk of one row.
-// A tile's are exact to fp32 (the mean first), tiles are joined by the sums'
-// update for two sets: n, mean and M2 of both give n, mean and M2 of the union.
+// Sum over a block of kT threads, for every thread.
+__device__ __forceinline__ float block_sum(float x, float* red) {
+  x = wave_sum(x);
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = x;
+  __syncthreads();
+  return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// Forward: mean and sum of squared differences from it of one piece of one row.  A
+// tile's are exact to fp32 (the mean first), tiles are joined by the update for two
+// sets: n, mean and M2 of both give n, mean and M2 of the union.
 template <typename T>
-__global__ __launch_bounds__(kT) void k_split_stats(NormPtrs a, bl_norm_desc_t d, long chunk, int chunks) {
-  constexpr int V = 16 / sizeof(T), tile = kT * V * kTileVecs;
-  __shared__ float red[1][kT / kWave];
-  const long row = blockIdx.x / (unsigned)chunks, piece = blockIdx.x % (unsigned)chunks;
-  const long from = piece * chunk, to = min((long)d.size, from + chunk);
+__global__ __launch_bounds__(kT) void k_split_stats(NormPtrs a, bl_norm_desc_t d, Split c) {
+  constexpr int V = 16 / sizeof(T);
+  const int chunks = c.pieces / kBlockWaves, lane = threadIdx.x % kWave;
+  const long row = blockIdx.x / (unsigned)chunks;
+  const int piece = blockIdx.x % (unsigned)chunks * kBlockWaves + threadIdx.x / kWave;
+  const long from = piece * c.piece, to = min((long)d.size, from + c.piece);
   const T* x = static_cast<const T*>(a.x) + row * d.x_stride;
   float n = 0.f, mean = 0.f, m2 = 0.f;
-  for (long at = from; at < to; at += tile) {
+  for (long at = from; at < to; at += wave_tile<T>()) {
     Held<T, V> v[kTileVecs];
-    float s[1] = {0.f};
+    float s = 0.f, q = 0.f;
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k) {
-      const long i = at + (long)(threadIdx.x + k * kT) * V;
+      const long i = at + (long)(lane + k * kWave) * V;
       v[k].load(x + i, to - i);
     }
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k) {
       v[k].refresh();
 #pragma unroll
-      for (int j = 0; j < V; ++j) s[0] += v[k][j];
+      for (int j = 0; j < V; ++j) s += v[k][j];
     }
-    block_sum(s, red);
-    const float nt = (float)min((long)tile, to - at), mt = s[0] / nt;
-    s[0] = 0.f;
+    const float nt = (float)min(wave_tile<T>(), to - at), mt = wave_sum(s) / nt;
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float c = v[k][j] - mt;
-        s[0] += at + (long)(threadIdx.x + k * kT) * V + j < to ? c * c : 0.f;
+        const float c0 = v[k][j] - mt;
+        q += at + (long)(lane + k * kWave) * V + j < to ? c0 * c0 : 0.f;
       }
-    block_sum(s, red);
     const float all = n + nt, diff = mt - mean;
     mean += diff * (nt / all);
-    m2 += s[0] + diff * diff * (n * nt / all);
+    m2 += wave_sum(q) + diff * diff * (n * nt / all);
     n = all;
   }
-  if (threadIdx.x == 0) {
-    float* o = a.sums + (size_t)blockIdx.x * 2;
-    o[0] = mean;
-    o[1] = m2;
-  }
+  if (lane < 2) a.sums[((size_t)row * c.pieces + piece) * 2 + lane] = lane ? m2 : mean;
 }
 
 template <typename T>
-__global__ __launch_bounds__(kT) void k_split_fwd(NormPtrs a, bl_norm_desc_t d, long chunk, int chunks) {
+__global__ __launch_bounds__(kT) void k_split_fwd(NormPtrs a, bl_norm_desc_t d, Split c) {
   constexpr int V = 16 / sizeof(T);
-  __shared__ float red[1][kT / kWave];
-  const long row = blockIdx.x / (unsigned)chunks, piece = blockIdx.x % (unsigned)chunks;
-  const long from = piece * chunk, to = min((long)d.size, from + chunk);
-  const float* sums = a.sums + (size_t)row * chunks * 2;
-  const bool mine = (int)threadIdx.x < chunks;
-  const float nc = mine ? (float)min(chunk, (long)d.size - (long)threadIdx.x * chunk) : 0.f;
+  __shared__ float red[kBlockWaves];
+  const int chunks = c.pieces / kBlockWaves;
+  const long row = blockIdx.x / (unsigned)chunks, chunk = c.piece * kBlockWaves;
+  const long from = blockIdx.x % (unsigned)chunks * chunk, to = min((long)d.size, from + chunk);
+  const float* sums = a.sums + (size_t)row * c.pieces * 2;
+  const long rest = (long)d.size - (long)threadIdx.x * c.piece;  // from this thread's piece on
+  const bool mine = (int)threadIdx.x < c.pieces && rest > 0;
+  const float nc = mine ? (float)min(c.piece, rest) : 0.f;
   const float mc = mine ? sums[2 * threadIdx.x] : 0.f, m2 = mine ? sums[2 * threadIdx.x + 1] : 0.f;
-  float s[1] = {nc * mc};
-  block_sum(s, red);
-  const float mean = s[0] / (float)d.size;
-  s[0] = m2 + nc * (mc - mean) * (mc - mean);
-  block_sum(s, red);
-  const float rstd = 1.f / sqrtf(s[0] / (float)d.size + (float)d.eps);
-  if (a.stats && piece == 0 && threadIdx.x == 0) {
+  const float mean = block_sum(nc * mc, red) / (float)d.size;
+  const float var = block_sum(m2 + nc * (mc - mean) * (mc - mean), red) / (float)d.size;
+  const float rstd = 1.f / sqrtf(var + (float)d.eps);
+  if (a.stats && from == 0 && threadIdx.x == 0) {
     a.stats[row] = mean;
     a.stats[d.outer + row] = rstd;
   }
@@ -321,27 +319,28 @@ __global__ __launch_bounds__(kT) void k_split_fwd(NormPtrs a, bl_norm_desc_t d, 
   }
 }
 
-// Backward: sums of u and u h of one chunk of one row.
+// Backward: sums of u and u h of one piece of one row.
 template <typename T>
-__global__ __launch_bounds__(kT) void k_split_sums(NormPtrs a, bl_norm_desc_t d, long chunk, int chunks) {
+__global__ __launch_bounds__(kT) void k_split_sums(NormPtrs a, bl_norm_desc_t d, Split c) {
   constexpr int V = 16 / sizeof(T);
-  __shared__ float red[2][kT / kWave];
-  const long row = blockIdx.x / (unsigned)chunks, piece = blockIdx.x % (unsigned)chunks;
-  const long from = piece * chunk, to = min((long)d.size, from + chunk);
+  const int chunks = c.pieces / kBlockWaves, lane = threadIdx.x % kWave;
+  const long row = blockIdx.x / (unsigned)chunks;
+  const int piece = blockIdx.x % (unsigned)chunks * kBlockWaves + threadIdx.x / kWave;
+  const long from = piece * c.piece, to = min((long)d.size, from + c.piece);
   const T* x = static_cast<const T*>(a.x) + row * d.x_stride;
   const T* dy = static_cast<const T*>(a.dy) + row * d.y_stride;
   const float mean = a.stats[row], rstd = a.stats[d.outer + row];
-  float s[2] = {0.f, 0.f};
-  for (long at = from; at < to; at += (long)kT * V * kTileVecs) {
+  float s0 = 0.f, s1 = 0.f;
+  for (long at = from; at < to; at += wave_tile<T>()) {
     Held<T, V> v[kTileVecs], g[kTileVecs];
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k) {
-      const long i = at + (long)(threadIdx.x + k * kT) * V;
+      const long i = at + (long)(lane + k * kWave) * V;
       v[k].load(x + i, to - i);
       g[k].load(dy + i, to - i);
     }
     float w[kTileVecs][V];
-    load_weights<T, V, kTileVecs>(a.w, d.wdtype == BL_F32, at + (long)threadIdx.x * V, kT * V, to, 1.f, w);
+    load_weights<T, V, kTileVecs>(a.w, d.wdtype == BL_F32, at + (long)lane * V, kWave * V, to, 1.f, w);
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k) {
       v[k].refresh();
@@ -349,53 +348,74 @@ __global__ __launch_bounds__(kT) void k_split_sums(NormPtrs a, bl_norm_desc_t d,
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float h = (v[k][j] - mean) * rstd, u = g[k][j] * w[k][j];
-        s[0] += u;
-        s[1] = fmaf(u, h, s[1]);
+        s0 += u;
+        s1 = fmaf(u, h, s1);
       }
     }
   }
-  block_sum(s, red);
-  if (threadIdx.x == 0) {
-    float* o = a.sums + (size_t)blockIdx.x * 2;
-    o[0] = s[0];
-    o[1] = s[1];
-  }
+  s0 = wave_sum(s0);
+  s1 = wave_sum(s1);
+  if (lane < 2) a.sums[((size_t)row * c.pieces + piece) * 2 + lane] = lane ? s1 : s0;
 }
 
 // dx of one chunk of every groups-th row, and this block's sums by column,
-// [group][2][M].  One vector a thread, so that the sums stay in registers.
+// [group][2][M].  One vector a thread, so that the sums stay in registers, and four
+// rows in flight together.
+constexpr int kRowsFlying = 4;
+constexpr int kRowsKnown = 128;  // rows whose statistics are in LDS at a time
 template <typename T>
-__global__ __launch_bounds__(kT) void k_split_bwd(NormPtrs a, bl_norm_desc_t d, long chunk, int chunks,
-                                                  int groups, bool sums) {
+__global__ __launch_bounds__(kT) void k_split_bwd(NormPtrs a, bl_norm_desc_t d, Split c, int groups, bool sums) {
   constexpr int V = 16 / sizeof(T);
-  __shared__ float red[2][kT / kWave];
+  __shared__ float4 known[kRowsKnown];  // mean, rstd and the means of u and u h
+  const int chunks = c.pieces / kBlockWaves, lane = threadIdx.x % kWave;
+  const long chunk = c.piece * kBlockWaves, M = d.size;
   const long first = blockIdx.x / (unsigned)chunks, from = blockIdx.x % (unsigned)chunks * chunk;
-  const long to = min((long)d.size, from + chunk), M = d.size;
-  const float inv = 1.f / (float)M;
+  const long to = min(M, from + chunk), rows = (d.outer - first + groups - 1) / groups;  // of this block
   for (long at = from; at < to; at += (long)kT * V) {
     const long i = at + (long)threadIdx.x * V;
     float w[1][V], aw[V] = {}, ab[V] = {};
     load_weights<T, V, 1>(a.w, d.wdtype == BL_F32, i, 0, to, 1.f, w);
-    for (long row = first; row < d.outer; row += groups) {
-      Held<T, V> v, g;
-      v.load(static_cast<const T*>(a.x) + row * d.x_stride + i, to - i);
-      g.load(static_cast<const T*>(a.dy) + row * d.y_stride + i, to - i);
-      const float* all = a.sums + (size_t)row * chunks * 2;
-      float s[2] = {0.f, 0.f};
-      if ((int)threadIdx.x < chunks) s[0] = all[2 * threadIdx.x], s[1] = all[2 * threadIdx.x + 1];
-      block_sum(s, red);
-      const float mean = a.stats[row], rstd = a.stats[d.outer + row], c1 = s[0] * inv, c2 = s[1] * inv;
-      v.refresh();
-      g.refresh();
-      Pack<T, V> o;
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float h = (v[j] - mean) * rstd, dyj = g[j];
-        aw[j] = fmaf(dyj, h, aw[j]);
-        ab[j] += dyj;
-        o.v[j] = (T)(rstd * (fmaf(dyj, w[0][j], -c1) - h * c2));
+    for (long r0 = 0; r0 < rows; r0 += kRowsKnown) {
+      const int n = (int)min((long)kRowsKnown, rows - r0);
+      if (at == from || rows > kRowsKnown) {
+        __syncthreads();
+        for (int r = threadIdx.x / kWave; r < n; r += kBlockWaves) {
+          const long row = first + (r0 + r) * groups;
+          const float* all = a.sums + (size_t)row * c.pieces * 2;
+          float s0 = 0.f, s1 = 0.f;
+          for (int p = lane; p < c.pieces; p += kWave) s0 += all[2 * p], s1 += all[2 * p + 1];
+          s0 = wave_sum(s0);
+          s1 = wave_sum(s1);
+          if (lane == 0) known[r] = make_float4(a.stats[row], a.stats[d.outer + row], s0 / (float)M, s1 / (float)M);
+        }
+        __syncthreads();
       }
-      store_part<T, V>(static_cast<T*>(a.dx) + row * d.x_stride + i, to - i, o);
+      for (int r = 0; r < n; r += kRowsFlying) {
+        Held<T, V> v[kRowsFlying], g[kRowsFlying];
+#pragma unroll
+        for (int k = 0; k < kRowsFlying; ++k) {
+          const long row = first + (r0 + r + k) * groups, left = r + k < n ? to - i : 0;
+          v[k].load(static_cast<const T*>(a.x) + row * d.x_stride + i, left);
+          g[k].load(static_cast<const T*>(a.dy) + row * d.y_stride + i, left);
+        }
+#pragma unroll
+        for (int k = 0; k < kRowsFlying; ++k) {
+          if (r + k >= n) break;
+          const long row = first + (r0 + r + k) * groups;
+          const float4 t = known[r + k];
+          v[k].refresh();
+          g[k].refresh();
+          Pack<T, V> o;
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const float h = (v[k][j] - t.x) * t.y, dyj = g[k][j];
+            aw[j] = fmaf(dyj, h, aw[j]);
+            ab[j] += dyj;
+            o.v[j] = (T)(t.y * (fmaf(dyj, w[0][j], -t.z) - h * t.w));
+          }
+          store_part<T, V>(static_cast<T*>(a.dx) + row * d.x_stride + i, to - i, o);
+        }
+      }
     }
     if (!sums) continue;
     float* part = a.part + (size_t)first * 2 * M;
@@ -466,14 +486,15 @@ bl_status_t launch_bwd(const bl_norm_plan_s* p, const NormPtrs& a, bool sums, hi
 template <typename T>
 bl_status_t forward(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s) {
   if (!p->fwd_split) return p->fwd.block ? launch_fwd<T, true>(p, a, s) : launch_fwd<T, false>(p, a, s);
-  const dim3 grid((unsigned)(p->chunks * p->d.outer));
+  const dim3 grid((unsigned)(p->pieces / kBlockWaves * p->d.outer));
+  const Split c{p->piece, p->pieces};
   const double bytes = (double)p->d.outer * p->d.size * sizeof(T);
   const bl_status_t st = timed_launch("norm_stats", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-    hipExtLaunchKernelGGL(k_split_stats<T>, grid, dim3(kT), 0, s, e0, e1, 0, a, p->d, p->chunk, p->chunks);
+    hipExtLaunchKernelGGL(k_split_stats<T>, grid, dim3(kT), 0, s, e0, e1, 0, a, p->d, c);
   });
   if (st != BL_OK) return st;
   return timed_launch("norm_fwd", 2 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-    hipExtLaunchKernelGGL(k_split_fwd<T>, grid, dim3(kT), 0, s, e0, e1, 0, a, p->d, p->chunk, p->chunks);
+    hipExtLaunchKernelGGL(k_split_fwd<T>, grid, dim3(kT), 0, s, e0, e1, 0, a, p->d, c);
   });
 }
 
@@ -484,15 +505,17 @@ bl_status_t backward(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s) 
   if (!p->bwd_split) {
     st = p->bwd.block ? launch_bwd<T, true>(p, a, sums, s) : launch_bwd<T, false>(p, a, sums, s);
   } else {
+    const unsigned chunks = p->pieces / kBlockWaves;
+    const Split c{p->piece, p->pieces};
     const double bytes = (double)p->d.outer * p->d.size * sizeof(T);
     st = timed_launch("norm_sums", 2 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-      hipExtLaunchKernelGGL(k_split_sums<T>, dim3((unsigned)(p->chunks * p->d.outer)), dim3(kT), 0, s, e0, e1, 0, a,
-                            p->d, p->chunk, p->chunks);
+      hipExtLaunchKernelGGL(k_split_sums<T>, dim3((unsigned)(chunks * p->d.outer)), dim3(kT), 0, s, e0, e1, 0, a, p->d,
+                            c);
     });
     if (st != BL_OK) return st;
     st = timed_launch("norm_bwd", 3 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-      hipExtLaunchKernelGGL(k_split_bwd<T>, dim3((unsigned)(p->chunks * p->row_groups)), dim3(kT), 0, s, e0, e1, 0, a,
-                            p->d, p->chunk, p->chunks, p->row_groups, sums);
+      hipExtLaunchKernelGGL(k_split_bwd<T>, dim3(chunks * p->row_groups), dim3(kT), 0, s, e0, e1, 0, a, p->d, c,
+                            p->row_groups, sums);
     });
   }
   return st == BL_OK && sums ? norm_sum_parts(p, a, p->parts, s) : st;
@@ -510,16 +533,18 @@ bl_status_t norm_rows_plan(bl_norm_plan_s* p) {
   p->bwd_split = !p->bwd.threads;
   if (p->fwd_split || p->bwd_split) {
     const long tile = (long)kT * V * kTileVecs;
-    const long chunks = std::min<long>(kT, (M + tile - 1) / tile);
-    p->chunk = ((M + chunks - 1) / chunks + tile - 1) / tile * tile;
-    p->chunks = (int)((M + p->chunk - 1) / p->chunk);
-    if (rows * p->chunks >= kMostBlocks) return BL_ERR_UNSUPPORTED;
+    long chunks = std::min<long>(kMostChunks, (M + tile - 1) / tile);
+    const long chunk = ((M + chunks - 1) / chunks + tile - 1) / tile * tile;
+    chunks = (M + chunk - 1) / chunk;
+    if (rows * chunks >= kMostBlocks) return BL_ERR_UNSUPPORTED;
+    p->piece = chunk / kBlockWaves;
+    p->pieces = (int)chunks * kBlockWaves;
     p->off_sums = 0;
-    p->bytes = round_up((size_t)rows * p->chunks * 2 * sizeof(float), 256);
+    p->bytes = round_up((size_t)rows * p->pieces * 2 * sizeof(float), 256);
   }
   p->off_part = p->bytes;
   if (p->bwd_split) {
-    p->row_groups = (int)std::min<long>(rows, std::max<long>(1, kTargetBlocks / p->chunks));
+    p->row_groups = (int)std::min<long>(rows, std::max<long>(1, kTargetBlocks / (p->pieces / kBlockWaves)));
     p->parts = p->row_groups;
   } else {
     const long each = p->bwd.block ? 1 : kT / p->bwd.threads;
