@@ -17,6 +17,7 @@ namespace {
 constexpr int kT = kNormThreads;
 constexpr int kMostThreads = 1024;
 constexpr int kTargetBlocks = 512;  // two a compute unit
+constexpr int kSplitBlocks = 1792;  // seven a compute unit
 
 // ---- sums over the lanes of a row ---------------------------------------------
 // BLOCK: over the block, by way of LDS; `red` alternates between two arrays from
@@ -41,7 +42,7 @@ __device__ __forceinline__ void row_sum(float (&x)[N], int lanes, float (*red)[k
   }
 }
 
-// E vectors of 16 bytes a lane.  Weights of few are kept over a block's rows.
+// E vectors of 16 bytes a lane; their weights are kept over a block's rows.
 template <typename T, int E, bool BLOCK>
 __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_fwd(NormPtrs a, bl_norm_desc_t d, int lanes) {
   constexpr int V = 16 / sizeof(T);
@@ -50,12 +51,9 @@ __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_fwd(NormPtrs
   const long rows = d.outer, M = d.size;
   const long each = BLOCK ? 1 : kT / lanes;
   const bool wide = d.wdtype == BL_F32;
-  constexpr bool keep = E * V <= 32;
-  float w[keep ? E : 1][V], b[keep ? E : 1][V];
-  if constexpr (keep) {
-    load_weights<T, V, E>(a.w, wide, (long)in * V, (long)step * V, M, 1.f, w);
-    load_weights<T, V, E>(a.b, wide, (long)in * V, (long)step * V, M, 0.f, b);
-  }
+  float w[E][V], b[E][V];
+  load_weights<T, V, E>(a.w, wide, (long)in * V, (long)step * V, M, 1.f, w);
+  load_weights<T, V, E>(a.b, wide, (long)in * V, (long)step * V, M, 0.f, b);
   for (long row = blockIdx.x * each + (BLOCK ? 0 : threadIdx.x / lanes); row < rows; row += gridDim.x * each) {
     const T* x = static_cast<const T*>(a.x) + row * d.x_stride;
     T* y = static_cast<T*>(a.y) + row * d.y_stride;
@@ -90,14 +88,9 @@ __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_fwd(NormPtrs
 #pragma unroll
     for (int k = 0; k < E; ++k) {
       const long i = (long)(in + k * step) * V;
-      const int at = keep ? k : 0;
-      if constexpr (!keep) {
-        load_weights<T, V, 1>(a.w, wide, i, 0, M, 1.f, w);
-        load_weights<T, V, 1>(a.b, wide, i, 0, M, 0.f, b);
-      }
       Pack<T, V> o;
 #pragma unroll
-      for (int j = 0; j < V; ++j) o.v[j] = (T)fmaf((v[k][j] - mean) * rstd, w[at][j], b[at][j]);
+      for (int j = 0; j < V; ++j) o.v[j] = (T)fmaf((v[k][j] - mean) * rstd, w[k][j], b[k][j]);
       store_part<T, V>(y + i, M - i, o);
     }
     if (a.stats && in == 0) {
@@ -224,15 +217,6 @@ __device__ __forceinline__ long wave_tile() {
   return (long)kWave * (16 / (int)sizeof(T)) * kTileVecs;
 }
 
-// Sum over a block of kT threads, for every thread.
-__device__ __forceinline__ float block_sum(float x, float* red) {
-  x = wave_sum(x);
-  __syncthreads();
-  if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = x;
-  __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
-}
-
 // Forward: mean and sum of squared differences from it of one piece of one row.  A
 // tile's are exact to fp32 (the mean first), tiles are joined by the update for two
 // sets: n, mean and M2 of both give n, mean and M2 of the union.
@@ -275,46 +259,70 @@ __global__ __launch_bounds__(kT) void k_split_stats(NormPtrs a, bl_norm_desc_t d
   if (lane < 2) a.sums[((size_t)row * c.pieces + piece) * 2 + lane] = lane ? m2 : mean;
 }
 
+// y of one tile of two vectors a thread of every groups-th row.  The tile's weights
+// stay in registers over the rows (in 16 bits they are four times the values).
+constexpr int kFwdVecs = 2;
+constexpr int kRowsKnown = 128;  // rows whose statistics are in LDS at a time
 template <typename T>
-__global__ __launch_bounds__(kT) void k_split_fwd(NormPtrs a, bl_norm_desc_t d, Split c) {
-  constexpr int V = 16 / sizeof(T);
-  __shared__ float red[kBlockWaves];
-  const int chunks = c.pieces / kBlockWaves;
-  const long row = blockIdx.x / (unsigned)chunks, chunk = c.piece * kBlockWaves;
-  const long from = blockIdx.x % (unsigned)chunks * chunk, to = min((long)d.size, from + chunk);
-  const float* sums = a.sums + (size_t)row * c.pieces * 2;
-  const long rest = (long)d.size - (long)threadIdx.x * c.piece;  // from this thread's piece on
-  const bool mine = (int)threadIdx.x < c.pieces && rest > 0;
-  const float nc = mine ? (float)min(c.piece, rest) : 0.f;
-  const float mc = mine ? sums[2 * threadIdx.x] : 0.f, m2 = mine ? sums[2 * threadIdx.x + 1] : 0.f;
-  const float mean = block_sum(nc * mc, red) / (float)d.size;
-  const float var = block_sum(m2 + nc * (mc - mean) * (mc - mean), red) / (float)d.size;
-  const float rstd = 1.f / sqrtf(var + (float)d.eps);
-  if (a.stats && from == 0 && threadIdx.x == 0) {
-    a.stats[row] = mean;
-    a.stats[d.outer + row] = rstd;
-  }
-  const T* x = static_cast<const T*>(a.x) + row * d.x_stride;
-  T* y = static_cast<T*>(a.y) + row * d.y_stride;
-  const bool wide = d.wdtype == BL_F32;
-  for (long at = from; at < to; at += (long)kT * V * kTileVecs) {
-    Held<T, V> v[kTileVecs];
+__global__ __launch_bounds__(kT) void k_split_fwd(NormPtrs a, bl_norm_desc_t d, Split c, unsigned tiles, int groups) {
+  constexpr int V = 16 / sizeof(T), kJoin = kMostChunks * kBlockWaves / kWave;
+  __shared__ float2 known[kRowsKnown];  // mean and rstd
+  const int lane = threadIdx.x % kWave;
+  const long first = blockIdx.x / tiles, M = d.size;
+  const long i = ((long)(blockIdx.x % tiles) * kFwdVecs * kT + threadIdx.x) * V;  // and kT V further
+  const long rows = (d.outer - first + groups - 1) / groups;                      // of this block
+  const T* x = static_cast<const T*>(a.x) + first * d.x_stride + i;
+  T* y = static_cast<T*>(a.y) + first * d.y_stride + i;
+  Held<T, V> v[kFwdVecs];
 #pragma unroll
-    for (int k = 0; k < kTileVecs; ++k) {
-      const long i = at + (long)(threadIdx.x + k * kT) * V;
-      v[k].load(x + i, to - i);
+  for (int k = 0; k < kFwdVecs; ++k) v[k].load(x + k * kT * V, M - i - k * kT * V);
+  float w[kFwdVecs][V], b[kFwdVecs][V];
+  load_weights<T, V, kFwdVecs>(a.w, d.wdtype == BL_F32, i, kT * V, M, 1.f, w);
+  load_weights<T, V, kFwdVecs>(a.b, d.wdtype == BL_F32, i, kT * V, M, 0.f, b);
+  for (long r0 = 0; r0 < rows; r0 += kRowsKnown) {
+    const int n = (int)min((long)kRowsKnown, rows - r0);
+    if (r0) __syncthreads();
+    for (int r = threadIdx.x / kWave; r < n; r += kBlockWaves) {
+      const long row = first + (r0 + r) * groups;
+      const float* all = a.sums + (size_t)row * c.pieces * 2;
+      float mc[kJoin], nc[kJoin], s = 0.f, q = 0.f;
+#pragma unroll
+      for (int u = 0; u < kJoin; ++u) {
+        const int p = lane + u * kWave;
+        const long left = M - p * c.piece;
+        nc[u] = p < c.pieces && left > 0 ? (float)min(c.piece, left) : 0.f;
+        mc[u] = nc[u] > 0.f ? all[2 * p] : 0.f;
+        q += nc[u] > 0.f ? all[2 * p + 1] : 0.f;
+        s = fmaf(nc[u], mc[u], s);
+      }
+      const float mean = wave_sum(s) / (float)M;
+#pragma unroll
+      for (int u = 0; u < kJoin; ++u) q = fmaf(nc[u] * (mc[u] - mean), mc[u] - mean, q);
+      const float rstd = 1.f / sqrtf(wave_sum(q) / (float)M + (float)d.eps);
+      if (lane == 0) known[r] = make_float2(mean, rstd);
+      if (a.stats && blockIdx.x % tiles == 0 && lane == 0) {
+        a.stats[row] = mean;
+        a.stats[d.outer + row] = rstd;
+      }
     }
-    float w[kTileVecs][V], b[kTileVecs][V];
-    load_weights<T, V, kTileVecs>(a.w, wide, at + (long)threadIdx.x * V, kT * V, to, 1.f, w);
-    load_weights<T, V, kTileVecs>(a.b, wide, at + (long)threadIdx.x * V, kT * V, to, 0.f, b);
+    __syncthreads();
+    for (int r = 0; r < n; ++r) {
+      const float2 t = known[r];
+      Pack<T, V> o[kFwdVecs];
 #pragma unroll
-    for (int k = 0; k < kTileVecs; ++k) {
-      const long i = at + (long)(threadIdx.x + k * kT) * V;
-      v[k].refresh();
-      Pack<T, V> o;
+      for (int k = 0; k < kFwdVecs; ++k) {
+        v[k].refresh();
 #pragma unroll
-      for (int j = 0; j < V; ++j) o.v[j] = (T)fmaf((v[k][j] - mean) * rstd, w[k][j], b[k][j]);
-      store_part<T, V>(y + i, to - i, o);
+        for (int j = 0; j < V; ++j) o[k].v[j] = (T)fmaf((v[k][j] - t.x) * t.y, w[k][j], b[k][j]);
+      }
+      if (r0 + r + 1 < rows) {  // the next row is on its way while this one is stored
+        x += (long)groups * d.x_stride;
+#pragma unroll
+        for (int k = 0; k < kFwdVecs; ++k) v[k].load(x + k * kT * V, M - i - k * kT * V);
+      }
+#pragma unroll
+      for (int k = 0; k < kFwdVecs; ++k) store_part<T, V>(y + k * kT * V, M - i - k * kT * V, o[k]);
+      y += (long)groups * d.y_stride;
     }
   }
 }
@@ -362,7 +370,6 @@ __global__ __launch_bounds__(kT) void k_split_sums(NormPtrs a, bl_norm_desc_t d,
 // [group][2][M].  One vector a thread, so that the sums stay in registers, and four
 // rows in flight together.
 constexpr int kRowsFlying = 4;
-constexpr int kRowsKnown = 128;  // rows whose statistics are in LDS at a time
 template <typename T>
 __global__ __launch_bounds__(kT) void k_split_bwd(NormPtrs a, bl_norm_desc_t d, Split c, int groups, bool sums) {
   constexpr int V = 16 / sizeof(T);
@@ -463,7 +470,7 @@ bl_status_t launch_fwd(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s
     if (r.each == 1) go(k_rows_fwd<T, 1, BLOCK>);
     else if (r.each == 2) go(k_rows_fwd<T, 2, BLOCK>);
     else if (r.each == 4) go(k_rows_fwd<T, 4, BLOCK>);
-    else go(k_rows_fwd<T, 8, true>);
+    else go(k_rows_fwd<float, 8, true>);
   });
 }
 
@@ -493,8 +500,14 @@ bl_status_t forward(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s) {
     hipExtLaunchKernelGGL(k_split_stats<T>, grid, dim3(kT), 0, s, e0, e1, 0, a, p->d, c);
   });
   if (st != BL_OK) return st;
+  const long tile = (long)kT * (16 / (long)sizeof(T)) * kFwdVecs, tiles = (p->d.size + tile - 1) / tile;
+  // about the blocks that are on the GPU together, with as many rows each as the others
+  const long most = std::min<long>(p->d.outer, std::max<long>(1, kSplitBlocks / tiles));
+  const long each = (p->d.outer + most - 1) / most;
+  const int groups = (int)((p->d.outer + each - 1) / each);
   return timed_launch("norm_fwd", 2 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-    hipExtLaunchKernelGGL(k_split_fwd<T>, grid, dim3(kT), 0, s, e0, e1, 0, a, p->d, c);
+    hipExtLaunchKernelGGL(k_split_fwd<T>, dim3((unsigned)(tiles * groups)), dim3(kT), 0, s, e0, e1, 0, a, p->d, c,
+                          (unsigned)tiles, groups);
   });
 }
 
@@ -525,9 +538,9 @@ bl_status_t backward(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s) 
 
 bl_status_t norm_rows_plan(bl_norm_plan_s* p) {
   const long rows = p->d.outer, M = p->d.size, V = 16 / dtype_bytes(p->d.dtype), nv = (M + V - 1) / V;
-  // fp32 values of x, dy, w and two sums of 32 16-bit values a lane would not fit a
-  // block of 1024's registers
-  p->fwd = rows_shape(nv, 8, false);
+  // more would not fit the registers of a block of 1024 (with x, in fp32: w and b, or
+  // backward dy, w and two sums)
+  p->fwd = rows_shape(nv, p->d.dtype == BL_F32 ? 8 : 4, false);
   p->bwd = rows_shape(nv, p->d.dtype == BL_F32 ? 4 : 2, true);
   p->fwd_split = !p->fwd.threads;
   p->bwd_split = !p->bwd.threads;
