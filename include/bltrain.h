@@ -9,8 +9,9 @@
  * nothing from one call for the next, make no host synchronisation and enqueue
  * their kernels on `stream` (a hipStream_t, NULL = the default stream), so they
  * can be captured in a HIP graph.  A workspace is scratch: its contents before
- * and after a call mean nothing, and it must be aligned to 16 bytes.  Other
- * tensors need the alignment of their element type only.
+ * and after a call mean nothing.  Workspaces and AdamW's state must be aligned to
+ * 16 bytes (else BL_ERR_INVALID_ARG); tensors need the alignment of their element
+ * type only.
  *
  * Errors: every call returns a bl_status_t.  Arguments are validated on the
  * host before anything is enqueued; a call that returns an error other than
@@ -64,7 +65,8 @@ typedef struct {
 
 typedef struct bl_norm_plan_s* bl_norm_plan_t;
 
-/* BL_ERR_UNSUPPORTED: size * inner >= 2^31, or outer * inner >= 2^31. */
+/* BL_ERR_UNSUPPORTED: size * inner >= 2^31, outer * inner >= 2^31, or rows (inner =
+ * 1) of over 16384 elements in such a number that they are cut into 2^24 chunks. */
 bl_status_t bl_norm_plan_create(bl_norm_plan_t* out, const bl_norm_desc_t* desc);
 bl_status_t bl_norm_plan_destroy(bl_norm_plan_t plan);
 /* Workspace bytes of either call (0: ws may be NULL). */
@@ -181,7 +183,7 @@ typedef struct {
 
 typedef struct bl_adamw_plan_s* bl_adamw_plan_t;
 
-/* BL_ERR_UNSUPPORTED: a tensor of 2^36 elements or more, or 2^31 or more blocks of 1024. */
+/* BL_ERR_UNSUPPORTED: a tensor of 2^35 elements or more, or 2^31 or more blocks of 1024. */
 bl_status_t bl_adamw_plan_create(bl_adamw_plan_t* out, const bl_adamw_desc_t* desc);
 bl_status_t bl_adamw_plan_destroy(bl_adamw_plan_t plan);
 /* Bytes of the state, elements of each moment's array, and start[count] (any may be NULL). */
@@ -199,7 +201,8 @@ bl_status_t bl_adamw_step(bl_adamw_plan_t plan, void* const* params, const void*
  * bits = 8 (which holds every 8-bit value exactly); and from fp32 values, rounded
  * to nearest with bits = 8 (half away from zero; S is the largest power of two
  * below the block's largest magnitude, so that values which bl_adamw_get_moments
- * gave are held again exactly). */
+ * gave are held again exactly).  Elements between the tensors must be 0 in what is
+ * set, as they are in what is given. */
 bl_status_t bl_adamw_get_moments(bl_adamw_plan_t plan, const void* state, void* m, void* v, void* stream);
 bl_status_t bl_adamw_set_moments(bl_adamw_plan_t plan, void* state, const float* m, const float* v, void* stream);
 

@@ -234,7 +234,8 @@ class LogProbPlan(_Plan):
 
 class AdamWTensors:
     """The parameters and gradients that an AdamW step goes over: the tensors,
-    which it keeps alive, and the list of their addresses."""
+    which it keeps alive, and the list of their addresses, taken once (a tensor
+    that is given other storage has to be bound again)."""
 
     def __init__(self, plan, params, grads):
         if len(params) != len(plan.sizes) or len(grads) != len(plan.sizes):
@@ -313,7 +314,8 @@ class AdamWPlan(_Plan):
         return m, v
 
     def load_moments(self, state, m, v, stream=None):
-        """Sets the moments from values (converted to float32) in the layout of moments()."""
+        """Sets the moments from values (converted to float32) in the layout of
+        moments(), 0 between the tensors."""
         with torch.cuda.stream(stream):
             m, v = m.float(), v.float()
         _check("bl_adamw_set_moments", self._lib.bl_adamw_set_moments(

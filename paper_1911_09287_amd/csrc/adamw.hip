@@ -210,6 +210,7 @@ __global__ __launch_bounds__(kT) void k_adamw(const TensorList<N> list, StepArgs
       const float gj = to_f32(g[k].v[j]) * gs;
       m[j] = decayed(m[j], a.b1, gj, a.r1);
       v[j] = decayed(v[j], a.b2, gj * gj, a.r2);
+      if (BITS == 8 && j >= n - 256 * k) m[j] = v[j] = 0.f;  // past the tensor: no part of its block
       const float down = fmaf(__builtin_amdgcn_sqrtf(v[j]), a.root, a.eps);
       const float x = fmaf(to_f32(p[k].v[j]), keep, -(m[j] * a.rate) * __builtin_amdgcn_rcpf(down));
       p[k].v[j] = round_param<P>(x, h[j]);
@@ -371,7 +372,7 @@ extern "C" bl_status_t bl_adamw_plan_create(bl_adamw_plan_t* out, const bl_adamw
   long long chunks = 0;
   for (int i = 0; i < d->count; ++i) {
     if (d->sizes[i] < 0) return BL_ERR_INVALID_ARG;
-    if (d->sizes[i] >= 1LL << 36) return BL_ERR_UNSUPPORTED;
+    if (d->sizes[i] >= 1LL << 35) return BL_ERR_UNSUPPORTED;
     chunks += (d->sizes[i] + kChunk - 1) / kChunk;
     if (chunks >= 1LL << 31) return BL_ERR_UNSUPPORTED;
   }
@@ -435,7 +436,7 @@ extern "C" bl_status_t bl_adamw_step(bl_adamw_plan_t p, void* const* params, con
     return BL_ERR_INVALID_ARG;
   if (!r.live && (r.step < 1 || !(r.lr >= 0.0) || !std::isfinite(r.lr))) return BL_ERR_INVALID_ARG;
   if (!p->first.back()) return BL_OK;
-  if (!params || !grads || !state) return BL_ERR_INVALID_ARG;
+  if (!params || !grads || !state || !aligned(state)) return BL_ERR_INVALID_ARG;
   for (size_t i = 0; i < p->sizes.size(); ++i)
     if (p->sizes[i] && (!params[i] || !grads[i])) return BL_ERR_INVALID_ARG;
   StepArgs a = state_of(p, state);
@@ -476,7 +477,7 @@ bl_status_t over_layout(const bl_adamw_plan_s* p, const char* name, double wide,
 extern "C" bl_status_t bl_adamw_get_moments(bl_adamw_plan_t p, const void* state, void* m, void* v, void* stream) {
   if (!p) return BL_ERR_INVALID_ARG;
   if (!p->first.back()) return BL_OK;
-  if (!state || !m || !v) return BL_ERR_INVALID_ARG;
+  if (!state || !m || !v || !aligned(state)) return BL_ERR_INVALID_ARG;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const StepArgs a = state_of(p, state);
   if (p->bits == 8)
@@ -494,7 +495,7 @@ extern "C" bl_status_t bl_adamw_set_moments(bl_adamw_plan_t p, void* state, cons
                                             void* stream) {
   if (!p) return BL_ERR_INVALID_ARG;
   if (!p->first.back()) return BL_OK;
-  if (!state || !m || !v) return BL_ERR_INVALID_ARG;
+  if (!state || !m || !v || !aligned(state)) return BL_ERR_INVALID_ARG;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const StepArgs a = state_of(p, state);
   return over_layout(p, "adamw_set", p->bits == 8 ? 10.0 : 16.0, kChunk, s,

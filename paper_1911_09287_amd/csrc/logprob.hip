@@ -586,7 +586,7 @@ extern "C" bl_status_t bl_logprob_forward(bl_logprob_plan_t p, const void* logit
                                           void* stream) {
   if (!p) return BL_ERR_INVALID_ARG;
   if (!p->d.rows) return BL_OK;
-  if (!logits || (p->d.top && (!top_logp || !top_index)) || (p->bytes && !ws)) return BL_ERR_INVALID_ARG;
+  if (!logits || (p->d.top && (!top_logp || !top_index)) || (p->bytes && (!ws || !aligned(ws)))) return BL_ERR_INVALID_ARG;
   const Ptrs a{logits, targets, logp, stats, top_logp, top_index, static_cast<u64*>(ws),
                reinterpret_cast<float*>(static_cast<char*>(ws) + p->off_sums)};
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -108,7 +108,7 @@ extern "C" bl_status_t bl_norm_workspace_size(bl_norm_plan_t p, size_t* bytes) {
 
 extern "C" bl_status_t bl_norm_forward(bl_norm_plan_t p, const void* x, const void* w, const void* b, void* y,
                                        float* stats, void* ws, void* stream) {
-  if (!p || (p->d.outer && (!x || !y || (p->bytes && !ws)))) return BL_ERR_INVALID_ARG;
+  if (!p || (p->d.outer && (!x || !y || (p->bytes && (!ws || !aligned(ws)))))) return BL_ERR_INVALID_ARG;
   if (!p->d.outer) return BL_OK;
   NormPtrs a{};
   a.x = x;
@@ -123,7 +123,7 @@ extern "C" bl_status_t bl_norm_forward(bl_norm_plan_t p, const void* x, const vo
 
 extern "C" bl_status_t bl_norm_backward(bl_norm_plan_t p, const void* dy, const void* x, const void* w,
                                         const float* stats, void* dx, void* dw, void* db, void* ws, void* stream) {
-  if (!p || (p->d.outer && (!dy || !x || !stats || !dx || (p->bytes && !ws)))) return BL_ERR_INVALID_ARG;
+  if (!p || (p->d.outer && (!dy || !x || !stats || !dx || (p->bytes && (!ws || !aligned(ws)))))) return BL_ERR_INVALID_ARG;
   NormPtrs a{};
   a.x = x;
   a.dy = dy;

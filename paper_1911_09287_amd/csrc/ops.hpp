@@ -2,6 +2,7 @@
 // adamw.hip): element types, vector loads of any alignment, wave reductions.
 #pragma once
 
+#include <cstdint>
 #include <type_traits>
 
 #include "bltrain.h"
@@ -144,6 +145,8 @@ __device__ __forceinline__ float wave_sum(float x, int lanes = kWave) {
 
 inline bool known_dtype(int d) { return d == BL_F32 || d == BL_BF16 || d == BL_F16; }
 inline int dtype_bytes(int d) { return d == BL_F32 ? 4 : 2; }
+// Whether a workspace or state starts where its widest accesses may.
+inline bool aligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 inline size_t round_up(size_t n, size_t a) { return (n + a - 1) / a * a; }
 
 }  // namespace blc

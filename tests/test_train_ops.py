@@ -101,6 +101,22 @@ def test_calls_refuse_null_arguments():
         assert lib.bl_adamw_step(adam._h, ptrs, ptrs, some, ctypes.byref(bad), None) == INVALID, name
 
 
+def test_calls_refuse_misaligned_workspaces_and_states():
+    lib = bltrain.load()
+    some, odd = ctypes.c_void_p(16), ctypes.c_void_p(24)
+    norm, prob, adam = bltrain.NormPlan(2, 100000), bltrain.LogProbPlan(2, 100000, top=1), bltrain.AdamWPlan([4])
+    assert norm.workspace_bytes and prob.workspace_bytes
+    for ws in (None, odd):
+        assert lib.bl_norm_forward(norm._h, some, None, None, some, None, ws, None) == INVALID
+        assert lib.bl_norm_backward(norm._h, some, some, None, some, some, None, None, ws, None) == INVALID
+        assert lib.bl_logprob_forward(prob._h, some, None, some, some, some, some, ws, None) == INVALID
+    args = bltrain.AdamWArgs(1e-3, 0.9, 0.999, 1e-8, 0.0, 1, 0, None, None)
+    ptrs = (ctypes.c_void_p * 1)(16)
+    assert lib.bl_adamw_step(adam._h, ptrs, ptrs, odd, ctypes.byref(args), None) == INVALID
+    assert lib.bl_adamw_get_moments(adam._h, odd, some, some, None) == INVALID
+    assert lib.bl_adamw_set_moments(adam._h, odd, some, some, None) == INVALID
+
+
 def test_binding_refuses_tensors_off_the_gpu_and_wrong_lists():
     plan = bltrain.NormPlan(2, 4)
     x = torch.zeros(2, 4)

@@ -273,6 +273,13 @@ def test_norm_refuses_wrong_tensors(torch):
         wide.forward(x, None, None, x, stats, wide.workspace())
 
 
+def test_norm_offsets_past_32_bits(torch):
+    # two slices more than 2^32 bytes apart: rows, long rows, channels
+    for shape, gap in [((2, 700, 1), 1 << 30), ((2, 40000, 1), 1 << 30), ((2, 24, 10), 1 << 30)]:
+        check_norm(torch, shape, "f32", "f32", x_gap=gap, seed=9)
+    check_norm(torch, (2, 24, 10), "bf16", "f32", y_gap=(1 << 31) + 6, seed=9)
+
+
 # ---- log probabilities ------------------------------------------------------------
 def logprob_reference(torch, z, targets, top, g=None, ge=None):
     z = z.double()
@@ -404,6 +411,12 @@ def test_logprob_not_finite(torch, classes):
     t = torch.tensor([1, 0, 1, 2])
     check_logprob(torch, z, t, 3, "f32")
     check_logprob(torch, z, t, 3, "bf16")
+
+
+def test_logprob_offsets_past_32_bits(torch):
+    for classes, top in [(300, 3), (20000, 3)]:
+        z = torch.randn(3, classes)
+        check_logprob(torch, z, torch.tensor([1, 2, 3]), top, "f32", gap=1 << 30)
 
 
 def test_logprob_optional_outputs_and_in_place(torch):
@@ -652,6 +665,42 @@ def test_adamw_bfloat16_parameters_move_on_average(torch):
         plan.step(tensors, state, lr=lr, eps=0.0, weight_decay=0.0, step=t, seed=1)
     moved = 1.5 - p.double().mean().item()
     assert abs(moved / (lr * steps) - 1) < 0.05
+
+
+def test_adamw_offsets_past_32_bits(torch):
+    n = (1 << 31) + 2500  # elements of one tensor: 2^33 bytes of parameters
+    for bits in (32, 8):
+        plan = bltrain.AdamWPlan([7, n], bits=bits, grad_dtype=torch.bfloat16)
+        p = [torch.ones(7, device="cuda"), torch.ones(n, device="cuda")]
+        g = [torch.ones(7, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")]
+        g[1][-3:] = 1.0
+        g[1][:2] = 1.0
+        tensors, state = plan.bind(p, g), plan.state()
+        plan.step(tensors, state, lr=0.25, weight_decay=0.0, step=1)
+        # the first step moves by lr where there is a gradient
+        assert (p[0] - 0.75).abs().max().item() < 1e-6
+        moved = p[1] != 1.0
+        assert moved.sum().item() == 5 and moved[:2].all() and moved[-3:].all()
+        m = plan.moments(state)[0]
+        assert m[plan.starts[1] + n - 1].item() > 0.09 and m[plan.starts[1] + n - 4].item() == 0
+        del p, g, tensors, state, m, moved
+        torch.cuda.empty_cache()
+
+
+def test_adamw_what_lies_between_tensors_has_no_part(torch):
+    # a block's power of two goes by the tensor's own values, whatever the state holds past its end
+    plan = bltrain.AdamWPlan([100], bits=8)
+    g = torch.full((100,), 1e-3, device="cuda")
+    state = plan.state()
+    full = torch.zeros(plan.total, device="cuda")
+    full[110] = 1e9
+    plan.load_moments(state, full, full)
+    p = torch.zeros(100, device="cuda")
+    tensors = plan.bind([p], [g])
+    plan.step(tensors, state, step=1)
+    m, v = plan.moments(state)
+    assert (m[100:] == 0).all() and (v[100:] == 0).all()
+    near(m[:100], torch.full((100,), 1e-4), 1e-4 / 8)
 
 
 def test_adamw_refuses_wrong_tensors(torch):
