@@ -234,7 +234,7 @@ __device__ __forceinline__ void add_terms(Held<T, V> (&v)[E], Sums& s, Exponent&
 // Pieces of rows (WAVES = 1: whole rows), E vectors a lane.  With `pieces` > 1 each
 // leaves its sums and keys, else it gives the row's results.
 template <typename T, int E, int WAVES, bool TOP>
-__global__ __launch_bounds__(kT) void k_logprob_fwd(Ptrs a, bl_logprob_desc_t d, int pieces, long piece) {
+__global__ __launch_bounds__(kT, TOP ? 6 : 8) void k_logprob_fwd(Ptrs a, bl_logprob_desc_t d, int pieces, long piece) {
   constexpr int V = 16 / sizeof(T), kParts = kWaves / WAVES;  // pieces of a block at a time
   __shared__ u64 room[kParts][TOP ? kRoom : 1];
   __shared__ unsigned largest[TOP ? WAVES * kWave : 1];

@@ -36,7 +36,7 @@ __device__ __forceinline__ unsigned offset_of(const Place& p, long first, long s
 }
 template <typename T, int N>
 __device__ __forceinline__ void store_at(T* p, unsigned bytes, bool there, const Pack<T, N>& v) {
-  if (there) store_pack<T, N>(reinterpret_cast<T*>(reinterpret_cast<char*>(p) + (size_t)bytes), v);
+  if (there) store_pack<T, N>(at_bytes(p, bytes), v);
 }
 
 // Weights into LDS, w[0 ... size), `one` without them; the caller synchronises.

@@ -56,6 +56,13 @@ __device__ __forceinline__ void store_part(T* p, long n, const Pack<T, N>& r) {
     if (j < n) p[j] = r.v[j];
 }
 
+// p, which a whole wave shares, and a lane's bytes from there: one address register.
+template <typename T>
+__device__ __forceinline__ T* at_bytes(T* p, unsigned bytes) {
+  return reinterpret_cast<T*>(reinterpret_cast<std::conditional_t<std::is_const_v<T>, const char, char>*>(p) +
+                              (size_t)bytes);
+}
+
 // N elements as they were loaded, in 32-bit words, for kernels that hold many.
 // refresh() after the loads keeps conversions (and the wait for a load) out of
 // the branch that loads, so that all loads of a lane are in flight together;
@@ -82,12 +89,11 @@ struct Held {
         }
     }
   }
-  // All of them at `bytes` from a pointer that the whole wave shares (one address
-  // register), or zeros.
+  // All of them at `bytes` from p, or zeros.
   __device__ __forceinline__ void load_at(const T* p, unsigned bytes, bool there) {
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = 0;
-    if (there) __builtin_memcpy(w, reinterpret_cast<const char*>(p) + (size_t)bytes, N * sizeof(T));
+    if (there) __builtin_memcpy(w, at_bytes(p, bytes), N * sizeof(T));
   }
   __device__ __forceinline__ float operator[](int j) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
