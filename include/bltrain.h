@@ -183,7 +183,7 @@ typedef struct {
 
 typedef struct bl_adamw_plan_s* bl_adamw_plan_t;
 
-/* BL_ERR_UNSUPPORTED: a tensor of 2^35 elements or more, or 2^31 or more blocks of 1024. */
+/* BL_ERR_UNSUPPORTED: a tensor of 2^34 elements or more, or 2^31 or more blocks of 1024. */
 bl_status_t bl_adamw_plan_create(bl_adamw_plan_t* out, const bl_adamw_desc_t* desc);
 bl_status_t bl_adamw_plan_destroy(bl_adamw_plan_t plan);
 /* Bytes of the state, elements of each moment's array, and start[count] (any may be NULL). */
@@ -201,7 +201,7 @@ bl_status_t bl_adamw_step(bl_adamw_plan_t plan, void* const* params, const void*
  * bits = 8 (which holds every 8-bit value exactly); and from fp32 values, rounded
  * to nearest with bits = 8 (half away from zero; S is the largest power of two
  * below the block's largest magnitude, so that values which bl_adamw_get_moments
- * gave are held again exactly).  Elements between the tensors must be 0 in what is
+ * gave are held again exactly; a negative v is held as NaN).  Elements between the tensors must be 0 in what is
  * set, as they are in what is given. */
 bl_status_t bl_adamw_get_moments(bl_adamw_plan_t plan, const void* state, void* m, void* v, void* stream);
 bl_status_t bl_adamw_set_moments(bl_adamw_plan_t plan, void* state, const float* m, const float* v, void* stream);
