@@ -69,6 +69,19 @@ __device__ __forceinline__ void load_weights(const void* w, bool wide, long from
   }
 }
 
+// Backward, every operation rounded by itself: u and its mean then cancel where they
+// are equal (of one value, or of equal u), and the gradient there is 0 and not what a
+// fused multiply-add would leave of u's rounding, times 1 / sqrt(eps).
+__device__ __forceinline__ void add_sums(float u, float h, float& s0, float& s1) {
+#pragma clang fp contract(off)
+  s0 += u;
+  s1 += u * h;
+}
+__device__ __forceinline__ float grad_of(float u, float c1, float h, float c2, float rstd) {
+#pragma clang fp contract(off)
+  return rstd * ((u - c1) - h * c2);
+}
+
 bl_status_t norm_rows_forward(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s);
 bl_status_t norm_rows_backward(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s);
 bl_status_t norm_maps_forward(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s);

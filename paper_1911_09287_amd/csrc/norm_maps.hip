@@ -178,8 +178,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_maps_bwd(NormPtrs a, bl_norm_des
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {  // (where there is no value dy is 0)
         const float h = (v[k][j] - mean[j]) * rstd[j], dyj = g[k][j], u = dyj * wc;
-        s[2 * j] += u;
-        s[2 * j + 1] = fmaf(u, h, s[2 * j + 1]);
+        add_sums(u, h, s[2 * j], s[2 * j + 1]);
         aw[k] = fmaf(dyj, h, aw[k]);
         ab[k] += dyj;
       }
@@ -190,6 +189,8 @@ __global__ __launch_bounds__(THREADS, 4) void k_maps_bwd(NormPtrs a, bl_norm_des
     channel_sum<2 * VEC, LANES, THREADS>(s, red[turn]);
     turn ^= 1;
 #pragma unroll
+    for (int j = 0; j < 2 * VEC; ++j) s[j] *= inv;
+#pragma unroll
     for (int k = 0; k < EACH; ++k) {
       const int c = group + k * groups;
       if (c >= size) break;
@@ -198,7 +199,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_maps_bwd(NormPtrs a, bl_norm_des
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const float h = (v[k][j] - mean[j]) * rstd[j];
-        o.v[j] = (T)(rstd[j] * (fmaf(g[k][j], wc, -s[2 * j] * inv) - h * (s[2 * j + 1] * inv)));
+        o.v[j] = (T)grad_of(g[k][j] * wc, s[2 * j], h, s[2 * j + 1], rstd[j]);
       }
       store_at<T, VEC>(dx + k * step, at_x, p.there, o);
       __builtin_amdgcn_sched_barrier(0);
@@ -284,8 +285,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_maps_bwd_stream(NormPtrs a, 
         float w[1][1];
         load_weights<T, 1, 1>(a.w, wide, c, 0, d.size, 1.f, w);
         const float u = to_f32(dy[c * d.inner]) * w[0][0];
-        s[0] += u;
-        s[1] = fmaf(u, (to_f32(x[c * d.inner]) - mean) * rstd, s[1]);
+        add_sums(u, (to_f32(x[c * d.inner]) - mean) * rstd, s[0], s[1]);
       }
     stream_sum(s, red[turn]);
     turn ^= 1;
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_maps_bwd_stream(NormPtrs a, 
       if (p.there) {
         h = (to_f32(x[c * d.inner]) - mean) * rstd;
         g = to_f32(dy[c * d.inner]);
-        dx[c * d.inner] = (T)(rstd * (fmaf(g, w[0][0], -c1) - h * c2));
+        dx[c * d.inner] = (T)grad_of(g * w[0][0], c1, h, c2, rstd);
       }
       if (!sums) continue;
       const float dw = wave_sum(g * h), db = wave_sum(g);

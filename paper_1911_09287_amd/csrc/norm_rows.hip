@@ -159,8 +159,7 @@ __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_bwd(NormPtrs
 #pragma unroll
       for (int j = 0; j < V; ++j) {  // (past the row dy is 0)
         const float h = (v[k][j] - mean) * rstd, dyj = g[k][j], u = dyj * w[k][j];
-        s[0] += u;
-        s[1] = fmaf(u, h, s[1]);
+        add_sums(u, h, s[0], s[1]);
         aw[k][j] = fmaf(dyj, h, aw[k][j]);
         ab[k][j] += dyj;
       }
@@ -177,7 +176,7 @@ __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_bwd(NormPtrs
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float h = (v[k][j] - mean) * rstd;
-        o.v[j] = (T)(rstd * (fmaf(g[k][j], w[k][j], -c1) - h * c2));
+        o.v[j] = (T)grad_of(g[k][j] * w[k][j], c1, h, c2, rstd);
       }
       store_part<T, V>(place<BLOCK>(dx, i), M - i, o);
     }
@@ -381,8 +380,7 @@ __global__ __launch_bounds__(kT) void k_split_sums(NormPtrs a, bl_norm_desc_t d,
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float h = (v[k][j] - mean) * rstd, u = g[k][j] * w[k][j];
-        s0 += u;
-        s1 = fmaf(u, h, s1);
+        add_sums(u, h, s0, s1);
       }
     }
   }
@@ -443,7 +441,7 @@ __global__ __launch_bounds__(kT) void k_split_bwd(NormPtrs a, bl_norm_desc_t d, 
             const float h = (v[k][j] - t.x) * t.y, dyj = g[k][j];
             aw[j] = fmaf(dyj, h, aw[j]);
             ab[j] += dyj;
-            o.v[j] = (T)(t.y * (fmaf(dyj, w[0][j], -t.z) - h * t.w));
+            o.v[j] = (T)grad_of(dyj * w[0][j], t.z, h, t.w, t.y);
           }
           store_part<T, V>(static_cast<T*>(a.dx) + row * d.x_stride + i, to - i, o);
         }

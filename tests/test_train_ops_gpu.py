@@ -203,6 +203,29 @@ def test_norm_not_finite_stays_in_its_row(torch):
     assert (y.isnan() == bad).all()
 
 
+@pytest.mark.parametrize("shape", [(5, 1, 1), (300, 1, 1), (2, 1, 163), (3, 1, 8)], ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norm_of_one_value_has_no_gradient(torch, shape, dtype):
+    # y = bias whatever x is; 1 / deviation is 1 / sqrt(eps) = 316 times any rounding left over
+    x, dy, w, b = norm_inputs(torch, shape, dtype, "f32", 1)
+    got = run_norm(torch, shape, x, dy, w, b, dtype, "f32", 1e-5)
+    assert (got["dx"] == 0).all() and (got["dw"] == 0).all()
+
+
+def test_norm_either_weight_gradient_alone(torch):
+    for shape in [(40, 300, 1), (2, 70000, 1), (3, 40, 50)]:
+        x, dy, w, b = (t.cuda() for t in norm_inputs(torch, shape, "f32", "f32", 2))
+        plan = bltrain.NormPlan(*shape)
+        ws, stats, y = plan.workspace(), torch.empty(plan.stats_shape(), device="cuda"), torch.empty_like(x)
+        plan.forward(x, w, b, y, stats, ws)
+        both = [torch.empty_like(w) for _ in range(2)]
+        plan.backward(dy, x, w, stats, torch.empty_like(x), *both, ws)
+        dw, db, dx = torch.empty_like(w), torch.empty_like(w), torch.empty_like(x)
+        plan.backward(dy, x, w, stats, dx, dw, None, ws)
+        plan.backward(dy, x, w, stats, dx, None, db, ws)
+        assert torch.equal(dw, both[0]) and torch.equal(db, both[1])
+
+
 def test_norm_of_no_rows(torch):
     plan = bltrain.NormPlan(0, 40)
     none = torch.empty(0, 40, device="cuda")
