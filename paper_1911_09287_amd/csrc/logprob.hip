@@ -2,20 +2,26 @@
 // logits, and the gradient of the logits.
 //
 // Forward: a row of up to 2048 classes lies in the registers of a wave, a longer one
-// is cut in pieces of up to 8192, each in the registers of a block; the logits are
-// read once.  A lane takes its own largest logit m and sums a = sum e^(z - m) and
-// b = sum e^(z - m) (z - m); two such triples over sets of classes join to one
-// (m' = max, a' = a e^(m - m'), b' = e^(m - m') (b + (m - m') a), added), over lanes,
-// waves and pieces, in an order that sizes alone decide.  log q_t = z_t - m - log a and
-// the entropy log a - b / a come from the row's.  Bound by HBM, in 16 bits nearly by
-// the exponentials.
+// is cut in pieces of up to 8 vectors a lane (8192 fp32, 16384 16-bit logits), each in
+// the registers of a block; the logits are read once.  A lane takes its own largest
+// logit m and sums a = sum e^(z - m) and b = sum e^(z - m) (z - m); two such triples
+// over sets of classes join to one (m' = max, a' = a e^(m - m'), b' = e^(m - m') (b +
+// (m - m') a), added), over lanes, waves and pieces, in an order that sizes alone
+// decide.  log q_t = z_t - m - log a and the entropy log a - b / a come from the row's.
+// Bound by HBM, in 16 bits nearly by the vector instructions (11 a logit).
 //
 // The `top` likeliest: a value and its class make one key of 64 bits whose order is
 // the wanted one.  The top-th of the largest values on each lane bounds the answer
-// from below, so that few values are left; these go to LDS and one wave sorts them, 64 keys on its lanes, by a
-// bitonic network.  Where more are left than there is room for (many equal values), or
-// the row holds NaN, the waves take 64 keys after another and join them to a sorted list.  Pieces leave their `top` keys
-// for a second launch that joins them.
+// from below, so that few values are left; these go to LDS and one wave sorts them, 64
+// keys on its lanes, by a bitonic network.  Where more are left than there is room for
+// (many equal values), or the row holds NaN, the waves take 64 keys after another and
+// join them to a sorted list.  Pieces leave their `top` keys for a second launch that
+// joins them.
+//
+// Measured: 4096 rows of 32000 logits without likeliest classes fp32 88 us, 6.0 TB/s,
+// bfloat16 51 us, 5.1 TB/s, with 8 of them 70 us; 513 rows of 50021 fp32 logits with
+// 20 of them 25.5 us, 4.0 TB/s, and 5.6 us for the join; one row of 131071 bfloat16
+// logits with 8 of them 5.4 + 5.5 us, hardly more than two launches take anyhow.
 #include <algorithm>
 #include <new>
 
