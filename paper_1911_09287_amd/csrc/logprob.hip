@@ -11,9 +11,12 @@
 // Bound by HBM, in 16 bits nearly by the vector instructions (11 a logit).
 //
 // The `top` likeliest: a value and its class make one key of 64 bits whose order is
-// the wanted one.  The top-th of the largest values on each lane bounds the answer
-// from below, so that few values are left; these go to LDS and one wave sorts them, 64
-// keys on its lanes, by a bitonic network.  Where more are left than there is room for
+// the wanted one.  Of the largest values on each lane, every wave of a block takes the
+// ceil(top / waves)-th; at least `top` values are no less than the least of these, so
+// that it bounds the answer from below and few values are left.  (The top-th over all
+// of a block's lanes is nearer by 1 to 3 % of the time at 20 and costs twice the time
+// at 64, where most lanes hold one.)  What is left goes to LDS and one wave sorts it,
+// 64 keys on its lanes, by a bitonic network.  Where more are left than there is room for
 // (many equal values), or the row holds NaN, the waves take 64 keys after another and
 // join them to a sorted list.  Pieces leave their `top` keys for a second launch that
 // joins them.
@@ -42,12 +45,6 @@ namespace {
 constexpr int kT = 256;
 constexpr int kWaves = kT / kWave;
 constexpr int kRoom = 512;  // keys that are left after the bound, for which LDS has room
-// `top` up to which a block's bound is the top-th of the largest values on each lane
-// over the waves; beyond, each wave's ceil(top / 4)-th of its lanes', and the least of
-// the waves.  The first is nearer where few are wanted (4096 rows of 32000 bfloat16
-// logits, top 8: 92 us against 99), the second where most lanes hold one (32000 fp32,
-// top 64: 286 against 170).
-constexpr int kFewTop = 24;
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 using u64 = unsigned long long;
 
@@ -243,7 +240,7 @@ template <typename T, int E, int WAVES, bool TOP>
 __global__ __launch_bounds__(kT, TOP ? 6 : 8) void k_logprob_fwd(Ptrs a, bl_logprob_desc_t d, int pieces, long piece) {
   constexpr int V = 16 / sizeof(T), kParts = kWaves / WAVES;  // pieces of a block at a time
   __shared__ u64 room[kParts][TOP ? kRoom : 1];
-  __shared__ unsigned largest[TOP ? WAVES * kWave : 1];
+  __shared__ unsigned bounds[WAVES];
   __shared__ int left[kParts];
   __shared__ Sums wave_sums[WAVES];
   const int part = WAVES == 1 ? threadIdx.x / kWave : 0, in = WAVES == 1 ? threadIdx.x % kWave : threadIdx.x;
@@ -272,11 +269,9 @@ __global__ __launch_bounds__(kT, TOP ? 6 : 8) void k_logprob_fwd(Ptrs a, bl_logp
       s.m = fmaxf(s.m, most[k]);
     }
     unsigned bound = 0;
-    const bool by_lanes = WAVES == 1 || d.top <= kFewTop;
     if (TOP) {
-      bound = order_of(s.m);
-      if (!by_lanes) bound = (unsigned)__builtin_amdgcn_readlane((int)sort64(bound), (d.top + WAVES - 1) / WAVES - 1);
-      if (WAVES > 1) largest[in] = bound;
+      bound = (unsigned)__builtin_amdgcn_readlane((int)sort64(order_of(s.m)), (d.top + WAVES - 1) / WAVES - 1);
+      if (WAVES > 1 && lane == 0) bounds[wave] = bound;
       if (in == 0) left[part] = 0;
     }
     const float base = s.m == -INFINITY ? 0.f : s.m;
@@ -303,11 +298,7 @@ __global__ __launch_bounds__(kT, TOP ? 6 : 8) void k_logprob_fwd(Ptrs a, bl_logp
     u64 list = 0, last = 0;
     if (TOP) {
 #pragma unroll
-      for (int w = 0; w < (WAVES > 1 ? WAVES : 0); ++w) {
-        const unsigned o = largest[lane + w * kWave];
-        bound = w == 0 ? o : by_lanes ? max(bound, o) : min(bound, o);
-      }
-      if (by_lanes) bound = (unsigned)__builtin_amdgcn_readlane((int)sort64(bound), d.top - 1);
+      for (int w = 0; w < (WAVES > 1 ? WAVES : 0); ++w) bound = min(bound, bounds[w]);
       const float least = value_of(bound);
       bool whole = s.a == s.a;  // no NaN
       if (whole) {
