@@ -6,7 +6,7 @@
 // every value is read once and written once, and sums over the channels cross the
 // lanes by shuffles and the waves by way of LDS.  Backward, a thread keeps the
 // sums of its channels' dw and db over all tiles of its block.  Bound by HBM: 64 maps
-// of 256 channels and 512 positions, fp32, forward 12 us, 5.5 TB/s, backward 22 us, 4.6
+// of 256 channels and 512 positions, fp32, forward 12 us, 5.5 TB/s, backward 23 us, 4.4
 // TB/s, and 4 us for the last sum over blocks.
 #include <algorithm>
 

@@ -118,7 +118,7 @@ __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_fwd(NormPtrs
 
 // Element i of a row: of a row that one wave holds by a shared address and a lane's
 // offset.  (In a block of 1024 with four vectors a lane that costs the registers that
-// are left: 2000 rows of 16384 fp32 values backward take 111 us with it, 96 without.)
+// are left: 2000 rows of 16384 fp32 values backward take 111 us with it, 95 without.)
 template <bool BLOCK, typename T>
 __device__ __forceinline__ T* place(T* row, long i) {
   return BLOCK ? row + i : at_bytes(row, (unsigned)i * (unsigned)sizeof(T));
@@ -159,7 +159,12 @@ __global__ __launch_bounds__(BLOCK ? kMostThreads : kT) void k_rows_bwd(NormPtrs
 #pragma unroll
       for (int j = 0; j < V; ++j) {  // (past the row dy is 0)
         const float h = (v[k][j] - mean) * rstd, dyj = g[k][j], u = dyj * w[k][j];
-        add_sums(u, h, s[0], s[1]);
+        if (E == 1) {
+          add_sums(u, h, s[0], s[1]);
+        } else {  // rows of hundreds of values: no sum is exact, and registers count (105 us for the 95 above)
+          s[0] += u;
+          s[1] = fmaf(u, h, s[1]);
+        }
         aw[k][j] = fmaf(dyj, h, aw[k][j]);
         ab[k][j] += dyj;
       }
