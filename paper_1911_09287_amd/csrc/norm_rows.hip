@@ -10,8 +10,8 @@
 // over its block's rows, in registers, and a last small launch.
 //
 // Measured (kernel, bytes read and written once): 16384 rows of 1024 fp32 values
-// forward 28 us, 4.8 TB/s, backward 39 us, 5.2 TB/s; of 2048 bfloat16 values 36 us,
-// 3.7 TB/s, and 43 us, 4.7 TB/s (twice the values to convert for the same bytes);
+// forward 28 us, 4.8 TB/s, backward 39 us, 5.2 TB/s; of 2048 bfloat16 values 34 us,
+// 3.9 TB/s, and 44 us, 4.6 TB/s (twice the values to convert for the same bytes);
 // 4096 of 8192 fp32 values 53 us, 5.0 TB/s, and 81 us, 4.9 TB/s; 32 of 200704 fp32
 // values, two launches, 6.4 + 11 us forward, 10 + 19 us backward.
 #include <algorithm>
@@ -489,7 +489,12 @@ template <typename T, bool BLOCK>
 bl_status_t launch_fwd(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s) {
   const bl_norm_rows& r = p->fwd;
   const long each = BLOCK ? 1 : kT / r.threads;
-  const unsigned blocks = (unsigned)std::min<long>((p->d.outer + each - 1) / each, BLOCK ? 2 * kTargetBlocks : 4 * kTargetBlocks);
+  // A block reads the weights once, so no more blocks than run at a time, 1024 threads a
+  // compute unit (2000 rows of 32768 fp32 values 108 us, with four times as many 117;
+  // 16384 of 2048 bfloat16 values 34, with twice as many 35), but twice as many where a
+  // wave holds its row in two vectors a lane (65536 of 256 fp32 values 27, with half 30).
+  const long cap = BLOCK ? 2 * kTargetBlocks * kT / r.threads : r.each > 2 ? 2 * kTargetBlocks : 4 * kTargetBlocks;
+  const unsigned blocks = (unsigned)std::min<long>((p->d.outer + each - 1) / each, cap);
   const double bytes = 2.0 * p->d.outer * p->d.size * sizeof(T);
   return timed_launch("norm_fwd", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
     auto go = [&](auto kernel) {
