@@ -46,6 +46,10 @@ constexpr int kT = 256;
 constexpr int kWaves = kT / kWave;
 constexpr int kRoom = 512;  // keys that are left after the bound, for which LDS has room
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
+// Lanes whose largest logit is no further from zero take the exponent by one fused
+// multiply-add: what the rounding of 1.5 * 2^20 leaves is 2^-4 at most.  Further out it
+// grows with the logit (128 at 4e9, where 2^r overflows): there z - base comes first.
+constexpr float kMostFused = 1048576.f;
 using u64 = unsigned long long;
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -275,14 +279,14 @@ __global__ __launch_bounds__(kT, TOP ? 6 : 8) void k_logprob_fwd(Ptrs a, bl_logp
       if (in == 0) left[part] = 0;
     }
     const float base = s.m == -INFINITY ? 0.f : s.m;
-    if (!__ballot(fabsf(base) > 1e38f)) {
+    if (!__ballot(fabsf(base) > kMostFused)) {
       // t = z log2 e + c with c rounded once: all terms are 2^r too large, r what the
       // rounding left, which is taken out of the sums
       const float c = -(base * kLog2e), left_over = fmaf(base, kLog2e, c), f = exp2_(-left_over);
       add_terms<T, V, E>(v, s, [&](float z) { return fmaf(z, kLog2e, c); });
       s.b = fmaf(-left_over, s.a, s.b) * f;
       s.a *= f;
-    } else {  // (there the product would overflow)
+    } else {
       add_terms<T, V, E>(v, s, [&](float z) { return (z - base) * kLog2e; });
     }
     if (!(s.a < INFINITY)) s.a = NAN;  // (infinite only beside an infinite logit)
