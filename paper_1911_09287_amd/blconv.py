@@ -214,8 +214,8 @@ class Plan:
         return s.cuda_stream
 
     def _ws(self, ws):
-        if ws is None or ws.numel() < self.workspace_bytes or not ws.is_cuda:
-            raise ValueError("workspace must be a GPU tensor of at least workspace_bytes bytes")
+        if ws is None or ws.numel() < self.workspace_bytes or not (ws.is_cuda and ws.is_contiguous()):
+            raise ValueError("workspace must be a contiguous GPU tensor of at least workspace_bytes bytes")
         return ws.data_ptr()
 
     def forward(self, x, w, y, ws, flags=0, stream=None):

@@ -134,8 +134,8 @@ class _Plan:
     def _ws(self, ws):
         if self.workspace_bytes == 0:
             return None
-        if ws is None or not ws.is_cuda or ws.nbytes < self.workspace_bytes:
-            raise ValueError("workspace must be a GPU tensor of at least workspace_bytes bytes")
+        if ws is None or not (ws.is_cuda and ws.is_contiguous()) or ws.nbytes < self.workspace_bytes:
+            raise ValueError("workspace must be a contiguous GPU tensor of at least workspace_bytes bytes")
         return ws.data_ptr()
 
 
