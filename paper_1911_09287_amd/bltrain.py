@@ -2,8 +2,9 @@
 
 Layer norm, log probabilities and the AdamW step, as plans like ``blconv.Plan``:
 argument marshalling only, every compute step runs in the HIP kernels of
-libblconv.so on the current stream (or the one given).  Buffers are the
-caller's; ``workspace()`` and ``state()`` make those whose size a plan sets.
+libblconv.so on the GPU that holds the tensors, all of them on one, and on that
+GPU's current stream (or the one given).  Buffers are the caller's;
+``workspace()`` and ``state()`` make those whose size a plan sets.
 """
 from __future__ import annotations
 
@@ -87,28 +88,50 @@ def _dtype_code(dtype, name):
     return code
 
 
-def _stream(stream, t):
-    """The HIP stream: the given one, or the current one of the device of tensor t."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
+def _gpu(t, name):
+    """Number of the GPU that holds tensor t."""
+    device = t.get_device()
+    if device < 0:
+        raise ValueError(f"{name} must be a tensor on the GPU")
+    return device
 
 
-def _flat(t, dtype, numel, name):
+def _stream(stream, device):
+    """The HIP stream: the given one, or the current one of the GPU."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    if stream.device_index != device:
+        raise ValueError(f"the stream is not one of the tensors' GPU {device}")
+    return stream.cuda_stream
+
+
+def _run(call, function, device, *args):
+    """One call of the library, whose launches go to the current GPU."""
+    if torch._C._cuda_getDevice() == device:
+        code = function(*args)
+    else:
+        with torch.cuda.device(device):
+            code = function(*args)
+    _check(call, code)
+
+
+def _flat(t, dtype, numel, name, device):
     """Device pointer of a contiguous tensor of `numel` elements, whatever its shape."""
     if t is None:
         return None
-    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor on the GPU")
+    if t.get_device() != device or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on GPU {device}, as the others")
     if t.numel() != numel:
         raise ValueError(f"{name} has {t.numel()} elements, expected {numel}")
     return t.data_ptr()
 
 
-def _sliced(t, dtype, outer, length, stride, name):
+def _sliced(t, dtype, outer, length, stride, name, device):
     """Device pointer of `outer` contiguous slices of `length` elements whose
     starts are `stride` apart: a contiguous tensor where stride = length, else
     one whose first axis has that stride."""
-    if not (t.is_cuda and t.dtype == dtype):
-        raise ValueError(f"{name} must be a {dtype} tensor on the GPU")
+    if t.get_device() != device or t.dtype != dtype:
+        raise ValueError(f"{name} must be a {dtype} tensor on GPU {device}, as the others")
     if t.numel() != outer * length:
         raise ValueError(f"{name} has {t.numel()} elements, expected {outer * length}")
     if stride == length or outer <= 1:
@@ -131,11 +154,11 @@ class _Plan:
     def workspace(self, device="cuda"):
         return torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
 
-    def _ws(self, ws):
+    def _ws(self, ws, device):
         if self.workspace_bytes == 0:
             return None
-        if ws is None or not (ws.is_cuda and ws.is_contiguous()) or ws.nbytes < self.workspace_bytes:
-            raise ValueError("workspace must be a contiguous GPU tensor of at least workspace_bytes bytes")
+        if ws is None or ws.get_device() != device or not ws.is_contiguous() or ws.nbytes < self.workspace_bytes:
+            raise ValueError("workspace must be a contiguous tensor of at least workspace_bytes bytes on the tensors' GPU")
         return ws.data_ptr()
 
 
@@ -168,29 +191,33 @@ class NormPlan(_Plan):
     def stats_shape(self):
         return (2, self.outer, self.inner)
 
-    def _x(self, t, name):
-        return _sliced(t, self.dtype, self.outer, self.size * self.inner, self.x_stride, name)
+    def _x(self, t, name, device):
+        return _sliced(t, self.dtype, self.outer, self.size * self.inner, self.x_stride, name, device)
 
-    def _y(self, t, name):
-        return _sliced(t, self.dtype, self.outer, self.size * self.inner, self.y_stride, name)
+    def _y(self, t, name, device):
+        return _sliced(t, self.dtype, self.outer, self.size * self.inner, self.y_stride, name, device)
 
-    def _stats(self, t):
-        return _flat(t, torch.float32, 2 * self.outer * self.inner, "stats")
+    def _w(self, t, name, device):
+        return _flat(t, self.wdtype, self.size, name, device)
+
+    def _stats(self, t, device):
+        return _flat(t, torch.float32, 2 * self.outer * self.inner, "stats", device)
 
     def forward(self, x, weight, bias, y, stats, ws, stream=None):
         """y, and mean and 1 / deviation in `stats` (None: not wanted); weight
         None: 1, bias None: 0."""
-        _check("bl_norm_forward", self._lib.bl_norm_forward(
-            self._h, self._x(x, "x"), _flat(weight, self.wdtype, self.size, "weight"),
-            _flat(bias, self.wdtype, self.size, "bias"), self._y(y, "y"), self._stats(stats), self._ws(ws),
-            _stream(stream, x)))
+        on = _gpu(x, "x")
+        _run("bl_norm_forward", self._lib.bl_norm_forward, on,
+             self._h, self._x(x, "x", on), self._w(weight, "weight", on), self._w(bias, "bias", on),
+             self._y(y, "y", on), self._stats(stats, on), self._ws(ws, on), _stream(stream, on))
 
     def backward(self, dy, x, weight, stats, dx, dweight, dbias, ws, stream=None):
         """dx, and the gradients of weight and bias (None: not wanted)."""
-        _check("bl_norm_backward", self._lib.bl_norm_backward(
-            self._h, self._y(dy, "dy"), self._x(x, "x"), _flat(weight, self.wdtype, self.size, "weight"),
-            self._stats(stats), self._x(dx, "dx"), _flat(dweight, self.wdtype, self.size, "dweight"),
-            _flat(dbias, self.wdtype, self.size, "dbias"), self._ws(ws), _stream(stream, x)))
+        on = _gpu(x, "x")
+        _run("bl_norm_backward", self._lib.bl_norm_backward, on,
+             self._h, self._y(dy, "dy", on), self._x(x, "x", on), self._w(weight, "weight", on),
+             self._stats(stats, on), self._x(dx, "dx", on), self._w(dweight, "dweight", on),
+             self._w(dbias, "dbias", on), self._ws(ws, on), _stream(stream, on))
 
 
 class LogProbPlan(_Plan):
@@ -214,22 +241,22 @@ class LogProbPlan(_Plan):
     def forward(self, logits, targets, logp, stats, top_logp, top_index, ws, stream=None):
         """logp [rows], stats [3][rows] (largest logit, log of the sum of
         exponentials over it, entropy), top_logp and top_index [rows][top]."""
-        _check("bl_logprob_forward", self._lib.bl_logprob_forward(
-            self._h, _sliced(logits, self.dtype, self.rows, self.classes, self.stride, "logits"),
-            _flat(targets, torch.int64, self.rows, "targets"), _flat(logp, torch.float32, self.rows, "logp"),
-            _flat(stats, torch.float32, 3 * self.rows, "stats"),
-            _flat(top_logp, torch.float32, self.rows * self.top, "top_logp"),
-            _flat(top_index, torch.int64, self.rows * self.top, "top_index"), self._ws(ws), _stream(stream, logits)))
+        on, n = _gpu(logits, "logits"), self.rows
+        _run("bl_logprob_forward", self._lib.bl_logprob_forward, on,
+             self._h, _sliced(logits, self.dtype, n, self.classes, self.stride, "logits", on),
+             _flat(targets, torch.int64, n, "targets", on), _flat(logp, torch.float32, n, "logp", on),
+             _flat(stats, torch.float32, 3 * n, "stats", on),
+             _flat(top_logp, torch.float32, n * self.top, "top_logp", on),
+             _flat(top_index, torch.int64, n * self.top, "top_index", on), self._ws(ws, on), _stream(stream, on))
 
     def backward(self, logits, targets, stats, g_logp, g_entropy, dlogits, stream=None):
         """The logits' gradient from those of logp and of the entropy (None: 0)."""
-        _check("bl_logprob_backward", self._lib.bl_logprob_backward(
-            self._h, _sliced(logits, self.dtype, self.rows, self.classes, self.stride, "logits"),
-            _flat(targets, torch.int64, self.rows, "targets"), _flat(stats, torch.float32, 3 * self.rows, "stats"),
-            _flat(g_logp, torch.float32, self.rows, "g_logp"),
-            _flat(g_entropy, torch.float32, self.rows, "g_entropy"),
-            _sliced(dlogits, self.dtype, self.rows, self.classes, self.grad_stride, "dlogits"),
-            _stream(stream, logits)))
+        on, n = _gpu(logits, "logits"), self.rows
+        _run("bl_logprob_backward", self._lib.bl_logprob_backward, on,
+             self._h, _sliced(logits, self.dtype, n, self.classes, self.stride, "logits", on),
+             _flat(targets, torch.int64, n, "targets", on), _flat(stats, torch.float32, 3 * n, "stats", on),
+             _flat(g_logp, torch.float32, n, "g_logp", on), _flat(g_entropy, torch.float32, n, "g_entropy", on),
+             _sliced(dlogits, self.dtype, n, self.classes, self.grad_stride, "dlogits", on), _stream(stream, on))
 
 
 class AdamWTensors:
@@ -241,10 +268,11 @@ class AdamWTensors:
         if len(params) != len(plan.sizes) or len(grads) != len(plan.sizes):
             raise ValueError(f"expected {len(plan.sizes)} parameters and gradients")
         self.plan, self.params, self.grads = plan, list(params), list(grads)
+        self.on = _gpu(self.params[0], "parameter 0") if self.params else None
         ptrs = _P * len(plan.sizes)
-        self._p = ptrs(*[_flat(t, plan.param_dtype, n, f"parameter {i}")
+        self._p = ptrs(*[_flat(t, plan.param_dtype, n, f"parameter {i}", self.on)
                          for i, (t, n) in enumerate(zip(params, plan.sizes))])
-        self._g = ptrs(*[_flat(t, plan.grad_dtype, n, f"gradient {i}")
+        self._g = ptrs(*[_flat(t, plan.grad_dtype, n, f"gradient {i}", self.on)
                          for i, (t, n) in enumerate(zip(grads, plan.sizes))])
 
 
@@ -278,7 +306,7 @@ class AdamWPlan(_Plan):
         return torch.zeros(self.state_bytes, dtype=torch.uint8, device=device)
 
     def _state(self, state):
-        if not (state.is_cuda and state.is_contiguous()) or state.nbytes != self.state_bytes:
+        if not state.is_contiguous() or state.nbytes != self.state_bytes:
             raise ValueError("state must be a contiguous GPU tensor of state_bytes bytes")
         return state.data_ptr()
 
@@ -293,10 +321,14 @@ class AdamWPlan(_Plan):
         that is read in the place of those two when the kernels run."""
         if tensors.plan is not self:
             raise ValueError("the tensors were bound to another plan")
+        on = _gpu(state, "state")
+        if tensors.on not in (None, on):
+            raise ValueError("the state and the tensors must be on one GPU")
         a = AdamWArgs(lr, betas[0], betas[1], eps, weight_decay, step, seed & 0xFFFFFFFF,
-                      _flat(grad_scale, torch.float32, 1, "grad_scale"), _flat(live, torch.float64, 2, "live"))
-        _check("bl_adamw_step", self._lib.bl_adamw_step(self._h, tensors._p, tensors._g, self._state(state),
-                                                        ctypes.byref(a), _stream(stream, state)))
+                      _flat(grad_scale, torch.float32, 1, "grad_scale", on),
+                      _flat(live, torch.float64, 2, "live", on))
+        _run("bl_adamw_step", self._lib.bl_adamw_step, on, self._h, tensors._p, tensors._g, self._state(state),
+             ctypes.byref(a), _stream(stream, on))
 
     def moments(self, state, m=None, v=None, stream=None):
         """(m, v), [total] each, tensor i's at starts[i]: of 32 bits as views of
@@ -304,20 +336,20 @@ class AdamWPlan(_Plan):
         if self.bits == 32 and m is None and v is None:
             both = state.view(torch.float32)
             return both[:self.total], both[self.total:]
-        dtype = torch.float32 if self.bits == 32 else torch.bfloat16
+        dtype, on = torch.float32 if self.bits == 32 else torch.bfloat16, _gpu(state, "state")
         with torch.cuda.stream(stream):  # (None: the current one) memory of the stream that writes it
             m = torch.empty(self.total, dtype=dtype, device=state.device) if m is None else m
             v = torch.empty(self.total, dtype=dtype, device=state.device) if v is None else v
-        _check("bl_adamw_get_moments", self._lib.bl_adamw_get_moments(
-            self._h, self._state(state), _flat(m, dtype, self.total, "m"), _flat(v, dtype, self.total, "v"),
-            _stream(stream, state)))
+        _run("bl_adamw_get_moments", self._lib.bl_adamw_get_moments, on, self._h, self._state(state),
+             _flat(m, dtype, self.total, "m", on), _flat(v, dtype, self.total, "v", on), _stream(stream, on))
         return m, v
 
     def load_moments(self, state, m, v, stream=None):
         """Sets the moments from values (converted to float32) in the layout of
         moments(), 0 between the tensors."""
+        on = _gpu(state, "state")
         with torch.cuda.stream(stream):
             m, v = m.float(), v.float()
-        _check("bl_adamw_set_moments", self._lib.bl_adamw_set_moments(
-            self._h, self._state(state), _flat(m, torch.float32, self.total, "m"),
-            _flat(v, torch.float32, self.total, "v"), _stream(stream, state)))
+        _run("bl_adamw_set_moments", self._lib.bl_adamw_set_moments, on, self._h, self._state(state),
+             _flat(m, torch.float32, self.total, "m", on), _flat(v, torch.float32, self.total, "v", on),
+             _stream(stream, on))
