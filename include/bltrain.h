@@ -183,7 +183,7 @@ typedef struct {
 
 typedef struct bl_adamw_plan_s* bl_adamw_plan_t;
 
-/* BL_ERR_UNSUPPORTED: a tensor of 2^34 elements or more, or 2^31 or more blocks of 1024. */
+/* BL_ERR_UNSUPPORTED: a tensor of more than 2^34 - 1024 elements, or 2^31 or more blocks of 1024. */
 bl_status_t bl_adamw_plan_create(bl_adamw_plan_t* out, const bl_adamw_desc_t* desc);
 bl_status_t bl_adamw_plan_destroy(bl_adamw_plan_t plan);
 /* Bytes of the state, elements of each moment's array, and start[count] (any may be NULL). */

@@ -399,7 +399,7 @@ extern "C" bl_status_t bl_adamw_plan_create(bl_adamw_plan_t* out, const bl_adamw
   long long chunks = 0;
   for (int i = 0; i < d->count; ++i) {
     if (d->sizes[i] < 0) return BL_ERR_INVALID_ARG;
-    if (d->sizes[i] >= 1LL << 34) return BL_ERR_UNSUPPORTED;
+    if (d->sizes[i] > kMostBlocks * kChunk) return BL_ERR_UNSUPPORTED;  // (a launch takes whole tensors)
     chunks += (d->sizes[i] + kChunk - 1) / kChunk;
     if (chunks >= 1LL << 31) return BL_ERR_UNSUPPORTED;
   }

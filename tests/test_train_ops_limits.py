@@ -145,3 +145,14 @@ def test_calls_refuse_a_stream_of_another_gpu(two_gpus):
         norm.forward(x, None, None, x, None, ws, stream=streams[0])
     norm.forward(x, None, None, x, None, ws, stream=streams[1])
     assert calls == [("bl_norm_forward", 1, 2001)]
+
+
+def test_adamw_tensors_as_large_as_a_launch():
+    # a block takes 1024 elements, and 2^24 blocks of 256 threads are more than a launch may have
+    most = (1 << 34) - 1024
+    assert bltrain.AdamWPlan([most]).starts == [0]
+    assert bltrain.AdamWPlan([most, 5, most]).starts == [0, most, most + 1024]
+    for sizes in ([most + 1], [(1 << 34) - 1], [5, most + 1], [(1 << 63) - 1]):
+        with pytest.raises(bltrain.BlError) as e:
+            bltrain.AdamWPlan(sizes)
+        assert e.value.code == 2  # BL_ERR_UNSUPPORTED
