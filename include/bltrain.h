@@ -65,8 +65,9 @@ typedef struct {
 
 typedef struct bl_norm_plan_s* bl_norm_plan_t;
 
-/* BL_ERR_UNSUPPORTED: size * inner >= 2^31, outer * inner >= 2^31, or rows (inner =
- * 1) of over 16384 elements in such a number that they are cut into 2^24 chunks. */
+/* BL_ERR_UNSUPPORTED: size * inner >= 2^31, size > 2^31 - 32, outer * inner >= 2^31, or
+ * rows (inner = 1) of over 16384 elements in such a number that they are cut into 2^24
+ * chunks. */
 bl_status_t bl_norm_plan_create(bl_norm_plan_t* out, const bl_norm_desc_t* desc);
 bl_status_t bl_norm_plan_destroy(bl_norm_plan_t plan);
 /* Workspace bytes of either call (0: ws may be NULL). */

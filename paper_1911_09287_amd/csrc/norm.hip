@@ -14,6 +14,7 @@ namespace {
 // parts leave slices without work: 10 parts of 200704 columns 14 us with 16 slices, 4
 // with one.)  512 parts of 2048 columns take 4 us.
 constexpr int kCols = 64;
+constexpr long long kMostColumns = 64LL * ((1LL << 26) - 1);  // a launch has fewer than 2^32 threads
 template <typename T, int SLICES>
 __global__ __launch_bounds__(kCols* SLICES) void k_norm_sum(const float* part, int parts, long size, void* dw,
                                                             void* db, bool wide) {
@@ -79,6 +80,7 @@ extern "C" bl_status_t bl_norm_plan_create(bl_norm_plan_t* out, const bl_norm_de
   if (d.x_stride < 0 || d.y_stride < 0) return BL_ERR_INVALID_ARG;
   const long long most = (1LL << 31) - 1;
   if (d.size > most || d.inner > most || d.size * d.inner > most) return BL_ERR_UNSUPPORTED;
+  if (2 * d.size > kMostColumns) return BL_ERR_UNSUPPORTED;  // (one thread a column of dw and db: few parts)
   if (d.outer > most || d.outer * d.inner > most) return BL_ERR_UNSUPPORTED;
   if (!d.x_stride) d.x_stride = d.size * d.inner;
   if (!d.y_stride) d.y_stride = d.size * d.inner;

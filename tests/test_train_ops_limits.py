@@ -156,3 +156,13 @@ def test_adamw_tensors_as_large_as_a_launch():
         with pytest.raises(bltrain.BlError) as e:
             bltrain.AdamWPlan(sizes)
         assert e.value.code == 2  # BL_ERR_UNSUPPORTED
+
+
+def test_norm_rows_whose_weight_gradients_fit_a_launch():
+    # the last sum has a thread for each of 2 size columns, 64 a block
+    assert bltrain.NormPlan(0, (1 << 31) - 32).workspace_bytes == 0
+    assert bltrain.NormPlan(1, (1 << 31) - 32).workspace_bytes > 0
+    for outer, size in ((0, (1 << 31) - 31), (1, (1 << 31) - 1)):
+        with pytest.raises(bltrain.BlError) as e:
+            bltrain.NormPlan(outer, size)
+        assert e.value.code == 2  # BL_ERR_UNSUPPORTED
