@@ -45,6 +45,7 @@ struct StepArgs {
   float b1, r1, b2, r2;    // beta, 1 - beta
   float eps, keep;         // keep: 1 - lr weight_decay
   float rate, root;        // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  int careful;             // eps so small that a subnormal v counts beside it
   unsigned key;            // of the dither
   unsigned seed;
   double beta1, beta2, wd;
@@ -55,10 +56,14 @@ struct StepArgs {
   float *ms, *vs;          // powers of two of their blocks
 };
 
-// What follows from lr and the step (on the device for a live step).
+// What follows from lr and the step (on the device for a live step), eps being set.  The
+// vector unit's square root and reciprocal take subnormal values for 0; sqrt(v) root of
+// such a v is 2^-63 root at most, and 2^-25 of an eps from 2^-38 root on (of 1e-8 for all
+// beta2 up to 1 - 2^-22).
 __host__ __device__ void step_scalars(StepArgs& a, double lr, double t) {
   a.rate = (float)(lr / (1.0 - pow(a.beta1, t)));
   a.root = (float)(1.0 / sqrt(1.0 - pow(a.beta2, t)));
+  a.careful = a.eps < a.root * 0x1p-38f;
   a.keep = (float)(1.0 - lr * a.wd);
   a.key = a.seed * 0x6A09E667u + (unsigned)(long long)t * 0xBB67AE85u;
 }
@@ -196,7 +201,7 @@ __device__ __forceinline__ bf16_t round_param<bf16_t>(float x, unsigned h) {
 // One step.  A wave takes 256 elements, a quarter of a chunk, four on each lane, so
 // that a block of 128 lies on half a wave.  (A whole chunk a wave, 16 elements on each
 // lane, is slower at every size: 11 million values with fp32 moments 62 us against 55.)
-// sqrt and reciprocal are the vector unit's, off by an ulp each.  Bound by HBM: 126
+// sqrt and reciprocal are the vector unit's, off by an ulp each (see `careful`).  Bound by HBM: 126
 // million values, moments of 8 bits, gradients in bfloat16 319 us, 5.6 TB/s (a large
 // copy reaches 5.0); 11 million, fp32 moments 56 us, 5.1 TB/s.  With bfloat16
 // parameters too (10 bytes a value) the arithmetic of the codes comes near: 3.6 TB/s.
@@ -244,10 +249,18 @@ __global__ __launch_bounds__(kT) void k_adamw(const TensorList<N> list, StepArgs
     const float gj = to_f32(g.v[j]) * gs;
     m[j] = decayed(m[j], a.b1, gj, a.r1);
     v[j] = decayed(v[j], a.b2, gj * gj, a.r2);
-    const float down = fmaf(__builtin_amdgcn_sqrtf(v[j]), a.root, a.eps);
-    const float x = fmaf(to_f32(p.v[j]), keep, -(m[j] * a.rate) * __builtin_amdgcn_rcpf(down));
-    p.v[j] = round_param<P>(x, h[j]);
   }
+  float go[4];  // the step
+  if (a.careful) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) go[j] = m[j] * a.rate / fmaf(sqrtf(v[j]), a.root, a.eps);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      go[j] = m[j] * a.rate * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[j]), a.root, a.eps));
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) p.v[j] = round_param<P>(fmaf(to_f32(p.v[j]), keep, -go[j]), h[j]);
   store_part<P, 4>(pp, n, p);
   if (BITS == 32) {
     store_part<float, 4>(a.m + at, n, Pack<float, 4>{{m[0], m[1], m[2], m[3]}});
@@ -471,7 +484,7 @@ extern "C" bl_status_t bl_adamw_step(bl_adamw_plan_t p, void* const* params, con
   a.r1 = (float)(1.0 - r.beta1);
   a.b2 = (float)r.beta2;
   a.r2 = (float)(1.0 - r.beta2);
-  a.eps = (float)r.eps;
+  a.eps = r.eps > 0.0 ? std::max((float)r.eps, 0x1p-149f) : 0.f;  // (a v and m of 0 leave the parameter where it is)
   a.seed = r.seed;
   a.beta1 = r.beta1;
   a.beta2 = r.beta2;

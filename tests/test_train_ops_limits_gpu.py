@@ -1,11 +1,11 @@
 """The operators around the convolution layer at the ends of their ranges (MI355X): logits
 of any finite size, subnormal moments, lists of tensors and workspaces as the kernels
 need them.  References and bounds are those of test_train_ops_gpu.py."""
-import math
-
+import numpy as np
 import pytest
 
-from test_train_ops_gpu import U, check_logprob, near, torch  # noqa: F401  (torch: the fixture)
+from paper_1911_09287_amd import bltrain
+from test_train_ops_gpu import U, check_logprob, held, torch, words  # noqa: F401  (torch: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +30,40 @@ def test_logprob_of_finite_logits_of_any_size(torch, classes, dtype):  # noqa: F
     t[10] = classes - 1
     for top in (0, 5):
         check_logprob(torch, z, t, top, dtype, entropy_grad=top == 0)
+
+
+@pytest.mark.parametrize("live", [False, True])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [0.0, 1e-50, 1e-42, 1e-20, 1e-12, 1e-8])
+def test_adamw_of_subnormal_second_moments(torch, eps, bits, live):  # noqa: F811
+    # gradients of 1e-19 to 1e-18: v is subnormal and sqrt(v) is not.  The step is the formula's of the fp32
+    # moments, with a dozen roundings of its own and three of the parameter, as at usual sizes
+    lr, b1, b2, seed, n = 3e-3, 0.9, 0.999, 5, 3000
+    gen = torch.Generator().manual_seed(7)
+    g = torch.exp(torch.rand(n, generator=gen) * np.log(10.0)) * 1e-19
+    g = g * torch.where(torch.rand(n, generator=gen) < 0.5, -1.0, 1.0)
+    if eps:  # (0 / 0 without it)
+        g[::7] = 0.0
+    p = (0.1 * torch.randn(n, generator=gen)).cuda()
+    plan = bltrain.AdamWPlan([n], bits=bits)
+    tensors, state = plan.bind([p], [g.cuda()]), plan.state()
+    clock = torch.zeros(2, dtype=torch.float64, device="cuda")
+    m, v = np.zeros(plan.total, np.float32), np.zeros(plan.total, np.float32)
+    gn = np.zeros(plan.total, np.float32)
+    gn[:n] = g.numpy()
+    for t in range(1, 4):
+        before = p.double().cpu().numpy()
+        clock.copy_(torch.tensor([lr, t], dtype=torch.float64))
+        plan.step(tensors, state, lr=lr, betas=(b1, b2), eps=eps, weight_decay=0.0, step=t, seed=seed,
+                  live=clock if live else None)
+        m = m * np.float32(b1) + gn * np.float32(1 - b1)
+        v = v * np.float32(b2) + gn * gn * np.float32(1 - b2)
+        m64, v64 = m[:n].astype(np.float64), v[:n].astype(np.float64)
+        assert (v64 < 2.0 ** -126).all() and (v64[gn[:n] != 0] > 0).all()
+        if bits == 8:
+            w = words(plan.total, t, seed)
+            m = np.copysign(held(np.abs(m), True, w & np.uint32(0xFFFF)), m)
+            v = held(v, False, w >> np.uint32(16))
+        up = lr / (1 - b1 ** t) * m64 / (np.sqrt(v64 / (1 - b2 ** t)) + eps)
+        off = np.abs(p.double().cpu().numpy() - (before - up)) - (16 * U * np.abs(up) + 3 * U * np.abs(before) + 1e-30)
+        assert off.max() <= 0, (t, off.max())
