@@ -268,7 +268,8 @@ class AdamWTensors:
         if len(params) != len(plan.sizes) or len(grads) != len(plan.sizes):
             raise ValueError(f"expected {len(plan.sizes)} parameters and gradients")
         self.plan, self.params, self.grads = plan, list(params), list(grads)
-        self.on = _gpu(self.params[0], "parameter 0") if self.params else None
+        there = [t for t in self.params + self.grads if t is not None]  # (None: of an empty tensor)
+        self.on = _gpu(there[0], "a parameter") if there else None
         ptrs = _P * len(plan.sizes)
         self._p = ptrs(*[_flat(t, plan.param_dtype, n, f"parameter {i}", self.on)
                          for i, (t, n) in enumerate(zip(params, plan.sizes))])

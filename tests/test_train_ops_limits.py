@@ -166,3 +166,14 @@ def test_norm_rows_whose_weight_gradients_fit_a_launch():
         with pytest.raises(bltrain.BlError) as e:
             bltrain.NormPlan(outer, size)
         assert e.value.code == 2  # BL_ERR_UNSUPPORTED
+
+
+def test_adamw_takes_none_for_empty_tensors(two_gpus):
+    use, calls = two_gpus
+    adam = use(bltrain.AdamWPlan([0, 4, 0]))
+    p, g = (placed(torch.zeros(4), 1) for _ in range(2))
+    tensors = adam.bind([None, p, None], [None, g, None])
+    adam.step(tensors, placed(torch.zeros(adam.state_bytes, dtype=torch.uint8), 1))
+    assert calls == [("bl_adamw_step", 1, 1001)]
+    none = use(bltrain.AdamWPlan([0]))
+    none.step(none.bind([None], [None]), placed(torch.zeros(0, dtype=torch.uint8), 1))
