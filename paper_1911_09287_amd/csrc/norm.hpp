@@ -69,9 +69,11 @@ __device__ __forceinline__ void load_weights(const void* w, bool wide, long from
   }
 }
 
-// Backward, every operation rounded by itself: u and its mean then cancel where they
-// are equal (of one value, or of equal u), and the gradient there is 0 and not what a
-// fused multiply-add would leave of u's rounding, times 1 / sqrt(eps).
+// Backward, every operation rounded by itself: of one value u and its mean are then the
+// same, and the gradient is 0 and not what a fused multiply-add would leave of u's
+// rounding, times 1 / sqrt(eps).  (Of several equal u the sum and the reciprocal of
+// their number round, so that their mean may differ from u by a few units of its last
+// place and a row of equal values have that times 1 / sqrt(eps) for a gradient.)
 __device__ __forceinline__ void add_sums(float u, float h, float& s0, float& s1) {
 #pragma clang fp contract(off)
   s0 += u;

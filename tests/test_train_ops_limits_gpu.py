@@ -5,7 +5,8 @@ import numpy as np
 import pytest
 
 from paper_1911_09287_amd import bltrain
-from test_train_ops_gpu import U, check_logprob, held, torch, words  # noqa: F401  (torch: the fixture)
+from test_train_ops_gpu import (U, check_logprob, held, near, norm_bounds, norm_reference, run_norm, torch,
+                                words)  # noqa: F401  (torch: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +68,22 @@ def test_adamw_of_subnormal_second_moments(torch, eps, bits, live):  # noqa: F81
         up = lr / (1 - b1 ** t) * m64 / (np.sqrt(v64 / (1 - b2 ** t)) + eps)
         off = np.abs(p.double().cpu().numpy() - (before - up)) - (16 * U * np.abs(up) + 3 * U * np.abs(before) + 1e-30)
         assert off.max() <= 0, (t, off.max())
+
+
+@pytest.mark.parametrize("shape", [(4, 3, 1), (4, 5, 1), (4, 50, 1), (3, 300, 1), (3, 3000, 1), (2, 40000, 1), (2, 3, 8),
+                                   (2, 50, 7), (2, 1100, 3)], ids=str)
+def test_norm_gradient_of_equal_values(torch, shape):  # noqa: F811
+    # x and dy the same all along a row: h and dx are 0 but for the roundings of two means, times 1 / sqrt(eps).
+    # Beside the bounds of other rows, which go by the exact h = 0, h's own error enters squared
+    outer, size, inner = shape
+    g = torch.Generator().manual_seed(size)
+    x, dy = (torch.rand(outer, 1, inner, generator=g).expand(shape).contiguous() for _ in range(2))
+    w, b = torch.ones(size), torch.zeros(size)
+    got = run_norm(torch, shape, x, dy, w, b, "f32", "f32", 1e-5)
+    x, dy, w, b = (t.double() for t in (x, dy, w, b))
+    r = norm_reference(x, w, b, dy, 1e-5)
+    bound = norm_bounds(x, w, b, dy, r, 1e-5, "f32", "f32")
+    dh = 16 * U * x * r["rstd"]
+    bound["dx"] = bound["dx"] + 2 * r["rstd"] * dh * dh * dy
+    for name in ("y", "mean", "rstd", "dx"):
+        near(got[name], r[name], bound[name], (shape, name))
