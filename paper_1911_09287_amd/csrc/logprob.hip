@@ -480,6 +480,14 @@ int vectors_of(long n, int threads, int wide) {
   return each;
 }
 
+// go(the vectors of a lane as a constant), of those that calls reach: powers of two from LEAST to MOST.
+template <int LEAST, int MOST, typename Go>
+void with_vectors(int each, Go&& go) {
+  if constexpr (LEAST < MOST)
+    if (each > LEAST) return with_vectors<2 * LEAST, MOST>(each, go);
+  go(std::integral_constant<int, LEAST>());
+}
+
 template <typename T, int WAVES, bool TOP>
 bl_status_t forward(const bl_logprob_plan_s* p, const Ptrs& a, hipStream_t s) {
   const bl_logprob_desc_t& d = p->d;
@@ -490,10 +498,9 @@ bl_status_t forward(const bl_logprob_plan_s* p, const Ptrs& a, hipStream_t s) {
     auto go = [&](auto kernel) {
       hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(kT), 0, s, e0, e1, 0, a, d, p->pieces, p->piece);
     };
-    if (p->each == 1) go(k_logprob_fwd<T, 1, WAVES, TOP>);
-    else if (p->each == 2) go(k_logprob_fwd<T, 2, WAVES, TOP>);
-    else if (p->each == 4) go(k_logprob_fwd<T, 4, WAVES, TOP>);
-    else go(k_logprob_fwd<T, 8, WAVES, TOP>);
+    // (a block's pieces have over 1024 classes; 2048 on a wave are four vectors of 16 bits)
+    constexpr int kLeast = WAVES > 1 && sizeof(T) == 4 ? 2 : 1, kMost = WAVES == 1 && sizeof(T) == 2 ? 4 : 8;
+    with_vectors<kLeast, kMost>(p->each, [&](auto e) { go(k_logprob_fwd<T, decltype(e)::value, WAVES, TOP>); });
   });
   if (st != BL_OK || p->pieces == 1) return st;
   const double left = (double)d.rows * p->pieces * (12 + 8 * d.top);
@@ -527,10 +534,9 @@ bl_status_t backward(const bl_logprob_plan_s* p, const GradPtrs& a, hipStream_t 
     auto go = [&](auto kernel) {
       hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(kT), 0, s, e0, e1, 0, a, d, pieces, piece);
     };
-    if (each == 1) go(k_logprob_bwd<T, 1, WAVES, ENTROPY>);
-    else if (each == 2) go(k_logprob_bwd<T, 2, WAVES, ENTROPY>);
-    else if (each == 4 || WAVES > 1 || sizeof(T) == 2) go(k_logprob_bwd<T, 4, WAVES, ENTROPY>);
-    else go(k_logprob_bwd<float, 8, 1, ENTROPY>);
+    // (a block's pieces have over 2048 classes)
+    constexpr int kLeast = WAVES == 1 ? 1 : sizeof(T) == 2 ? 2 : 4, kMost = WAVES == 1 && sizeof(T) == 4 ? 8 : 4;
+    with_vectors<kLeast, kMost>(each, [&](auto e) { go(k_logprob_bwd<T, decltype(e)::value, WAVES, ENTROPY>); });
   });
 }
 

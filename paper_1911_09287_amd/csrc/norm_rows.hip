@@ -474,7 +474,7 @@ bl_norm_rows rows_shape(long nv, int most, bool backward) {
     return r;
   }
   r.block = true;
-  r.each = backward ? 1 : 2;
+  r.each = 2;
   r.threads = 256;
   while ((long)r.threads * r.each < nv) {
     if (r.each < (backward ? 2 : 4)) r.each *= 2;
@@ -500,7 +500,7 @@ bl_status_t launch_fwd(const bl_norm_plan_s* p, const NormPtrs& a, hipStream_t s
     auto go = [&](auto kernel) {
       hipExtLaunchKernelGGL(kernel, dim3(blocks), dim3(BLOCK ? r.threads : kT), 0, s, e0, e1, 0, a, p->d, r.threads);
     };
-    if (r.each == 1) go(k_rows_fwd<T, 1, BLOCK>);
+    if (r.each == 1) go(k_rows_fwd<T, 1, false>);
     else if (r.each == 2) go(k_rows_fwd<T, 2, BLOCK>);
     else if (r.each == 4) go(k_rows_fwd<T, 4, BLOCK>);
     else go(k_rows_fwd<float, 8, true>);
@@ -516,7 +516,7 @@ bl_status_t launch_bwd(const bl_norm_plan_s* p, const NormPtrs& a, bool sums, hi
       hipExtLaunchKernelGGL(kernel, dim3(p->parts), dim3(BLOCK ? r.threads : kT), 0, s, e0, e1, 0, a, p->d, r.threads,
                             sums);
     };
-    if (r.each == 1) go(k_rows_bwd<T, 1, BLOCK>);
+    if (r.each == 1) go(k_rows_bwd<T, 1, false>);
     else if (r.each == 2) go(k_rows_bwd<T, 2, BLOCK>);
     else if (BLOCK) go(k_rows_bwd<float, 4, true>);
     else go(k_rows_bwd<T, 4, false>);
