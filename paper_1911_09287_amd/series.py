@@ -1,4 +1,4 @@
-"""Training a time-series classifier from the library's operators alone.
+"""Training a time-series classifier with the library's convolutions, norms, loss and step.
 
 The three-layer fully convolutional network of the time-series workload: band-limited
 convolutions (8, 5 and 3 taps), each followed by a layer norm over the channels at
