@@ -7,8 +7,9 @@
  * Ownership: as in blconv.h, the caller owns every device buffer and creating
  * and querying a plan makes no HIP call.  Compute calls allocate nothing, keep
  * nothing from one call for the next, make no host synchronisation and enqueue
- * their kernels on `stream` (a hipStream_t, NULL = the default stream), so they
- * can be captured in a HIP graph.  A workspace is scratch: its contents before
+ * their kernels on `stream` (a hipStream_t, NULL = the default stream) of the
+ * current device, which has to be the buffers' own, so they can be captured in a
+ * HIP graph.  A workspace is scratch: its contents before
  * and after a call mean nothing.  Workspaces and AdamW's state must be aligned to
  * 16 bytes (else BL_ERR_INVALID_ARG); tensors need the alignment of their element
  * type only.
@@ -140,7 +141,9 @@ bl_status_t bl_logprob_backward(bl_logprob_plan_t plan, const void* logits, cons
  *   p = p (1 - lr weight_decay) - (lr / (1 - beta1^t)) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  *
  * (weight decay where the tensor's decay byte is set.)  Parameters are fp32 or
- * bfloat16, gradients fp32, bfloat16 or fp16.
+ * bfloat16, gradients fp32, bfloat16 or fp16.  With eps = 0 a value without any
+ * gradient so far becomes NaN (0 / 0), and one whose g g is below fp32's least
+ * subnormal value infinite.
  *
  * State: one device buffer of the caller's, filled with zero bytes before the
  * first step.  Tensor i's moments start at element start[i] of both moments'
@@ -179,7 +182,8 @@ typedef struct {
   unsigned seed;           /* of the dither */
   const float* grad_scale; /* device; NULL: 1 */
   const double* live;      /* device {lr, step} in the place of the two above, read when
-                              the kernels run, so that a captured step can go on; or NULL */
+                              the kernels run, so that a captured step can go on; or NULL.
+                              Moments of 8 bits take about twice the time with it */
 } bl_adamw_args_t;
 
 typedef struct bl_adamw_plan_s* bl_adamw_plan_t;

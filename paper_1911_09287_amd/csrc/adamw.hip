@@ -201,10 +201,12 @@ __device__ __forceinline__ bf16_t round_param<bf16_t>(float x, unsigned h) {
 // One step.  A wave takes 256 elements, a quarter of a chunk, four on each lane, so
 // that a block of 128 lies on half a wave.  (A whole chunk a wave, 16 elements on each
 // lane, is slower at every size: 11 million values with fp32 moments 62 us against 55.)
-// sqrt and reciprocal are the vector unit's, off by an ulp each (see `careful`).  Bound by HBM: 126
-// million values, moments of 8 bits, gradients in bfloat16 319 us, 5.6 TB/s (a large
-// copy reaches 5.0); 11 million, fp32 moments 56 us, 5.1 TB/s.  With bfloat16
-// parameters too (10 bytes a value) the arithmetic of the codes comes near: 3.6 TB/s.
+// sqrt and reciprocal are the vector unit's, off by an ulp each (see `careful`).  Bound
+// by HBM: 126 million values, moments of 8 bits, gradients in bfloat16 313 us, 5.7 TB/s
+// (a large copy reaches 5.0); 11 million, fp32 moments 56 us, 5.2 TB/s.  With bfloat16
+// parameters too (10 bytes a value) the arithmetic of the codes comes near: 294 us, 4.3
+// TB/s.  A live step takes its scalars' powers in 64 bits on every lane: 579 us instead
+// of the 313, but 60 instead of the 56 (and 1 more of the smallest).
 template <typename P, typename G, int BITS, bool LIVE, int N>
 __global__ __launch_bounds__(kT) void k_adamw(const TensorList<N> list, StepArgs a) {
   const unsigned lane = threadIdx.x & 63;

@@ -22,9 +22,13 @@
 // joins them.
 //
 // Measured: 4096 rows of 32000 logits without likeliest classes fp32 88 us, 6.0 TB/s,
-// bfloat16 51 us, 5.1 TB/s, with 8 of them 70 us; 513 rows of 50021 fp32 logits with
-// 20 of them 25.5 us, 4.0 TB/s, and 5.6 us for the join; one row of 131071 bfloat16
-// logits with 8 of them 5.4 + 5.5 us, hardly more than two launches take anyhow.
+// bfloat16 50 us, 5.2 TB/s, with 8 of them 68 us; 513 rows of 50021 fp32 logits with
+// 20 of them 26 us, 4.0 TB/s, and 5.7 us for the join; one row of 131071 bfloat16
+// logits with 8 of them 5.6 + 5.6 us, hardly more than two launches take anyhow.  Rows
+// with hardly any class left (the others at minus infinity) leave lanes without one, the
+// bound falls to minus infinity and 64 keys after another are taken: 513 rows of 50021 with
+// 300 left 46 us, with 16 56; 4096 of 32000 bfloat16 with 16 left 221.  Rows of 1025 to 2048
+// fp32 logits with likeliest classes are short of five registers a lane (3.8 TB/s).
 #include <algorithm>
 #include <new>
 
@@ -414,7 +418,8 @@ __global__ __launch_bounds__(kT) void k_logprob_join(Ptrs a, bl_logprob_desc_t d
 }
 
 // Gradient: E vectors of a piece a lane (WAVES = 1: a row by a wave), read and
-// written once.  Bound by HBM: 4096 rows of 65536 bfloat16 logits 210 us, 5.1 TB/s.
+// written once.  Bound by HBM: 4096 rows of 65536 bfloat16 logits 212 us, 5.1 TB/s, with
+// the entropy's gradient 213.
 struct GradPtrs {
   const void* logits;
   const long long* targets;
@@ -468,7 +473,12 @@ __global__ __launch_bounds__(kT) void k_logprob_bwd(GradPtrs a, bl_logprob_desc_
 using namespace blc;
 
 namespace {
-constexpr long kWaveClasses = 2048;   // rows up to so many lie on one wave
+// Rows up to so many classes lie on one wave.  8192 rows, wave / block, forward with 8
+// likeliest classes and without, backward: 1100 fp32 16.5 / 31, 9.4 / 14.7, 15.5 / 14.0
+// us; 2048 18.6 / 32, 12.5 / 14.8, 28 / 28; 2048 bfloat16 18.2 / 35, 9.0 / 14, 15.9 /
+// 13.4; 4096 fp32 105 / 40 (registers), 105 / 24, 56 / 48.  4096 bfloat16 take 23 us on a
+// wave and 40 on a block, but 64 rows of 2048 6.6 and 5.5.
+constexpr long kWaveClasses = 2048;
 constexpr long kPieceVectors = 8 * kT; // and pieces of longer ones on a block, 8 vectors a lane
 constexpr unsigned kGrid = 1u << 20;  // blocks of a launch, which go on with what is left
 
@@ -504,6 +514,8 @@ bl_status_t forward(const bl_logprob_plan_s* p, const Ptrs& a, hipStream_t s) {
   });
   if (st != BL_OK || p->pieces == 1) return st;
   const double left = (double)d.rows * p->pieces * (12 + 8 * d.top);
+  // (wave / block: 513 rows of 7 pieces with 8 classes 4.1 / 5.4 us, 16 5.2 / 5.4, 20 5.2 / 5.7,
+  // 32 7.6 / 5.6; 4096 of 2 with 8 5.4 / 14.6; one of 64 with 8 10 / 5.5)
   const bool by_waves = p->pieces <= kWave && (long)p->pieces * d.top <= 2 * kWave;
   const long long join = by_waves ? (d.rows + kWaves - 1) / kWaves : d.rows;
   return timed_launch("logprob_join", left, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
@@ -563,7 +575,9 @@ extern "C" bl_status_t bl_logprob_plan_create(bl_logprob_plan_t* out, const bl_l
   p->d = d;
   p->block = d.classes > kWaveClasses;
   long most = kPieceVectors * (16 / dtype_bytes(d.dtype));
-  // few rows in pieces anyway: smaller ones, until there is one for each compute unit
+  // few rows in pieces anyway: smaller ones, until there is one for each compute unit (until
+  // 128 / 256 / 512, and the join: 32 rows of 50021 fp32 logits with 20 classes 7.1 + 4.7 / 6.9
+  // + 4.9 / 7.9 + 6.0 us; 4 of 131071 bfloat16 with 8 6.4 + 4.4 / 5.8 + 5.7 / 6.0 + 5.7)
   while (d.classes > kPieceVectors * (16 / dtype_bytes(d.dtype)) && most > kWaveClasses && d.rows * ((d.classes + most - 1) / most) < 256) most /= 2;
   p->pieces = p->block ? (int)((d.classes + most - 1) / most) : 1;
   p->piece = p->pieces == 1 ? (long)d.classes : ((d.classes + p->pieces - 1) / p->pieces + 15) / 16 * 16;

@@ -6,8 +6,12 @@
 // every value is read once and written once, and sums over the channels cross the
 // lanes by shuffles and the waves by way of LDS.  Backward, a thread keeps the
 // sums of its channels' dw and db over all tiles of its block.  Bound by HBM: 64 maps
-// of 256 channels and 512 positions, fp32, forward 12 us, 5.5 TB/s, backward 23 us, 4.4
-// TB/s, and 4 us for the last sum over blocks.
+// of 256 channels and 512 positions, fp32, forward 12 us, 5.6 TB/s, backward 23 us, 4.4
+// TB/s, while the tensors lie in the 256 MB cache; from memory 19 us, 3.5 TB/s, and 24
+// us, 4.2 TB/s; and 4 us for the last sum over blocks.  More than 512 channels in fp32
+// leave room for one block a compute unit (1024: forward 61 us at four times the size,
+// 4.4 TB/s, backward 130 us, 3.1 TB/s); backward of 257 to 1024 channels in 16 bits is short
+// of two or three registers a lane.
 #include <algorithm>
 
 #include "norm.hpp"
@@ -221,8 +225,9 @@ __global__ __launch_bounds__(THREADS, 4) void k_maps_bwd(NormPtrs a, bl_norm_des
 }
 
 // More channels than a block's registers hold (over 1024): they are read again for
-// the squares and for the result (from L2).  One position a lane: 8 maps of 2000
-// channels and 512 positions take 100 us forward and 160 us backward, 0.6 TB/s.
+// the squares and for the result (from L2).  One position a lane, and one load of a lane
+// in flight: 8 maps of 2000 channels and 512 positions, 64 blocks, take 102 us forward
+// and 162 us backward, 0.6 TB/s.
 constexpr int kStreamThreads = 1024;
 __device__ __forceinline__ void stream_sum(float (&x)[2], float (*red)[2 * kWave]) { channel_sum<2, kWave, kStreamThreads>(x, red); }
 
@@ -435,7 +440,10 @@ bl_status_t norm_maps_plan(bl_norm_plan_s* p) {
   }
   unsigned per_slice;
   const long tiles = tiles_of(p->d, shapes[1].vec, shapes[1].lanes, &per_slice);
-  // as many blocks as are on the GPU at once: each gives a row of partial sums
+  // as many blocks as are on the GPU at once: each gives a row of partial sums (half of
+  // them / these / twice, with the last sum, fp32 at 512 positions: 64 maps of 256
+  // channels 25 + 4 / 23 + 4 / 26.5 + 6.5 us, of 512 63 + 4 / 45 + 4 / 47 + 4; on blocks
+  // of 1024 of 1024 channels 177 + 4 / 129 + 4 / 130 + 5)
   p->parts = (int)std::min<long>(tiles, shapes[1].threads == kMostThreads ? 256 : 512);
   p->off_part = 0;
   p->bytes = (size_t)p->parts * 2 * p->d.size * sizeof(float);

@@ -10,10 +10,12 @@
 // over its block's rows, in registers, and a last small launch.
 //
 // Measured (kernel, bytes read and written once): 16384 rows of 1024 fp32 values
-// forward 28 us, 4.8 TB/s, backward 39 us, 5.2 TB/s; of 2048 bfloat16 values 34 us,
-// 3.9 TB/s, and 44 us, 4.6 TB/s (twice the values to convert for the same bytes);
-// 4096 of 8192 fp32 values 53 us, 5.0 TB/s, and 81 us, 4.9 TB/s; 32 of 200704 fp32
-// values, two launches, 6.4 + 11 us forward, 10 + 19 us backward.
+// forward 27 us, 4.9 TB/s, backward 38 us, 5.2 TB/s; of 2048 bfloat16 values 33 us,
+// 4.1 TB/s, and 43 us, 4.7 TB/s (twice the values to convert for the same bytes);
+// 4096 of 8192 fp32 values 52 us, 5.2 TB/s, and 82 us, 4.9 TB/s (of over 8192
+// backward 4.3 TB/s: a lane's 128 registers are short by five); 32 of 200704 fp32
+// values, two launches, 6.3 + 11 us forward, 10 + 19 us backward while the tensors lie
+// in the 256 MB cache, 8.3 + 11 and 14 + 19 from memory.
 #include <algorithm>
 
 #include "norm.hpp"
@@ -24,7 +26,9 @@ namespace {
 constexpr int kT = kNormThreads;
 constexpr int kMostThreads = 1024;
 constexpr int kTargetBlocks = 512;  // two a compute unit
-constexpr int kSplitBlocks = 1792;  // seven a compute unit
+// Seven a compute unit (half of them / these / twice: 32 rows of 200704 fp32 values
+// 12.0 / 11.4 / 12.6 us, 200 of 50000 14.9 / 13.4 / 13.9, 2000 of 60000 bfloat16 127 / 114 / 109).
+constexpr int kSplitBlocks = 1792;
 
 // ---- sums over the lanes of a row ---------------------------------------------
 // BLOCK: over the block, by way of LDS; `red` alternates between two arrays from
@@ -463,11 +467,14 @@ __global__ __launch_bounds__(kT) void k_split_bwd(NormPtrs a, bl_norm_desc_t d, 
   }
 }
 
-// How a row of nv vectors lies on lanes, `most` vectors on one at most.
+// How a row of nv vectors lies on lanes, `most` vectors on one at most: on a wave up to
+// four a lane, else on a block.  16384 rows, wave / block of 256, forward and backward:
+// 600 fp32 values 14.9 / 22.2 and 27 / 41 us, 1024 27.1 / 29.7 and 38 / 43, 2048
+// bfloat16 33 / 35 and 43 / 52.  Of 2048 fp32 values, eight on a wave / block: 53.5 / 51
+// and 77 / 71; of 4096 bfloat16 63 / 61 and 108 / 83.
 bl_norm_rows rows_shape(long nv, int most, bool backward) {
   bl_norm_rows r{};
-  const int wave_each = 4;
-  if (nv <= (long)kWave * wave_each) {
+  if (nv <= 4L * kWave) {
     r.each = nv <= kWave ? 1 : nv <= 2 * kWave ? 2 : 4;
     r.threads = 1;
     while ((long)r.threads * r.each < nv) r.threads *= 2;
@@ -593,6 +600,10 @@ bl_status_t norm_rows_plan(bl_norm_plan_s* p) {
     p->row_groups = (int)std::min<long>(rows, std::max<long>(1, kTargetBlocks / (p->pieces / kBlockWaves)));
     p->parts = p->row_groups;
   } else {
+    // as many blocks as run at a time, each with a row of partial sums (half of them /
+    // these / twice, with the last sum: 16384 rows of 2048 bfloat16 values 49 + 4 / 43 +
+    // 4 / 47 + 6.5 us, of 1024 fp32 43 + 4 / 38 + 4 / 42 + 6.6; on blocks of 1024 2000
+    // of 16384 113 + 4 / 92 + 6 / 103 + 11)
     const long each = p->bwd.block ? 1 : kT / p->bwd.threads;
     p->parts = (int)std::min<long>((rows + each - 1) / each, p->bwd.block && p->bwd.threads > 512 ? kTargetBlocks / 2 : kTargetBlocks);
   }
