@@ -1,8 +1,9 @@
 /*
  * bltrain.h -- what a training step or an answer needs around the band-limited
- * convolution layer of blconv.h: layer norm, the log probabilities that a
- * classifier's or a language model's loss is made of, and the AdamW update of
- * many tensors, for AMD Instinct MI355X (gfx950).
+ * convolution layer of blconv.h: layer norm, group norm with an activation, a
+ * gated linear recurrence, the log probabilities that a classifier's or a
+ * language model's loss is made of, the AdamW update of many tensors and the
+ * orthogonalised update of many matrices, for AMD Instinct MI355X (gfx950).
  *
  * Ownership: as in blconv.h, the caller owns every device buffer and creating
  * and querying a plan makes no HIP call.  Compute calls allocate nothing, keep
@@ -10,7 +11,7 @@
  * their kernels on `stream` (a hipStream_t, NULL = the default stream) of the
  * current device, which has to be the buffers' own, so they can be captured in a
  * HIP graph.  A workspace is scratch: its contents before
- * and after a call mean nothing.  Workspaces and AdamW's state must be aligned to
+ * and after a call mean nothing.  Workspaces and optimisers' states must be aligned to
  * 16 bytes (else BL_ERR_INVALID_ARG); tensors need the alignment of their element
  * type only.
  *
@@ -20,7 +21,7 @@
  *
  * Arithmetic: values are converted to fp32 when they are loaded; sums,
  * statistics, moments and norms are held in fp32 and a result is rounded once,
- * to nearest even, when it is stored (AdamW's parameters of 16 bits and moments
+ * to nearest even, when it is stored (optimisers' parameters of 16 bits and moments
  * of 8 bits: by a dither, see there).  Sums are taken in an order that depends
  * on sizes alone: the same call on the same values gives the same bits.
  *
@@ -86,6 +87,125 @@ bl_status_t bl_norm_forward(bl_norm_plan_t plan, const void* x, const void* w, c
  * may be dy or x (the same pointer and strides). */
 bl_status_t bl_norm_backward(bl_norm_plan_t plan, const void* dy, const void* x, const void* w, const float* stats,
                              void* dx, void* dw, void* db, void* ws, void* stream);
+
+/* ---- group norm with an activation ---------------------------------------------
+ *
+ * Of x [batch][sites][channels] (BL_CHANNELS_LAST) or [batch][channels][sites]
+ * (BL_CHANNELS_FIRST: the convolution layer's maps), whose channels fall into
+ * `groups` of channels / groups neighbours each.  Over the sites and channels of
+ * every sample n and group g, `size` = sites channels / groups values,
+ *
+ *   mean = sum x / size,   rstd = 1 / sqrt(sum (x - mean)^2 / size + eps)
+ *   z = (x - mean) rstd w[c] + b[c],   y = act(z)
+ *
+ * act: z itself, max(z, 0) or z / (1 + exp(-z)).  x and dx have `dtype` and lie
+ * samples x_stride elements apart (0: dense), y and dy likewise with y_stride.
+ * w, b, dw, db [channels] have `wdtype`: fp32, or dtype. */
+#define BL_CHANNELS_LAST 0
+#define BL_CHANNELS_FIRST 1
+
+#define BL_ACT_NONE 0
+#define BL_ACT_RELU 1
+#define BL_ACT_SILU 2
+
+typedef struct {
+  long long batch;    /* >= 0; 0: the calls do nothing but zero dw and db */
+  long long sites;    /* >= 1 */
+  long long channels; /* >= 1, a multiple of groups */
+  long long groups;   /* >= 1 */
+  int layout, act;
+  int dtype, wdtype;
+  double eps; /* >= 0 */
+  long long x_stride, y_stride;
+} bl_group_norm_desc_t;
+
+typedef struct bl_group_norm_plan_s* bl_group_norm_plan_t;
+
+/* BL_ERR_UNSUPPORTED: sites channels >= 2^31, batch channels >= 2^31, batch >= 2^31. */
+bl_status_t bl_group_norm_plan_create(bl_group_norm_plan_t* out, const bl_group_norm_desc_t* desc);
+bl_status_t bl_group_norm_plan_destroy(bl_group_norm_plan_t plan);
+/* Workspace bytes of either call (0: ws may be NULL). */
+bl_status_t bl_group_norm_workspace_size(bl_group_norm_plan_t plan, size_t* bytes);
+
+/* y, and in stats [2][batch][groups] (fp32; NULL: not wanted) mean and rstd.
+ * w NULL: 1, b NULL: 0.  y may be x (the same pointer and strides). */
+bl_status_t bl_group_norm_forward(bl_group_norm_plan_t plan, const void* x, const void* w, const void* b, void* y,
+                                  float* stats, void* ws, void* stream);
+
+/* Gradients of <dy, y>: with h = (x - mean) rstd, dz = dy act'(z) and u = dz w,
+ *   dx = rstd (u - mean u - h mean (u h)) with means over the group's values,
+ *   dw[c] = sum over batch and sites of dz h,  db[c] = sum of dz.
+ * stats: what bl_group_norm_forward gave, of the same x, w and b; max(z, 0) has
+ * the gradient 1 where the forward call's z is above 0, else 0.  dw or db NULL: not
+ * wanted; w NULL: 1, b NULL: 0.  dx may be dy or x (the same pointer and strides). */
+bl_status_t bl_group_norm_backward(bl_group_norm_plan_t plan, const void* dy, const void* x, const void* w,
+                                   const void* b, const float* stats, void* dx, void* dw, void* db, void* ws,
+                                   void* stream);
+
+/* ---- gated linear recurrence ---------------------------------------------------
+ *
+ * Along the middle axis of [outer][length][inner]: at every (o, i), from h_(-1) = h0,
+ *
+ *   h_t = a_t h_(t-1) + b_t
+ *
+ * BL_GATE_SIGMOID: a = 1 / (1 + exp(-gate)), b = (1 - a) x;  BL_GATE_EXP: a =
+ * exp(gate), b = x.  inner = 1 runs along the samples of the convolution layer's
+ * [N][C][L] maps (outer = N C), inner = channels along tokens with their channels
+ * side by side; length = 1 takes one more token from the state that the last call
+ * left.
+ *
+ * resets [outer][length] (bytes; NULL: none): at a step whose byte is not 0 the
+ * state is dropped, h_t = b_t, whatever it was, NaN and infinity among it, and no
+ * gradient passes to the steps before.  So sequences packed one after another are
+ * kept apart by a reset at each one's first step, and what follows a padded
+ * sequence's end by one at its first unused step.
+ *
+ * The sums are taken over stretches of steps: h over a stretch is (product of a)
+ * h_before + (what its own steps give).  With exp(gate) above 1 a stretch's product can
+ * exceed fp32's range, or h0 times it be NaN, where the single steps' results would
+ * not: gates above 0 are for lengths over which their sum stays below 88.
+ *
+ * gate, x, dgate and dx have `dtype`; element (o, t, i) lies at o in_outer + t
+ * in_step + i (0: dense, in_step = inner and in_outer = length in_step), so that gates
+ * and values may be parts of one tensor; y and dy likewise with out_outer and
+ * out_step.  States are fp32 [outer][inner]. */
+#define BL_GATE_SIGMOID 0
+#define BL_GATE_EXP 1
+
+typedef struct {
+  long long outer;  /* >= 0 */
+  long long length; /* >= 0; 0: last = h0, dh0 = dlast */
+  long long inner;  /* >= 1 */
+  int gate, dtype;
+  long long in_outer, in_step, out_outer, out_step;
+} bl_recurrence_desc_t;
+
+typedef struct bl_recurrence_plan_s* bl_recurrence_plan_t;
+
+/* BL_ERR_UNSUPPORTED: outer inner >= 2^31, length >= 2^31. */
+bl_status_t bl_recurrence_plan_create(bl_recurrence_plan_t* out, const bl_recurrence_desc_t* desc);
+bl_status_t bl_recurrence_plan_destroy(bl_recurrence_plan_t plan);
+/* Workspace bytes of either call (0: ws may be NULL), and elements (fp32) of `states`. */
+bl_status_t bl_recurrence_workspace_size(bl_recurrence_plan_t plan, size_t* bytes);
+bl_status_t bl_recurrence_states_size(bl_recurrence_plan_t plan, long long* elements);
+
+/* y = h of every step (rounded to dtype); last: h of the last one (fp32; NULL: not
+ * wanted); states: what the backward call needs (NULL: not wanted).  h0 NULL: 0.  y
+ * may be x (the same pointer and strides), last may be h0. */
+bl_status_t bl_recurrence_forward(bl_recurrence_plan_t plan, const void* gate, const void* x,
+                                  const unsigned char* resets, const float* h0, void* y, float* last, float* states,
+                                  void* ws, void* stream);
+
+/* Gradients of <dy, y> + <dlast, last>: with dh_t = dy_t + a_(t+1) dh_(t+1),
+ *   BL_GATE_SIGMOID: dgate_t = dh_t (h_(t-1) - x_t) a_t (1 - a_t),  dx_t = dh_t (1 - a_t)
+ *   BL_GATE_EXP:     dgate_t = dh_t h_(t-1) a_t,                    dx_t = dh_t
+ *   dh0 = a_0 dh_0
+ * (h_(t-1) = 0 and nothing passed on at a reset).  states: what bl_recurrence_forward
+ * gave.  dlast NULL: 0; dh0 NULL: not wanted.  dgate may be gate and dx may be x (the
+ * same pointers), dh0 may be dlast. */
+bl_status_t bl_recurrence_backward(bl_recurrence_plan_t plan, const void* gate, const void* x,
+                                   const unsigned char* resets, const float* states, const void* dy,
+                                   const float* dlast, void* dgate, void* dx, float* dh0, void* ws, void* stream);
 
 /* ---- log probabilities ------------------------------------------------------
  *
@@ -210,6 +330,75 @@ bl_status_t bl_adamw_step(bl_adamw_plan_t plan, void* const* params, const void*
  * set, as they are in what is given. */
 bl_status_t bl_adamw_get_moments(bl_adamw_plan_t plan, const void* state, void* m, void* v, void* stream);
 bl_status_t bl_adamw_set_moments(bl_adamw_plan_t plan, void* state, const float* m, const float* v, void* stream);
+
+/* ---- orthogonalised update -----------------------------------------------------
+ *
+ * The Muon optimiser's step over `count` matrices (after Jordan et al., "Muon: An
+ * optimizer for hidden layers in neural networks", 2024), with s = *grad_scale:
+ *
+ *   g = s grad,  m = momentum m + g,  u = g + momentum m (nesterov) or m
+ *   X = u / (|u| + eps)  (Frobenius norm), then `steps` times
+ *   A = X X^T,  B = a I + b A + c A A,  X = B X
+ *   p = p (1 - lr weight_decay) - lr scale X
+ *
+ * which takes every singular value t of X to a t + b t^3 + c t^5 with that step's
+ * coefficients (a, b, c).  The usual ones, 3.4445, -4.7750, 2.0315 five times,
+ * bring all but the smallest singular values to 0.7 ... 1.2; any others have to keep
+ * them at most 1.75 from step to step, beginning with 0 ... 1.  A matrix of more rows
+ * than columns is taken by its transpose.  A matrix that holds a NaN or an infinity,
+ * or whose |u| does, gives NaN throughout; one of zeros stays.
+ *
+ * Matrices are dense, rows x cols; weights of a convolution layer are [C_out][C_in
+ * taps].  Parameters are fp32 or bfloat16 (rounded by the hash of AdamW's, of the
+ * element's place in the state's layout), gradients fp32, bfloat16 or fp16.  The products
+ * are taken on the matrix cores from values held as two fp16 parts with a power of two
+ * for each quantity, 22 bits from its largest possible magnitude down to 2^-14 of it and
+ * 2^-39 of it below, and summed in fp32.
+ *
+ * State: one device buffer of the caller's that holds m in fp32, filled with zero
+ * bytes before the first step: matrix i starts at element start[i], a multiple of
+ * 64; elements between them stay as they are. */
+typedef struct {
+  int count;              /* >= 0 */
+  const long long* rows;  /* [count] >= 0 (host memory, copied, as all that follow) */
+  const long long* cols;  /* [count] >= 0 */
+  const unsigned char* decay; /* [count] 1: weight decay applies; NULL: to all */
+  const double* scale;    /* [count]; NULL: sqrt(max(1, rows / cols)) */
+  int steps;              /* 1 ... 16 */
+  const double* coef;     /* [steps][3]; NULL: the usual ones in every step */
+  int param_dtype;        /* BL_F32 or BL_BF16 */
+  int grad_dtype;
+} bl_muon_desc_t;
+
+typedef struct {
+  double lr, momentum, eps, weight_decay; /* momentum 0 ... < 1, eps > 0 */
+  int nesterov;
+  long long step;          /* of the rounding's hash, as is seed */
+  unsigned seed;
+  const float* grad_scale; /* device; NULL: 1 */
+  const double* live;      /* device {lr, step} in the place of the two above, read when the
+                              kernels run; or NULL */
+} bl_muon_args_t;
+
+typedef struct bl_muon_plan_s* bl_muon_plan_t;
+
+/* BL_ERR_INVALID_ARG: coefficients that let a singular value of 0 ... 1 grow over 1.75.
+ * BL_ERR_UNSUPPORTED: a side over 65536, a matrix of 2^31 elements or more. */
+bl_status_t bl_muon_plan_create(bl_muon_plan_t* out, const bl_muon_desc_t* desc);
+bl_status_t bl_muon_plan_destroy(bl_muon_plan_t plan);
+/* Bytes of the state, elements of m's layout, and start[count] (any may be NULL). */
+bl_status_t bl_muon_state_size(bl_muon_plan_t plan, size_t* bytes, long long* total, long long* start);
+/* Workspace bytes of either call below. */
+bl_status_t bl_muon_workspace_size(bl_muon_plan_t plan, size_t* bytes);
+
+/* params, grads: host arrays of `count` device pointers (those of empty matrices may
+ * be NULL).  Parameters and state are updated in place. */
+bl_status_t bl_muon_step(bl_muon_plan_t plan, void* const* params, const void* const* grads, void* state, void* ws,
+                         const bl_muon_args_t* args, void* stream);
+/* X of u = grad alone, rounded to nearest, to out (matrices of the parameters' type;
+ * out[i] may be grads[i] where the types agree). */
+bl_status_t bl_muon_orthogonalize(bl_muon_plan_t plan, void* const* out, const void* const* grads, void* ws,
+                                  double eps, void* stream);
 
 #ifdef __cplusplus
 }

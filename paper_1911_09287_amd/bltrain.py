@@ -1,7 +1,7 @@
 """ctypes binding of the operators around the convolution layer (include/bltrain.h).
 
-Layer norm, log probabilities and the AdamW step, as plans like ``blconv.Plan``:
-argument marshalling only, every compute step runs in the HIP kernels of
+Layer norm, group norm, the gated recurrence, log probabilities and the AdamW and
+orthogonalised steps, as plans like ``blconv.Plan``: argument marshalling only, every compute step runs in the HIP kernels of
 libblconv.so on the GPU that holds the tensors, all of them on one, and on that
 GPU's current stream (or the one given).  Buffers are the caller's;
 ``workspace()`` and ``state()`` make those whose size a plan sets.
@@ -16,12 +16,20 @@ from . import blconv
 from .blconv import BlError, _check  # noqa: F401  (BlError: what these calls raise)
 
 BL_F32, BL_BF16, BL_F16 = 0, 1, 2
+BL_CHANNELS_LAST, BL_CHANNELS_FIRST = 0, 1
+BL_ACT_NONE, BL_ACT_RELU, BL_ACT_SILU = 0, 1, 2
+BL_GATE_SIGMOID, BL_GATE_EXP = 0, 1
 
 EXPORTED = (
     "bl_norm_plan_create", "bl_norm_plan_destroy", "bl_norm_workspace_size", "bl_norm_forward", "bl_norm_backward",
     "bl_logprob_plan_create", "bl_logprob_plan_destroy", "bl_logprob_workspace_size", "bl_logprob_forward",
     "bl_logprob_backward", "bl_adamw_plan_create", "bl_adamw_plan_destroy", "bl_adamw_state_size",
     "bl_adamw_state_layout", "bl_adamw_step", "bl_adamw_get_moments", "bl_adamw_set_moments",
+    "bl_group_norm_plan_create", "bl_group_norm_plan_destroy", "bl_group_norm_workspace_size",
+    "bl_group_norm_forward", "bl_group_norm_backward", "bl_recurrence_plan_create", "bl_recurrence_plan_destroy",
+    "bl_recurrence_workspace_size", "bl_recurrence_states_size", "bl_recurrence_forward", "bl_recurrence_backward",
+    "bl_muon_plan_create", "bl_muon_plan_destroy", "bl_muon_state_size", "bl_muon_workspace_size", "bl_muon_step",
+    "bl_muon_orthogonalize",
 )
 
 _P, _I, _L, _D, _S = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_double, ctypes.c_size_t
@@ -43,6 +51,27 @@ class AdamWDesc(ctypes.Structure):
 
 class AdamWArgs(ctypes.Structure):
     _fields_ = [("lr", _D), ("beta1", _D), ("beta2", _D), ("eps", _D), ("weight_decay", _D), ("step", _L),
+                ("seed", ctypes.c_uint), ("grad_scale", _P), ("live", _P)]
+
+
+class GroupNormDesc(ctypes.Structure):
+    _fields_ = [("batch", _L), ("sites", _L), ("channels", _L), ("groups", _L), ("layout", _I), ("act", _I),
+                ("dtype", _I), ("wdtype", _I), ("eps", _D), ("x_stride", _L), ("y_stride", _L)]
+
+
+class RecurrenceDesc(ctypes.Structure):
+    _fields_ = [("outer", _L), ("length", _L), ("inner", _L), ("gate", _I), ("dtype", _I), ("in_outer", _L),
+                ("in_step", _L), ("out_outer", _L), ("out_step", _L)]
+
+
+class MuonDesc(ctypes.Structure):
+    _fields_ = [("count", _I), ("rows", ctypes.POINTER(_L)), ("cols", ctypes.POINTER(_L)),
+                ("decay", ctypes.POINTER(ctypes.c_ubyte)), ("scale", ctypes.POINTER(_D)), ("steps", _I),
+                ("coef", ctypes.POINTER(_D)), ("param_dtype", _I), ("grad_dtype", _I)]
+
+
+class MuonArgs(ctypes.Structure):
+    _fields_ = [("lr", _D), ("momentum", _D), ("eps", _D), ("weight_decay", _D), ("nesterov", _I), ("step", _L),
                 ("seed", ctypes.c_uint), ("grad_scale", _P), ("live", _P)]
 
 
@@ -70,7 +99,22 @@ def load():
     lib.bl_adamw_step.argtypes = [_P, _P, _P, _P, ctypes.POINTER(AdamWArgs), _P]
     lib.bl_adamw_get_moments.argtypes = [_P] * 5
     lib.bl_adamw_set_moments.argtypes = [_P] * 5
-    for name in ("bl_norm_plan_destroy", "bl_logprob_plan_destroy", "bl_adamw_plan_destroy"):
+    lib.bl_group_norm_plan_create.argtypes = [pp, ctypes.POINTER(GroupNormDesc)]
+    lib.bl_group_norm_workspace_size.argtypes = [_P, ctypes.POINTER(_S)]
+    lib.bl_group_norm_forward.argtypes = [_P] * 8
+    lib.bl_group_norm_backward.argtypes = [_P] * 11
+    lib.bl_recurrence_plan_create.argtypes = [pp, ctypes.POINTER(RecurrenceDesc)]
+    lib.bl_recurrence_workspace_size.argtypes = [_P, ctypes.POINTER(_S)]
+    lib.bl_recurrence_states_size.argtypes = [_P, ctypes.POINTER(_L)]
+    lib.bl_recurrence_forward.argtypes = [_P] * 10
+    lib.bl_recurrence_backward.argtypes = [_P] * 12
+    lib.bl_muon_plan_create.argtypes = [pp, ctypes.POINTER(MuonDesc)]
+    lib.bl_muon_state_size.argtypes = [_P, ctypes.POINTER(_S), ctypes.POINTER(_L), ctypes.POINTER(_L)]
+    lib.bl_muon_workspace_size.argtypes = [_P, ctypes.POINTER(_S)]
+    lib.bl_muon_step.argtypes = [_P, _P, _P, _P, _P, ctypes.POINTER(MuonArgs), _P]
+    lib.bl_muon_orthogonalize.argtypes = [_P, _P, _P, _P, _D, _P]
+    for name in ("bl_norm_plan_destroy", "bl_logprob_plan_destroy", "bl_adamw_plan_destroy",
+                 "bl_group_norm_plan_destroy", "bl_recurrence_plan_destroy", "bl_muon_plan_destroy"):
         getattr(lib, name).argtypes = [_P]
     for name in EXPORTED:
         getattr(lib, name)  # every declared symbol must be exported
@@ -220,6 +264,159 @@ class NormPlan(_Plan):
              self._w(dbias, "dbias", on), self._ws(ws, on), _stream(stream, on))
 
 
+class GroupNormPlan(_Plan):
+    """Group norm with an activation (None, "relu" or "silu") of [batch][sites][channels]
+    (channels_last) or [batch][channels][sites], the convolution layer's maps with
+    L or H * W sites.  Tensors may have any shape of that many elements.
+    ``x_stride`` and ``y_stride`` (elements between samples, 0: dense) are those of
+    x and dx, and of y and dy.
+    """
+
+    _destroy = "bl_group_norm_plan_destroy"
+    _acts = {None: BL_ACT_NONE, "none": BL_ACT_NONE, "relu": BL_ACT_RELU, "silu": BL_ACT_SILU}
+
+    def __init__(self, batch, sites, channels, groups, channels_last=False, act=None, dtype=None, wdtype=None, eps=1e-5,
+                 x_stride=0, y_stride=0):
+        self._lib = load()
+        if act not in self._acts:
+            raise ValueError(f"act must be None, 'relu' or 'silu', not {act!r}")
+        self.dtype = torch.float32 if dtype is None else dtype
+        self.wdtype = torch.float32 if wdtype is None else wdtype
+        d = GroupNormDesc(batch, sites, channels, groups, BL_CHANNELS_LAST if channels_last else BL_CHANNELS_FIRST,
+                          self._acts[act], _dtype_code(self.dtype, "dtype"), _dtype_code(self.wdtype, "wdtype"),
+                          float(eps), x_stride, y_stride)
+        self._h = _P()
+        _check("bl_group_norm_plan_create", self._lib.bl_group_norm_plan_create(ctypes.byref(self._h), ctypes.byref(d)))
+        self.batch, self.sites, self.channels, self.groups = batch, sites, channels, groups
+        self.x_stride, self.y_stride = x_stride or sites * channels, y_stride or sites * channels
+        n = _S()
+        _check("bl_group_norm_workspace_size", self._lib.bl_group_norm_workspace_size(self._h, ctypes.byref(n)))
+        self.workspace_bytes = n.value
+
+    def stats_shape(self):
+        return (2, self.batch, self.groups)
+
+    def _x(self, t, name, device):
+        return _sliced(t, self.dtype, self.batch, self.sites * self.channels, self.x_stride, name, device)
+
+    def _y(self, t, name, device):
+        return _sliced(t, self.dtype, self.batch, self.sites * self.channels, self.y_stride, name, device)
+
+    def _w(self, t, name, device):
+        return _flat(t, self.wdtype, self.channels, name, device)
+
+    def _stats(self, t, device):
+        return _flat(t, torch.float32, 2 * self.batch * self.groups, "stats", device)
+
+    def forward(self, x, weight, bias, y, stats, ws, stream=None):
+        """y, and mean and 1 / deviation of the groups in `stats` (None: not
+        wanted); weight None: 1, bias None: 0."""
+        on = _gpu(x, "x")
+        _run("bl_group_norm_forward", self._lib.bl_group_norm_forward, on,
+             self._h, self._x(x, "x", on), self._w(weight, "weight", on), self._w(bias, "bias", on),
+             self._y(y, "y", on), self._stats(stats, on), self._ws(ws, on), _stream(stream, on))
+
+    def backward(self, dy, x, weight, bias, stats, dx, dweight, dbias, ws, stream=None):
+        """dx, and the gradients of weight and bias (None: not wanted)."""
+        on = _gpu(x, "x")
+        _run("bl_group_norm_backward", self._lib.bl_group_norm_backward, on,
+             self._h, self._y(dy, "dy", on), self._x(x, "x", on), self._w(weight, "weight", on),
+             self._w(bias, "bias", on), self._stats(stats, on), self._x(dx, "dx", on),
+             self._w(dweight, "dweight", on), self._w(dbias, "dbias", on), self._ws(ws, on), _stream(stream, on))
+
+
+class RecurrencePlan(_Plan):
+    """h_t = a_t h_(t-1) + b_t along the middle axis of [outer][length][inner], with
+    a = sigmoid(gate), b = (1 - a) x (gate="sigmoid") or a = exp(gate), b = x
+    (gate="exp").
+
+    Tokens: ``RecurrencePlan(N, tokens, channels)``; the samples of the convolution
+    layer's maps: ``RecurrencePlan(N * C, L)``.  Tensors are [outer, length, inner],
+    or of any shape where they are contiguous and dense.  ``in_strides`` and
+    ``out_strides`` are the elements between two outer entries and two steps (0:
+    dense) of gate, x and their gradients, and of y and dy.
+    """
+
+    _destroy = "bl_recurrence_plan_destroy"
+    _gates = {"sigmoid": BL_GATE_SIGMOID, "exp": BL_GATE_EXP}
+
+    def __init__(self, outer, length, inner=1, gate="sigmoid", dtype=None, in_strides=(0, 0), out_strides=(0, 0)):
+        self._lib = load()
+        if gate not in self._gates:
+            raise ValueError(f"gate must be 'sigmoid' or 'exp', not {gate!r}")
+        self.dtype = torch.float32 if dtype is None else dtype
+        d = RecurrenceDesc(outer, length, inner, self._gates[gate], _dtype_code(self.dtype, "dtype"), *in_strides,
+                           *out_strides)
+        self._h = _P()
+        _check("bl_recurrence_plan_create", self._lib.bl_recurrence_plan_create(ctypes.byref(self._h), ctypes.byref(d)))
+        self.outer, self.length, self.inner = outer, length, inner
+
+        def strides(given):
+            step = given[1] or inner
+            return given[0] or length * step, step
+        self.in_strides, self.out_strides = strides(in_strides), strides(out_strides)
+        n, m = _S(), _L()
+        _check("bl_recurrence_workspace_size", self._lib.bl_recurrence_workspace_size(self._h, ctypes.byref(n)))
+        _check("bl_recurrence_states_size", self._lib.bl_recurrence_states_size(self._h, ctypes.byref(m)))
+        self.workspace_bytes, self.states_elements = n.value, m.value
+
+    def states(self, device="cuda"):
+        """What forward() leaves for backward()."""
+        return torch.empty(self.states_elements, device=device)
+
+    def _steps(self, t, strides, name, device):
+        if t.get_device() != device or t.dtype != self.dtype:
+            raise ValueError(f"{name} must be a {self.dtype} tensor on GPU {device}, as the others")
+        shape = (self.outer, self.length, self.inner)
+        if t.numel() != self.outer * self.length * self.inner:
+            raise ValueError(f"{name} has {t.numel()} elements, expected {self.outer * self.length * self.inner}")
+        if t.numel() == 0:
+            return t.data_ptr()
+        dense = strides == (self.length * self.inner, self.inner) or t.numel() == self.inner
+        if dense and t.is_contiguous():
+            return t.data_ptr()
+        if t.shape != shape or any(n > 1 and s != want for n, s, want in zip(shape, t.stride(), (*strides, 1))):
+            raise ValueError(f"{name} must be {shape} with strides {(*strides, 1)}, "
+                             f"not {tuple(t.shape)} with {t.stride()}")
+        return t.data_ptr()
+
+    def _in(self, t, name, device):
+        return self._steps(t, self.in_strides, name, device)
+
+    def _out(self, t, name, device):
+        return self._steps(t, self.out_strides, name, device)
+
+    def _state(self, t, name, device):
+        return _flat(t, torch.float32, self.outer * self.inner, name, device)
+
+    def _resets(self, t, device):
+        if t is not None and t.dtype == torch.bool:
+            t = t.view(torch.uint8)
+        return _flat(t, torch.uint8, self.outer * self.length, "resets", device)
+
+    def _saved(self, t, device):
+        return _flat(t, torch.float32, self.states_elements, "states", device)
+
+    def forward(self, gate, x, y, ws, h0=None, last=None, resets=None, states=None, stream=None):
+        """y = h of every step; `last`: the last one in float32; `states`: what
+        backward() needs (both None: not wanted); h0 None: 0.  resets: bytes or
+        truth values [outer][length], the steps at which the state is dropped."""
+        on = _gpu(x, "x")
+        _run("bl_recurrence_forward", self._lib.bl_recurrence_forward, on,
+             self._h, self._in(gate, "gate", on), self._in(x, "x", on), self._resets(resets, on),
+             self._state(h0, "h0", on), self._out(y, "y", on), self._state(last, "last", on),
+             self._saved(states, on), self._ws(ws, on), _stream(stream, on))
+
+    def backward(self, gate, x, dy, states, dgate, dx, ws, dlast=None, dh0=None, resets=None, stream=None):
+        """dgate, dx and dh0 (None: not wanted) from dy and dlast (None: 0)."""
+        on = _gpu(x, "x")
+        _run("bl_recurrence_backward", self._lib.bl_recurrence_backward, on,
+             self._h, self._in(gate, "gate", on), self._in(x, "x", on), self._resets(resets, on),
+             self._saved(states, on), self._out(dy, "dy", on), self._state(dlast, "dlast", on),
+             self._in(dgate, "dgate", on), self._in(dx, "dx", on), self._state(dh0, "dh0", on), self._ws(ws, on),
+             _stream(stream, on))
+
+
 class LogProbPlan(_Plan):
     """Log probabilities of given classes, entropies and the `top` likeliest
     classes of rows of logits, and the logits' gradient."""
@@ -259,8 +456,8 @@ class LogProbPlan(_Plan):
              _sliced(dlogits, self.dtype, n, self.classes, self.grad_stride, "dlogits", on), _stream(stream, on))
 
 
-class AdamWTensors:
-    """The parameters and gradients that an AdamW step goes over: the tensors,
+class StepTensors:
+    """The parameters and gradients that an optimiser's step goes over: the tensors,
     which it keeps alive, and the list of their addresses, taken once (a tensor
     that is given other storage has to be bound again)."""
 
@@ -275,6 +472,9 @@ class AdamWTensors:
                          for i, (t, n) in enumerate(zip(params, plan.sizes))])
         self._g = ptrs(*[_flat(t, plan.grad_dtype, n, f"gradient {i}", self.on)
                          for i, (t, n) in enumerate(zip(grads, plan.sizes))])
+
+
+AdamWTensors = StepTensors
 
 
 class AdamWPlan(_Plan):
@@ -313,7 +513,7 @@ class AdamWPlan(_Plan):
 
     def bind(self, params, grads):
         """The list of tensors that step() takes: contiguous, of the plan's sizes and types."""
-        return AdamWTensors(self, params, grads)
+        return StepTensors(self, params, grads)
 
     def step(self, tensors, state, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, step=1, grad_scale=None,
              seed=0, live=None, stream=None):
@@ -354,3 +554,83 @@ class AdamWPlan(_Plan):
         _run("bl_adamw_set_moments", self._lib.bl_adamw_set_moments, on, self._h, self._state(state),
              _flat(m, torch.float32, self.total, "m", on), _flat(v, torch.float32, self.total, "v", on),
              _stream(stream, on))
+
+
+class MuonPlan(_Plan):
+    """One step of the Muon optimiser over matrices of the given shapes (rows,
+    columns): momentum, orthogonalised by Newton-Schulz products.  `decay`: for each
+    matrix whether weight decay applies (None: to all); `scales`: its factor on the
+    learning rate (None: sqrt(max(1, rows / columns))); `coefficients`: (a, b, c) of
+    each product step (None: the usual ones, five times)."""
+
+    _destroy = "bl_muon_plan_destroy"
+
+    def __init__(self, shapes, param_dtype=None, grad_dtype=None, decay=None, scales=None, coefficients=None):
+        self._lib = load()
+        self.shapes = [(int(r), int(c)) for r, c in shapes]
+        self.sizes = [r * c for r, c in self.shapes]
+        self.param_dtype = torch.float32 if param_dtype is None else param_dtype
+        self.grad_dtype = torch.float32 if grad_dtype is None else grad_dtype
+        count = len(self.shapes)
+        for name, given in (("decay", decay), ("scales", scales)):
+            if given is not None and len(given) != count:
+                raise ValueError(f"{name} must have a value for each matrix")
+        flat = None if coefficients is None else [float(v) for step in coefficients for v in step]
+        if flat is not None and len(flat) != 3 * len(coefficients):
+            raise ValueError("coefficients must be three values for each step")
+        d = MuonDesc(count, (_L * count)(*[r for r, _ in self.shapes]), (_L * count)(*[c for _, c in self.shapes]),
+                     None if decay is None else (ctypes.c_ubyte * count)(*[bool(x) for x in decay]),
+                     None if scales is None else (_D * count)(*[float(x) for x in scales]),
+                     5 if flat is None else len(coefficients), None if flat is None else (_D * len(flat))(*flat),
+                     _dtype_code(self.param_dtype, "param_dtype"), _dtype_code(self.grad_dtype, "grad_dtype"))
+        self._h = _P()
+        _check("bl_muon_plan_create", self._lib.bl_muon_plan_create(ctypes.byref(self._h), ctypes.byref(d)))
+        n, total, start, m = _S(), _L(), (_L * count)(), _S()
+        _check("bl_muon_state_size", self._lib.bl_muon_state_size(self._h, ctypes.byref(n), ctypes.byref(total), start))
+        _check("bl_muon_workspace_size", self._lib.bl_muon_workspace_size(self._h, ctypes.byref(m)))
+        self.state_bytes, self.total, self.starts, self.workspace_bytes = n.value, total.value, list(start), m.value
+
+    def state(self, device="cuda"):
+        """A new state: momentum of zero."""
+        return torch.zeros(self.state_bytes, dtype=torch.uint8, device=device)
+
+    def _state(self, state):
+        if not state.is_contiguous() or state.nbytes != self.state_bytes:
+            raise ValueError("state must be a contiguous GPU tensor of state_bytes bytes")
+        return state.data_ptr()
+
+    def momentum(self, state):
+        """The momentum [total] as a view of the state, matrix i's at starts[i]."""
+        self._state(state)
+        return state.view(torch.float32)
+
+    def bind(self, params, grads):
+        """The list of matrices that step() and orthogonalize() take: contiguous, of the
+        plan's sizes and types."""
+        return StepTensors(self, params, grads)
+
+    def _bound(self, tensors):
+        if tensors.plan is not self:
+            raise ValueError("the matrices were bound to another plan")
+        return tensors.on
+
+    def step(self, tensors, state, ws, lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, eps=1e-7, step=1,
+             grad_scale=None, seed=0, live=None, stream=None):
+        """One step, in place.  `grad_scale`: a float32 GPU tensor of one element
+        that gradients are multiplied by.  `live`: a float64 GPU tensor (lr, step)
+        that is read in the place of those two when the kernels run."""
+        on = _gpu(state, "state")
+        if self._bound(tensors) not in (None, on):
+            raise ValueError("the state and the matrices must be on one GPU")
+        a = MuonArgs(lr, momentum, eps, weight_decay, bool(nesterov), step, seed & 0xFFFFFFFF,
+                     _flat(grad_scale, torch.float32, 1, "grad_scale", on), _flat(live, torch.float64, 2, "live", on))
+        _run("bl_muon_step", self._lib.bl_muon_step, on, self._h, tensors._p, tensors._g, self._state(state),
+             self._ws(ws, on), ctypes.byref(a), _stream(stream, on))
+
+    def orthogonalize(self, tensors, ws, eps=1e-7, stream=None):
+        """The orthogonalised gradients, in the place of the parameters of bind()."""
+        on = self._bound(tensors)
+        if on is None:
+            return
+        _run("bl_muon_orthogonalize", self._lib.bl_muon_orthogonalize, on, self._h, tensors._p, tensors._g,
+             self._ws(ws, on), eps, _stream(stream, on))

@@ -1,0 +1,104 @@
+// Group norm with an activation: plan, arguments and what both layouts share (gnorm.hip:
+// plan, dispatch and the sums that need no values; gnorm_last.hip, gnorm_first.hip: the layouts).
+#pragma once
+
+#include "ops.hpp"
+
+struct bl_group_norm_plan_s {
+  bl_group_norm_desc_t d;
+  long each;       // channels of a group
+  int vec;         // channels last: values of an access, a divisor of channels
+  int lanes;       // channels last: accesses of a site that a block takes; first: lanes of a channel's sites
+  int tiles;       // channels last: blocks along channels
+  long chunk;      // sites of a block
+  int chunks;      // of them
+  size_t off_part, off_sums, off_own, bytes;
+};
+
+namespace blc {
+
+struct GroupNormArgs {
+  const void *x, *dy, *w, *b;
+  void *y, *dx, *dw, *db;
+  float* stats;  // [2][batch][groups] mean, rstd
+  float* part;   // [batch][chunks][channels][2]: forward mean and squares, backward sums of dz and dz h
+  float* sums;   // backward [batch][groups][2]: means of u and of u h
+  float* own;    // backward [batch][channels][2]: part, summed over a sample
+  long batch, sites, channels, groups, each;
+  long x_stride, y_stride;
+  long chunk;
+  int chunks, lanes, tiles;
+  bool wide;     // w, b, dw and db in fp32
+  float eps;
+};
+
+// z of the definition.  Both directions take it from here, so that the backward call
+// finds max(z, 0) where the forward call left it.
+__device__ __forceinline__ float norm_z(float x, float mean, float rstd, float w, float b) {
+  return fmaf((x - mean) * rstd, w, b);
+}
+__device__ __forceinline__ float logistic(float z) { return 1.f / (1.f + expf(-z)); }
+template <int ACT>
+__device__ __forceinline__ float act_of(float z) {
+  if (ACT == BL_ACT_RELU) return z > 0.f ? z : z != z ? z : 0.f;
+  if (ACT == BL_ACT_SILU) return z * logistic(z);
+  return z;
+}
+// dy act'(z)
+template <int ACT>
+__device__ __forceinline__ float act_grad(float z, float dy) {
+  if (ACT == BL_ACT_RELU) return z > 0.f ? dy : z != z ? z : 0.f;
+  if (ACT == BL_ACT_SILU) {
+    const float q = logistic(z);
+    return dy * fmaf(z * q, 1.f - q, q);
+  }
+  return dy;
+}
+
+// dx.  Every operation rounds by itself (as in the groups' means): of a group of one
+// value u is its mean, and the gradient is 0 and not a rounding of u times rstd.
+__device__ __forceinline__ float norm_grad(float dz, float w, float c1, float h, float c2, float rstd) {
+#pragma clang fp contract(off)
+  const float u = dz * w;
+  return rstd * ((u - c1) - h * c2);
+}
+
+// A weight at c (NULL: `one`).
+template <typename T>
+__device__ __forceinline__ float weight_at(const void* w, bool wide, long c, float one) {
+  return !w ? one : wide ? static_cast<const float*>(w)[c] : to_f32(static_cast<const T*>(w)[c]);
+}
+
+// Mean and sum of squares about it, of values that come in tiles: each tile's own are
+// taken in registers and joined (Chan, Golub and LeVeque, "Updating formulae and a
+// pairwise algorithm for computing sample variances", 1979), so that no square of a
+// value far from 0 is summed.
+struct Moments {
+  float n, mean, m2;
+};
+__device__ __forceinline__ void moments_join(Moments& a, const Moments& b) {
+  const float n = a.n + b.n, d = b.mean - a.mean, share = n > 0.f ? b.n / n : 0.f;
+  a.mean = fmaf(d, share, a.mean);
+  a.m2 += fmaf(d * d, a.n * share, b.m2);
+  a.n = n;
+}
+
+bl_status_t gnorm_last_forward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
+bl_status_t gnorm_last_backward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
+bl_status_t gnorm_first_forward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
+bl_status_t gnorm_first_backward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
+// Statistics from the parts; backward: means over groups and sums over samples from theirs.
+bl_status_t gnorm_join_forward(const GroupNormArgs& a, hipStream_t s);
+bl_status_t gnorm_join_backward(const GroupNormArgs& a, int dtype, hipStream_t s);
+// dw and db from the samples' sums (batch = 0: zeros).
+bl_status_t gnorm_weights(const GroupNormArgs& a, int dtype, hipStream_t s);
+
+// go(act) as a constant.
+template <typename Go>
+void with_act(int act, Go&& go) {
+  if (act == BL_ACT_RELU) go(std::integral_constant<int, BL_ACT_RELU>());
+  else if (act == BL_ACT_SILU) go(std::integral_constant<int, BL_ACT_SILU>());
+  else go(std::integral_constant<int, BL_ACT_NONE>());
+}
+
+}  // namespace blc

@@ -1,0 +1,133 @@
+// Orthogonalised update: plan and launch arguments (muon.hip: plan, momentum, norms and
+// dispatch; muon_gemm.hip: the Newton-Schulz products).
+#pragma once
+
+#include <vector>
+
+#include "ops.hpp"
+
+namespace blc {
+
+constexpr int kMuonList = 64;   // matrices of a launch: their list is part of the kernel's arguments
+constexpr int kMuonTile = 128;  // rows and columns of a product's tile: matrices are padded to it with zeros
+constexpr int kMuonSlab = 4096; // elements of a block that takes squares
+constexpr int kMuonSteps = 16;
+constexpr size_t kMuonBytes = 1ull << 36; // of a launch's matrices, which keeps its blocks far below 2^24
+
+// A matrix of a launch.  m and n: its shorter and longer side in tiles; `tall`: it has
+// more rows than columns and is taken by its transpose.
+struct MuonItem {
+  void* p;
+  const void* g;
+  long long start;  // in the momentum's layout
+  int rows, cols;
+  float scale;
+  unsigned off;     // of its part of the workspace, in 256 bytes
+  unsigned short m, n, tall, decay;
+};
+
+struct MuonList {
+  int count;
+  unsigned first[kMuonList + 1];  // blocks before each matrix's (all ones past the last)
+  MuonItem item[kMuonList];
+};
+
+// What the products alone need.
+struct MuonShapes {
+  int count;
+  unsigned first[kMuonList + 1];
+  unsigned off[kMuonList];
+  unsigned short m[kMuonList], n[kMuonList];
+};
+
+struct MuonArgs {
+  char* ws;        // matrices' parts
+  double* squares; // a sum of squares for each slab
+  float* momentum; // null: u is the gradient
+  const float* grad_scale;
+  const double* live;
+  double lr, wd, eps;
+  float beta;
+  int nesterov, set;  // set: the result is the parameter
+  unsigned key, seed;
+};
+
+// One product of a Newton-Schulz step: powers of two that its operands hold and its result
+// is stored with, and the step's coefficients.
+struct MuonProduct {
+  char* ws;
+  float scale;    // of the accumulated sum
+  float a, b, c;  // (poly: of I, A, A A, with the powers of two)
+  int turn;       // which of the two transposes is read
+};
+
+}  // namespace blc
+
+struct bl_muon_plan_s {
+  struct Matrix {
+    long long rows, cols, start;
+    double scale;
+    unsigned char decay;
+  };
+  struct Step {
+    double a, b, c;
+    float scale_b;  // power of two that B is stored with
+  };
+  // Matrices that are taken together, by their numbers.
+  struct Batch {
+    std::vector<int> of;
+    std::vector<unsigned> off;
+    size_t bytes;
+    long slabs;
+  };
+  std::vector<Matrix> matrices;
+  std::vector<Step> steps;
+  std::vector<Batch> batches;
+  int param_dtype, grad_dtype;
+  long long total;
+  size_t bytes, off_squares;
+};
+
+namespace blc {
+
+// Values are held as two fp16 parts, high and low, 32 of a row's high parts and then their
+// low ones side by side.  X is held times 2^15 (no singular value of it is above 1.75),
+// A = X X^T times 2^14.
+constexpr float kHoldX = 32768.f, kHoldA = 16384.f;
+
+// Byte offsets in a matrix's part: X [m][n], its transpose twice, A and B [m][m].
+struct MuonPlaces {
+  size_t x, t0, t1, a, b, bytes;
+  __host__ __device__ size_t t(int turn) const { return turn ? t1 : t0; }
+};
+__host__ __device__ inline MuonPlaces muon_places(unsigned m, unsigned n) {
+  const size_t tile = (size_t)kMuonTile * kMuonTile * 4, mn = (size_t)m * n * tile, mm = (size_t)m * m * tile;
+  return MuonPlaces{0, mn, 2 * mn, 3 * mn, 3 * mn + mm, 3 * mn + 2 * mm};
+}
+
+__device__ __forceinline__ unsigned muon_find(const unsigned* first, int count, unsigned block) {
+  int lo = 0, hi = count;  // first[lo] <= block < first[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (first[mid] <= block) lo = mid;
+    else hi = mid;
+  }
+  return (unsigned)lo;
+}
+
+// 16 bits that round a bfloat16 parameter, from the element's place (the AdamW step's hash).
+__device__ __forceinline__ unsigned muon_dither(unsigned long long place, unsigned key) {
+  unsigned x = (unsigned)place * 0x9E3779B9u + key;
+  x = (x ^ (x >> 15)) * 0xBB67AE85u;
+  x ^= x >> 16;
+  return (x * 0x6A09E667u) >> 16;
+}
+
+enum MuonMode { kGram, kPoly, kApply };
+bl_status_t muon_product(int mode, const MuonShapes& shapes, unsigned blocks, double flops, const MuonProduct& q,
+                         hipStream_t s);
+// The last step's product, and the parameters' update from its tiles.
+bl_status_t muon_update(int param_dtype, const MuonList& list, unsigned blocks, double flops, const MuonProduct& q,
+                        const MuonArgs& a, hipStream_t s);
+
+}  // namespace blc

@@ -1,0 +1,385 @@
+// Gated linear recurrence h_t = a_t h_(t-1) + b_t: plan, dispatch and the forward pass.
+//
+// A stretch of steps takes the state h to A h + B with A the product of its a and B the
+// sum of its b, each times the a behind it; two stretches join to one, (A2 A1, A2 B1 + B2).
+// So a block reads a tile of steps once, every thread joins its own few steps, the
+// stretches before a thread's are joined over lanes and waves, and each thread then goes
+// through its steps again in registers.  Bound by HBM: gate and x are read once, y is
+// written once.
+#include <algorithm>
+#include <new>
+
+#include "recur.hpp"
+
+namespace blc {
+namespace {
+
+template <typename T, int GATE, int LAYOUT, int WAVES, bool RESETS>
+__global__ __launch_bounds__(WAVES* kWave) void k_recur_fwd(RecurArgs r) {
+  using S = RecurShape<T, LAYOUT>;
+  constexpr int N = S::kVec, EACH = recur_each<T, LAYOUT, false>(), TILE = S::kSlices * WAVES * EACH;
+  __shared__ float sa[2][WAVES][S::kLanes][N], sb[2][WAVES][S::kLanes][N];
+  __shared__ int sd[2][WAVES];
+  const RecurPlace<T, LAYOUT, WAVES> p(r);
+  const long chunk = blockIdx.y, begin = chunk * r.chunk, end = min(r.length, begin + r.chunk);
+  const long sites = r.outer * r.inner, at = p.o * r.inner + p.i;
+  const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer + p.i;
+  const T* x = static_cast<const T*>(r.x) + p.o * r.in_outer + p.i;
+  T* y = static_cast<T*>(r.y) + p.o * r.out_outer + p.i;
+  const unsigned char* resets = RESETS ? r.resets + p.o * r.length : nullptr;
+  float h[N];  // before the tile
+  if (gridDim.y > 1) {
+    state_at<N, RESETS>(r, p.o, p.i, p.n, 0, 1, chunk, h);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) h[j] = r.h0 && j < p.n ? r.h0[at + j] : 0.f;
+  }
+  const long mine = begin + p.slice * EACH;  // this thread's steps of the first tile
+  RecurRaw<T, LAYOUT, EACH> g, v;
+  g.load(gate + mine * r.in_step, r.in_step, end - mine, p.n);
+  v.load(x + mine * r.in_step, r.in_step, end - mine, p.n);
+  unsigned bits = reset_bits<EACH, RESETS>(resets + mine, end - mine);
+  int turn = 0;
+  for (long t = mine; t - mine + begin < end; t += TILE, turn ^= 1) {
+    const long there = end - t;
+    float a[EACH][N], b[EACH][N];
+    Stretch<N> own = stretch_none<N>();
+    g.refresh();
+    v.refresh();
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        float rest;
+        gate_of<GATE>(g.at(k, j), a[k][j], rest);
+        b[k][j] = rest * v.at(k, j);
+        if (k >= there) a[k][j] = 1.f, b[k][j] = 0.f;
+        const bool drop = RESETS && (bits >> k & 1);
+        own.b[j] = drop ? b[k][j] : fmaf(a[k][j], own.b[j], b[k][j]);
+        own.a[j] *= a[k][j];
+      }
+    }
+    own.drop = RESETS && bits;
+    const unsigned now = bits;
+    // the next tile's loads are in flight while this one's state is found
+    g.load(gate + (t + TILE) * r.in_step, r.in_step, there - TILE, p.n);
+    v.load(x + (t + TILE) * r.in_step, r.in_step, there - TILE, p.n);
+    bits = reset_bits<EACH, RESETS>(resets + t + TILE, there - TILE);
+    Stretch<N> all;
+    const Stretch<N> before = wave_others<N, S::kLanes, RESETS, true>(own, all);
+    float s[N];  // this thread's state
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[j] = h[j];
+    if constexpr (WAVES == 1) {
+      stretch_apply<N, RESETS>(all, h);
+    } else {
+      if (p.lane < S::kLanes) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) sa[turn][p.wave][p.lane][j] = all.a[j], sb[turn][p.wave][p.lane][j] = all.b[j];
+        if (p.lane == 0) sd[turn][p.wave] = all.drop;
+      }
+      __syncthreads();  // (the other half is written before the next one)
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        Stretch<N> o;
+#pragma unroll
+        for (int j = 0; j < N; ++j) o.a[j] = sa[turn][w][p.lane % S::kLanes][j], o.b[j] = sb[turn][w][p.lane % S::kLanes][j];
+        o.drop = RESETS && sd[turn][w];
+        if (w == p.wave)
+#pragma unroll
+          for (int j = 0; j < N; ++j) s[j] = h[j];
+        stretch_apply<N, RESETS>(o, h);
+      }
+    }
+    stretch_apply<N, RESETS>(before, s);
+    if (r.states && there > 0 && t % r.every == 0) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < p.n) r.states[t / r.every * sites + at + j] = s[j];
+    }
+    RecurOut<T, LAYOUT, EACH> out;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        s[j] = RESETS && (now >> k & 1) ? b[k][j] : fmaf(a[k][j], s[j], b[k][j]);
+        out.set(k, j, s[j]);
+      }
+    out.store(y + t * r.out_step, r.out_step, there, p.n);
+  }
+  if (r.last && end == r.length && p.slice == 0) {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < p.n) r.last[at + j] = h[j];
+  }
+}
+
+template <typename T, int GATE, int LAYOUT, bool RESETS>
+__global__ __launch_bounds__(8 * kWave) void k_recur_fwd_part(RecurArgs r) {
+  using S = RecurShape<T, LAYOUT>;
+  constexpr int N = S::kVec, EACH = recur_each<T, LAYOUT, false>(), SLICES = S::kSlices * 8;
+  const RecurPlace<T, LAYOUT, 8> p(r);
+  const long chunk = blockIdx.y, stretch = r.chunk / SLICES;  // (a multiple of EACH)
+  const long begin = chunk * r.chunk + p.slice * stretch, end = min(r.length, begin + stretch);
+  const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer + p.i;
+  const T* x = static_cast<const T*>(r.x) + p.o * r.in_outer + p.i;
+  Stretch<N> own = stretch_none<N>();
+  for (long t = begin; t < end; t += EACH) {
+    RecurRaw<T, LAYOUT, EACH> g, v;
+    g.load(gate + t * r.in_step, r.in_step, end - t, p.n);
+    v.load(x + t * r.in_step, r.in_step, end - t, p.n);
+    const unsigned bits = reset_bits<EACH, RESETS>(RESETS ? r.resets + p.o * r.length + t : nullptr, end - t);
+    g.refresh();
+    v.refresh();
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+      if (k < end - t) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          float a, rest;
+          gate_of<GATE>(g.at(k, j), a, rest);
+          const float b = rest * v.at(k, j);
+          own.b[j] = RESETS && (bits >> k & 1) ? b : fmaf(a, own.b[j], b);
+          own.a[j] *= a;
+        }
+      }
+    own.drop |= RESETS && bits;
+  }
+  chunk_part<N, S::kLanes, 8, RESETS, true>(r, p, own, chunk, r.h0, chunk == 0);
+}
+
+// Few steps of many channels: a thread walks all of its channels' steps.
+template <typename T, int GATE, bool RESETS>
+__global__ __launch_bounds__(kThreads) void k_recur_serial(RecurArgs r, int vec_per) {
+  constexpr int N = 8 / (int)sizeof(T);
+  const long q = (long)blockIdx.x * kThreads + threadIdx.x, o = q / vec_per, i = (q - o * vec_per) * N, n = r.inner - i;
+  if (o >= r.outer) return;
+  const long sites = r.outer * r.inner, at = o * r.inner + i;
+  const T* gate = static_cast<const T*>(r.gate) + o * r.in_outer + i;
+  const T* x = static_cast<const T*>(r.x) + o * r.in_outer + i;
+  T* y = static_cast<T*>(r.y) + o * r.out_outer + i;
+  float h[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) h[j] = r.h0 && j < n ? r.h0[at + j] : 0.f;
+  for (long t = 0; t < r.length; ++t) {
+    Held<T, N> g, v;
+    g.load(gate + t * r.in_step, n);
+    v.load(x + t * r.in_step, n);
+    const bool drop = RESETS && r.resets[o * r.length + t];
+    if (r.states && t % r.every == 0) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (j < n) r.states[t / r.every * sites + at + j] = h[j];
+    }
+    g.refresh();
+    v.refresh();
+    Pack<T, N> out;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      float a, rest;
+      gate_of<GATE>(g[j], a, rest);
+      h[j] = drop ? rest * v[j] : fmaf(a, h[j], rest * v[j]);
+      out.v[j] = (T)h[j];
+    }
+    store_part(y + t * r.out_step, n, out);
+  }
+  if (r.last) {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < n) r.last[at + j] = h[j];
+  }
+}
+
+// A state of no steps: the one from outside.
+__global__ void k_recur_none(const float* from, float* to, long n) {
+  const long i = (long)blockIdx.x * kThreads + threadIdx.x;
+  if (i < n) to[i] = from ? from[i] : 0.f;
+}
+
+// Up to this many steps a thread walks them alone.
+constexpr long kSerialSteps = 8;
+
+long blocks_of(const bl_recurrence_desc_t& d, int layout) {
+  const long lanes = layout == kWide ? 16 * (8 / dtype_bytes(d.dtype)) : layout == kNarrow ? 4 : 1;
+  return d.outer * ((d.inner + lanes - 1) / lanes);
+}
+
+template <typename T>
+bl_status_t forward(const bl_recurrence_plan_s* p, RecurArgs r, hipStream_t s) {
+  const bl_recurrence_desc_t& d = p->d;
+  const double bytes = 3.0 * d.outer * d.length * d.inner * sizeof(T);
+  if (d.length <= kSerialSteps) {
+    constexpr int N = 8 / (int)sizeof(T);
+    const int per = (int)((d.inner + N - 1) / N);
+    const dim3 grid((unsigned)((d.outer * per + kThreads - 1) / kThreads));
+    return timed_launch("recur_fwd", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+      recur_dispatch(d.gate, kWide, 1, r.resets, [&](auto g, auto, auto, auto z) {
+        hipExtLaunchKernelGGL((k_recur_serial<T, decltype(g)::value, decltype(z)::value>), grid, dim3(kThreads), 0, s,
+                              e0, e1, 0, r, per);
+      });
+    });
+  }
+  const dim3 grid((unsigned)blocks_of(d, p->layout), (unsigned)p->chunks[0]);
+  r.chunk = p->chunk[0];
+  if (p->chunks[0] > 1) {
+    const bl_status_t st = timed_launch("recur_fwd_part", bytes * 2 / 3, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+      recur_dispatch(d.gate, p->layout, 8, r.resets, [&](auto g, auto l, auto, auto z) {
+        hipExtLaunchKernelGGL((k_recur_fwd_part<T, decltype(g)::value, decltype(l)::value, decltype(z)::value>), grid,
+                              dim3(8 * kWave), 0, s, e0, e1, 0, r);
+      });
+    });
+    if (st != BL_OK) return st;
+  }
+  return timed_launch("recur_fwd", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    recur_dispatch(d.gate, p->layout, p->waves[0], r.resets, [&](auto g, auto l, auto w, auto z) {
+      hipExtLaunchKernelGGL((k_recur_fwd<T, decltype(g)::value, decltype(l)::value, decltype(w)::value, decltype(z)::value>),
+                            grid, dim3(decltype(w)::value * kWave), 0, s, e0, e1, 0, r);
+    });
+  });
+}
+
+RecurArgs args_of(const bl_recurrence_plan_s* p, void* ws) {
+  RecurArgs r{};
+  const bl_recurrence_desc_t& d = p->d;
+  r.outer = d.outer;
+  r.length = d.length;
+  r.inner = d.inner;
+  r.in_outer = d.in_outer;
+  r.in_step = d.in_step;
+  r.out_outer = d.out_outer;
+  r.out_step = d.out_step;
+  r.every = p->every;
+  const long parts = std::max(p->chunks[0], p->chunks[1]) + 1, sites = d.outer * d.inner;
+  r.part_a = static_cast<float*>(ws);
+  r.part_b = r.part_a + parts * sites;
+  r.part_drop = reinterpret_cast<unsigned char*>(r.part_b + parts * sites);
+  return r;
+}
+
+}  // namespace
+
+bl_status_t recur_none(const float* from, float* to, long n, hipStream_t s) {
+  if (!to) return BL_OK;
+  return timed_launch("recur_none", 8.0 * n, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    hipExtLaunchKernelGGL(k_recur_none, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, e0, e1, 0,
+                          from, to, n);
+  });
+}
+
+}  // namespace blc
+
+using namespace blc;
+
+extern "C" bl_status_t bl_recurrence_plan_create(bl_recurrence_plan_t* out, const bl_recurrence_desc_t* desc) {
+  if (!out || !desc) return BL_ERR_INVALID_ARG;
+  *out = nullptr;
+  bl_recurrence_desc_t d = *desc;
+  if (d.outer < 0 || d.length < 0 || d.inner < 1 || !known_dtype(d.dtype)) return BL_ERR_INVALID_ARG;
+  if (d.gate != BL_GATE_SIGMOID && d.gate != BL_GATE_EXP) return BL_ERR_INVALID_ARG;
+  if (d.in_outer < 0 || d.in_step < 0 || d.out_outer < 0 || d.out_step < 0) return BL_ERR_INVALID_ARG;
+  const long long most = (1LL << 31) - 1;
+  if (d.outer > most || d.inner > most || d.length > most || d.outer * d.inner > most) return BL_ERR_UNSUPPORTED;
+  if (!d.in_step) d.in_step = d.inner;
+  if (!d.out_step) d.out_step = d.inner;
+  // (no offset of an element may leave 62 bits)
+  const __int128 bound = (__int128)1 << 60;
+  if ((__int128)d.in_step * d.length > bound || (__int128)d.out_step * d.length > bound) return BL_ERR_UNSUPPORTED;
+  if (!d.in_outer) d.in_outer = d.length * d.in_step;
+  if (!d.out_outer) d.out_outer = d.length * d.out_step;
+  if ((__int128)d.in_outer * d.outer > bound || (__int128)d.out_outer * d.outer > bound) return BL_ERR_UNSUPPORTED;
+  // steps and sequences may interleave, but no two elements may share a place: the
+  // larger of two strides spans what the smaller one covers
+  auto apart = [&](long long step, long long per) {
+    if (d.length > 1 && step < d.inner) return false;
+    if (d.outer <= 1 || !d.length) return true;
+    return per >= step ? per >= (d.length - 1) * step + d.inner
+                       : per >= d.inner && (d.length <= 1 || step >= (d.outer - 1) * per + d.inner);
+  };
+  if (!apart(d.in_step, d.in_outer) || !apart(d.out_step, d.out_outer)) return BL_ERR_INVALID_ARG;
+  bl_recurrence_plan_s* p = new (std::nothrow) bl_recurrence_plan_s{};
+  if (!p) return BL_ERR_OOM;
+  p->d = d;
+  const bool row = d.inner == 1 && d.in_step == 1 && d.out_step == 1;
+  p->layout = row ? kRow : d.inner <= 4 ? kNarrow : kWide;
+  const long slices = row ? kWave : p->layout == kNarrow ? 16 : 4, blocks = std::max(blocks_of(d, p->layout), 1L);
+  const long each[2] = {row ? 16 / dtype_bytes(d.dtype) : 8, row ? 16 / dtype_bytes(d.dtype) : 4};
+  for (int i = 0; i < 2; ++i) {
+    const long tile = slices * each[i];  // of one wave
+    // one wave a block: rows in such a number that they fill the GPU, or sequences of one tile
+    p->waves[i] = p->layout != kNarrow && (d.length <= tile || (row && blocks >= 2048)) ? 1 : 8;
+    // as many chunks as bring 512 blocks onto the GPU, each of four tiles at least
+    const long part = 8 * tile;
+    const long want = p->waves[i] == 1 ? 1 : std::max(1L, std::min<long>(512 / blocks, d.length / (4 * part)));
+    p->chunk[i] = want > 1 ? ((d.length + want - 1) / want + part - 1) / part * part : std::max<long>(d.length, 1);
+    p->chunks[i] = want > 1 ? (d.length + p->chunk[i] - 1) / p->chunk[i] : 1;
+  }
+  // a state at every tile of the backward pass
+  p->every = slices * each[1] * p->waves[1];
+  const size_t parts = std::max(p->chunks[0], p->chunks[1]);
+  p->bytes = parts > 1 ? (parts + 1) * ((size_t)d.outer * d.inner * 8 + d.outer) : 0;
+  *out = p;
+  return BL_OK;
+}
+
+extern "C" bl_status_t bl_recurrence_plan_destroy(bl_recurrence_plan_t p) {
+  if (!p) return BL_ERR_INVALID_ARG;
+  delete p;
+  return BL_OK;
+}
+
+extern "C" bl_status_t bl_recurrence_workspace_size(bl_recurrence_plan_t p, size_t* bytes) {
+  if (!p || !bytes) return BL_ERR_INVALID_ARG;
+  *bytes = p->bytes;
+  return BL_OK;
+}
+
+extern "C" bl_status_t bl_recurrence_states_size(bl_recurrence_plan_t p, long long* elements) {
+  if (!p || !elements) return BL_ERR_INVALID_ARG;
+  *elements = (p->d.length + p->every - 1) / p->every * p->d.outer * p->d.inner;
+  return BL_OK;
+}
+
+extern "C" bl_status_t bl_recurrence_forward(bl_recurrence_plan_t p, const void* gate, const void* x,
+                                             const unsigned char* resets, const float* h0, void* y, float* last,
+                                             float* states, void* ws, void* stream) {
+  if (!p) return BL_ERR_INVALID_ARG;
+  const bl_recurrence_desc_t& d = p->d;
+  if (!d.outer) return BL_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!d.length) return recur_none(h0, last, d.outer * d.inner, s);
+  if (!gate || !x || !y || (p->bytes && (!ws || !aligned(ws)))) return BL_ERR_INVALID_ARG;
+  RecurArgs r = args_of(p, ws);
+  r.gate = gate;
+  r.x = x;
+  r.resets = resets;
+  r.h0 = h0;
+  r.y = y;
+  r.last = last;
+  r.states = states;
+  if (d.dtype == BL_F32) return forward<float>(p, r, s);
+  if (d.dtype == BL_BF16) return forward<bf16_t>(p, r, s);
+  return forward<f16_t>(p, r, s);
+}
+
+extern "C" bl_status_t bl_recurrence_backward(bl_recurrence_plan_t p, const void* gate, const void* x,
+                                              const unsigned char* resets, const float* states, const void* dy,
+                                              const float* dlast, void* dgate, void* dx, float* dh0, void* ws,
+                                              void* stream) {
+  if (!p) return BL_ERR_INVALID_ARG;
+  const bl_recurrence_desc_t& d = p->d;
+  if (!d.outer) return BL_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!d.length) return recur_none(dlast, dh0, d.outer * d.inner, s);
+  if (!gate || !x || !states || !dy || !dgate || !dx || (p->bytes && (!ws || !aligned(ws)))) return BL_ERR_INVALID_ARG;
+  RecurArgs r = args_of(p, ws);
+  r.gate = gate;
+  r.x = x;
+  r.resets = resets;
+  r.states = const_cast<float*>(states);
+  r.dy = dy;
+  r.dlast = dlast;
+  r.dgate = dgate;
+  r.dx = dx;
+  r.dh0 = dh0;
+  return recur_backward(p, r, s);
+}
