@@ -313,6 +313,10 @@ extern "C" bl_status_t bl_recurrence_plan_create(bl_recurrence_plan_t* out, cons
     p->chunk[i] = want > 1 ? ((d.length + want - 1) / want + part - 1) / part * part : std::max<long>(d.length, 1);
     p->chunks[i] = want > 1 ? (d.length + p->chunk[i] - 1) / p->chunk[i] : 1;
   }
+  if (blocks >= (1LL << 32) / kWave / std::max(p->waves[0], p->waves[1])) {  // (a launch has fewer threads)
+    delete p;
+    return BL_ERR_UNSUPPORTED;
+  }
   // a state at every tile of the backward pass
   p->every = slices * each[1] * p->waves[1];
   const size_t parts = std::max(p->chunks[0], p->chunks[1]);
