@@ -14,93 +14,125 @@
 namespace blc {
 namespace {
 
-// u of element e (of a matrix whose momentum lies at m, or null).
-template <typename G>
-__device__ __forceinline__ float update_of(const G* g, const float* m, size_t e, float gs, const MuonArgs& a) {
-  const float v = gs * to_f32(g[e]);
-  if (!m) return v;
-  return a.nesterov ? fmaf(a.beta, m[e], v) : m[e];
+// u of four elements from their gradients and (new) momenta.
+__device__ __forceinline__ float update_of(float g, float m, float gs, const MuonArgs& a) {
+  return !a.momentum ? gs * g : a.nesterov ? fmaf(a.beta, m, gs * g) : m;
+}
+
+// Sum over a block, in each thread.
+__device__ __forceinline__ double block_sum(double sum, double (&red)[kThreads / kWave]) {
+  for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
+  if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = sum;
+  __syncthreads();
+  sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < kThreads / kWave; ++w) sum += red[w];
+  return sum;
 }
 
 // The new momentum of a slab, and the sum of its u's squares in double precision (which
-// holds the squares of all fp32 values).
+// holds the squares of all fp32 values).  A thread's loads are all in flight together.
 template <typename G>
 __global__ __launch_bounds__(kThreads) void k_muon_momentum(MuonList list, MuonArgs a) {
+  constexpr int kEach = kMuonSlab / kThreads / 4;
   __shared__ double red[kThreads / kWave];
   const unsigned at = muon_find(list.first, list.count, blockIdx.x);
   const MuonItem& it = list.item[at];
-  const size_t size = (size_t)it.rows * it.cols, from = (size_t)(blockIdx.x - list.first[at]) * kMuonSlab;
-  const size_t end = min(size, from + kMuonSlab);
-  const G* g = static_cast<const G*>(it.g);
-  float* m = a.momentum ? a.momentum + it.start : nullptr;
+  const long size = (long)it.rows * it.cols, from = (long)(blockIdx.x - list.first[at]) * kMuonSlab + threadIdx.x * 4;
+  const G* g = static_cast<const G*>(it.g) + from;
+  float* m = a.momentum ? a.momentum + it.start + from : nullptr;
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
-  double sum = 0.0;
-  for (size_t e = from + threadIdx.x; e < end; e += kThreads) {
-    if (m) m[e] = fmaf(a.beta, m[e], gs * to_f32(g[e]));
-    const double u = update_of(g, m, e, gs, a);
-    sum += u * u;
+  Held<G, 4> gv[kEach];
+  Held<float, 4> mv[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    gv[k].load(g + k * kThreads * 4, size - from - k * kThreads * 4);
+    mv[k].load(m + k * kThreads * 4, m ? size - from - k * kThreads * 4 : 0);
   }
-  for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
-  if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = sum;
-  __syncthreads();
-  if (threadIdx.x) return;
-  sum = 0.0;
-  for (int w = 0; w < kThreads / kWave; ++w) sum += red[w];
-  a.squares[blockIdx.x] = sum;
+  double sum = 0.0;
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    gv[k].refresh();
+    mv[k].refresh();
+    Pack<float, 4> next;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      next.v[j] = fmaf(a.beta, mv[k][j], gs * gv[k][j]);
+      const double u = update_of(gv[k][j], next.v[j], gs, a);  // (0 where there is none)
+      sum = fma(u, u, sum);
+    }
+    if (m) store_part(m + k * kThreads * 4, size - from - k * kThreads * 4, next);
+  }
+  sum = block_sum(sum, red);
+  if (threadIdx.x == 0) a.squares[blockIdx.x] = sum;
 }
 
-// X and its transpose: a block takes 32 x 32 elements.  `slab`: first slab of each matrix.
+// X and its transpose: a block takes 64 x 64 elements of a matrix as it lies in memory.
 struct MuonSlabs {
-  unsigned first[kMuonList + 1];
+  unsigned first[kMuonList + 1];  // first slab of each matrix
 };
-constexpr int kLay = 32;
+constexpr int kLayRow = kMuonPad + 1;
+// Eight values of the tile, `step` apart, as high and low parts of a row of the layout.
+__device__ __forceinline__ void lay_eight(const float* v, int step, char* row, int c) {
+  Pack<f16_t, 8> hi, lo;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float x = v[j * step];
+    hi.v[j] = (f16_t)x;
+    lo.v[j] = (f16_t)(x - (float)hi.v[j]);
+  }
+  f16_t* to = reinterpret_cast<f16_t*>(row + c / 32 * 128 + c % 32 * 2);
+  store_pack(to, hi);
+  store_pack(to + 32, lo);
+}
 template <typename G>
 __global__ __launch_bounds__(kThreads) void k_muon_lay(MuonList list, MuonSlabs slabs, MuonArgs a) {
+  constexpr int kEach = kMuonPad * kMuonPad / 4 / kThreads;
   __shared__ double red[kThreads / kWave];
-  __shared__ float tile[kLay][kLay + 1];
+  __shared__ float tile[kMuonPad * kLayRow];
   const unsigned at = muon_find(list.first, list.count, blockIdx.x);
   const MuonItem& it = list.item[at];
+  const unsigned across = it.tall ? it.m : it.n, block = blockIdx.x - list.first[at];
+  const int r0 = (int)(block / across) * kMuonPad, c0 = (int)(block % across) * kMuonPad, cols = it.cols;
+  const float gs = a.grad_scale ? *a.grad_scale : 1.f;
+  const int c = c0 + threadIdx.x % 16 * 4;
+  Held<G, 4> gv[kEach];
+  Held<float, 4> mv[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int r = r0 + k * 16 + threadIdx.x / 16;
+    const long e = (long)r * cols + c, n = r < it.rows ? cols - c : 0;
+    gv[k].load(static_cast<const G*>(it.g) + e, n);
+    mv[k].load(a.momentum + it.start + e, a.momentum ? n : 0);
+  }
   double sum = 0.0;
   for (unsigned k = slabs.first[at] + threadIdx.x; k < slabs.first[at + 1]; k += kThreads) sum += a.squares[k];
-  for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
-  if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = sum;
-  __syncthreads();
-  sum = 0.0;
-  for (int w = 0; w < kThreads / kWave; ++w) sum += red[w];
+  sum = block_sum(sum, red);
   // (what is not finite makes all of the matrix NaN)
-  const double inv = sum < (double)INFINITY ? 1.0 / (sqrt(sum) + a.eps) : (double)NAN;
-  const G* g = static_cast<const G*>(it.g);
-  const float* m = a.momentum ? a.momentum + it.start : nullptr;
-  const float gs = a.grad_scale ? *a.grad_scale : 1.f;
-  // the matrix as it lies in memory, padded: rows by cols, of which the longer is n
-  const unsigned across = (it.tall ? it.m : it.n) * (kMuonTile / kLay), block = blockIdx.x - list.first[at];
-  const int r0 = (int)(block / across) * kLay, c0 = (int)(block % across) * kLay;
-  for (int k = threadIdx.x; k < kLay * kLay; k += kThreads) {
-    const int r = r0 + k / kLay, c = c0 + k % kLay;
-    float v = 0.f;
-    if (r < it.rows && c < it.cols)
-      v = (float)((double)update_of(g, m, (size_t)r * it.cols + c, gs, a) * inv) * kHoldX;
-    tile[k / kLay][k % kLay] = v;
+  const double inv = (sum < (double)INFINITY ? 1.0 / (sqrt(sum) + a.eps) : (double)NAN) * kHoldX;
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    gv[k].refresh();
+    mv[k].refresh();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = k * 16 + threadIdx.x / 16;
+      const bool there = r0 + r < it.rows && c + j < cols;
+      tile[r * kLayRow + threadIdx.x % 16 * 4 + j] = there ? (float)((double)update_of(gv[k][j], mv[k][j], gs, a) * inv) : 0.f;
+    }
   }
   __syncthreads();
   const MuonPlaces w = muon_places(it.m, it.n);
   char* part = a.ws + (size_t)it.off * 256;
-  // as it lies, and its transpose: X and t[0] or, tall, the other way round
-  const size_t mm = (size_t)it.m * kMuonTile * 4, nn = (size_t)it.n * kMuonTile * 4;
-  f16_t* as = reinterpret_cast<f16_t*>(part + (it.tall ? w.t0 : w.x));
-  f16_t* turned = reinterpret_cast<f16_t*>(part + (it.tall ? w.x : w.t0));
-  const size_t as_row = (it.tall ? mm : nn) / 2, turned_row = (it.tall ? nn : mm) / 2;
-  for (int k = threadIdx.x; k < kLay * kLay; k += kThreads) {
-    const int i = k / kLay, j = k % kLay;
-    const float v = tile[i][j], t = tile[j][i];
-    const f16_t vh = (f16_t)v, th = (f16_t)t;
-    // 32 values of a row: their high parts, then their low ones
-    f16_t* pv = as + (size_t)(r0 + i) * as_row + (size_t)c0 * 2 + j;
-    f16_t* pt = turned + (size_t)(c0 + i) * turned_row + (size_t)r0 * 2 + j;
-    pv[0] = vh;
-    pv[32] = (f16_t)(v - (float)vh);
-    pt[0] = th;
-    pt[32] = (f16_t)(t - (float)th);
+  // as it lies, and its transpose: X and t0 or, tall, the other way round
+  const size_t mm = muon_row(it.m), nn = muon_row(it.n), as_row = it.tall ? mm : nn, turned_row = it.tall ? nn : mm;
+  char* as = part + (it.tall ? w.t0 : w.x) + r0 * as_row + c0 * 4;
+  char* turned = part + (it.tall ? w.x : w.t0) + c0 * turned_row + r0 * 4;
+#pragma unroll
+  for (int k = 0; k < kMuonPad * kMuonPad / 8 / kThreads; ++k) {
+    const int i = k * (kThreads / 8) + threadIdx.x / 8, j = threadIdx.x % 8 * 8;
+    lay_eight(tile + i * kLayRow + j, 1, as + i * as_row, j);
+    lay_eight(tile + j * kLayRow + i, kLayRow, turned + i * turned_row, j);
   }
 }
 
@@ -126,6 +158,7 @@ double most_of_step(double a, double b, double c, double t) {
 
 constexpr double kUsual[3] = {3.4445, -4.7750, 2.0315};
 constexpr double kMostSingular = 1.75;
+constexpr unsigned kMuonFill = 512;  // tiles of 128 that a launch needs to go by them
 
 bl_status_t run(const bl_muon_plan_s* p, void* const* out, const void* const* grads, MuonArgs a, void* ws, hipStream_t s) {
   a.ws = static_cast<char*>(ws);
@@ -150,8 +183,8 @@ bl_status_t run(const bl_muon_plan_s* p, void* const* out, const void* const* gr
       it.tall = x.rows > x.cols;
       it.decay = x.decay;
       const long long m = std::min(x.rows, x.cols), n = std::max(x.rows, x.cols);
-      it.m = shapes.m[k] = (unsigned short)((m + kMuonTile - 1) / kMuonTile);
-      it.n = shapes.n[k] = (unsigned short)((n + kMuonTile - 1) / kMuonTile);
+      it.m = shapes.m[k] = (unsigned short)((m + kMuonPad - 1) / kMuonPad);
+      it.n = shapes.n[k] = (unsigned short)((n + kMuonPad - 1) / kMuonPad);
       gram += 3.0 * m * m * n;
       poly += 3.0 * m * m * m;
       apply += 6.0 * m * m * n;
@@ -180,7 +213,7 @@ bl_status_t run(const bl_muon_plan_s* p, void* const* out, const void* const* gr
       });
     });
     if (st != BL_OK) return st;
-    blocks = lay(list.first, [&](int k) { return (unsigned)list.item[k].m * list.item[k].n * 16; });
+    blocks = lay(list.first, [&](int k) { return (unsigned)list.item[k].m * list.item[k].n; });
     st = timed_launch("muon_lay", values * 16.0, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
       typed([&](auto g) {
         hipExtLaunchKernelGGL(k_muon_lay<decltype(g)>, dim3(blocks), dim3(kThreads), 0, s, e0, e1, 0, list, slabs, a);
@@ -192,23 +225,36 @@ bl_status_t run(const bl_muon_plan_s* p, void* const* out, const void* const* gr
       q.ws = a.ws;
       q.turn = (int)(k % 2);
       q.scale = kHoldA / (kHoldX * kHoldX);
-      blocks = lay(shapes.first, [&](int i) { return (unsigned)shapes.m[i] * (shapes.m[i] + 1) / 2; });
-      st = muon_product(kGram, shapes, blocks, gram, q, s);
+      auto triangle = [&](int side) {
+        return lay(shapes.first, [&](int i) {
+          const unsigned m = (shapes.m[i] * 64u + side - 1) / side;
+          return m * (m + 1) / 2;
+        });
+      };
+      auto all = [&](unsigned* first, int side) {
+        return lay(first, [&](int i) {
+          return (shapes.m[i] * 64u + side - 1) / side * ((shapes.n[i] * 64u + side - 1) / side);
+        });
+      };
+      int side = triangle(128) >= kMuonFill ? 128 : 64;
+      blocks = triangle(side);
+      st = muon_product(kGram, side, shapes, blocks, gram, q, s);
       if (st != BL_OK) return st;
       q.a = (float)(step.a * step.scale_b);
       q.b = (float)(step.b * step.scale_b / kHoldA);
       q.c = (float)(step.c * step.scale_b / ((double)kHoldA * kHoldA));
-      st = muon_product(kPoly, shapes, blocks, poly, q, s);
+      st = muon_product(kPoly, side, shapes, blocks, poly, q, s);
       if (st != BL_OK) return st;
       const bool last = k + 1 == p->steps.size();
       q.scale = 1.f / step.scale_b;  // (X keeps its power of two)
+      side = all(shapes.first, 128) >= kMuonFill ? 128 : 64;
       if (last) {
         q.scale /= kHoldX;
-        blocks = lay(list.first, [&](int i) { return (unsigned)shapes.m[i] * shapes.n[i]; });
-        st = muon_update(p->param_dtype, list, blocks, apply, q, a, s);
+        blocks = all(list.first, side);
+        st = muon_update(p->param_dtype, side, list, blocks, apply, q, a, s);
       } else {
-        blocks = lay(shapes.first, [&](int i) { return (unsigned)shapes.m[i] * shapes.n[i]; });
-        st = muon_product(kApply, shapes, blocks, apply, q, s);
+        blocks = all(shapes.first, side);
+        st = muon_product(kApply, side, shapes, blocks, apply, q, s);
       }
     }
     if (st != BL_OK) return st;
@@ -251,14 +297,23 @@ extern "C" bl_status_t bl_muon_plan_create(bl_muon_plan_t* out, const bl_muon_de
       // the largest power of two that keeps B below fp16's largest value, up to 2^14
       p->steps.push_back({c[0], c[1], c[2], (float)std::exp2(std::min(14.0, std::floor(std::log2(60000.0 / poly))))});
     }
+    std::vector<int> order;  // of those that are not empty: the longest sums first
     for (int i = 0; i < d->count; ++i) {
       const long long r = d->rows[i], c = d->cols[i];
       const double scale = d->scale ? d->scale[i] : std::sqrt(std::max(1.0, c ? (double)r / (double)c : 1.0));
       p->matrices.push_back({r, c, p->total, scale, (unsigned char)(!d->decay || d->decay[i])});
       p->total += (r * c + 63) / 64 * 64;
-      if (!r || !c) continue;
-      const unsigned m = (unsigned)((std::min(r, c) + kMuonTile - 1) / kMuonTile);
-      const unsigned n = (unsigned)((std::max(r, c) + kMuonTile - 1) / kMuonTile);
+      if (r && c) order.push_back(i);
+    }
+    auto longer = [&](int i, int j) {
+      const auto &x = p->matrices[i], &y = p->matrices[j];
+      return std::max(x.rows, x.cols) > std::max(y.rows, y.cols);
+    };
+    std::stable_sort(order.begin(), order.end(), longer);
+    for (int i : order) {
+      const long long r = d->rows[i], c = d->cols[i];
+      const unsigned m = (unsigned)((std::min(r, c) + kMuonPad - 1) / kMuonPad);
+      const unsigned n = (unsigned)((std::max(r, c) + kMuonPad - 1) / kMuonPad);
       if (p->batches.empty() || p->batches.back().of.size() == kMuonList ||
           p->batches.back().bytes + muon_places(m, n).bytes > kMuonBytes)
         p->batches.emplace_back();

@@ -9,12 +9,12 @@
 namespace blc {
 
 constexpr int kMuonList = 64;   // matrices of a launch: their list is part of the kernel's arguments
-constexpr int kMuonTile = 128;  // rows and columns of a product's tile: matrices are padded to it with zeros
-constexpr int kMuonSlab = 4096; // elements of a block that takes squares
+constexpr int kMuonPad = 64;    // matrices are padded to multiples of it with zeros
+constexpr int kMuonSlab = 4096;  // elements of a block that takes squares
 constexpr int kMuonSteps = 16;
 constexpr size_t kMuonBytes = 1ull << 36; // of a launch's matrices, which keeps its blocks far below 2^24
 
-// A matrix of a launch.  m and n: its shorter and longer side in tiles; `tall`: it has
+// A matrix of a launch.  m and n: its shorter and longer side in 64s; `tall`: it has
 // more rows than columns and is taken by its transpose.
 struct MuonItem {
   void* p;
@@ -95,14 +95,17 @@ namespace blc {
 // A = X X^T times 2^14.
 constexpr float kHoldX = 32768.f, kHoldA = 16384.f;
 
+// Bytes of a row of n 64s.
+__host__ __device__ inline size_t muon_row(unsigned n) { return (size_t)n * kMuonPad * 4; }
 // Byte offsets in a matrix's part: X [m][n], its transpose twice, A and B [m][m].
 struct MuonPlaces {
   size_t x, t0, t1, a, b, bytes;
   __host__ __device__ size_t t(int turn) const { return turn ? t1 : t0; }
 };
 __host__ __device__ inline MuonPlaces muon_places(unsigned m, unsigned n) {
-  const size_t tile = (size_t)kMuonTile * kMuonTile * 4, mn = (size_t)m * n * tile, mm = (size_t)m * m * tile;
-  return MuonPlaces{0, mn, 2 * mn, 3 * mn, 3 * mn + mm, 3 * mn + 2 * mm};
+  const size_t x = (size_t)m * kMuonPad * muon_row(n), t = (size_t)n * kMuonPad * muon_row(m),
+               s = (size_t)m * kMuonPad * muon_row(m);
+  return MuonPlaces{0, x, x + t, x + 2 * t, x + 2 * t + s, x + 2 * t + 2 * s};
 }
 
 __device__ __forceinline__ unsigned muon_find(const unsigned* first, int count, unsigned block) {
@@ -124,10 +127,11 @@ __device__ __forceinline__ unsigned muon_dither(unsigned long long place, unsign
 }
 
 enum MuonMode { kGram, kPoly, kApply };
-bl_status_t muon_product(int mode, const MuonShapes& shapes, unsigned blocks, double flops, const MuonProduct& q,
+// side: of the tiles, 64 or 128.
+bl_status_t muon_product(int mode, int side, const MuonShapes& shapes, unsigned blocks, double flops, const MuonProduct& q,
                          hipStream_t s);
 // The last step's product, and the parameters' update from its tiles.
-bl_status_t muon_update(int param_dtype, const MuonList& list, unsigned blocks, double flops, const MuonProduct& q,
+bl_status_t muon_update(int param_dtype, int side, const MuonList& list, unsigned blocks, double flops, const MuonProduct& q,
                         const MuonArgs& a, hipStream_t s);
 
 }  // namespace blc
