@@ -1,10 +1,16 @@
 // Orthogonalised update of many matrices: plan, momentum, norms and the order of launches.
 //
 // A launch takes momentum and squares of slabs of 4096 elements, a second divides by the
-// norm and lays the matrices out for the products, and three launches a Newton-Schulz step
-// (muon_gemm.hip) follow, the last of which writes the parameters.  The matrices of a
-// launch are part of its arguments, so that nothing is copied to the device beforehand and
-// a captured step replays.
+// norm and lays the matrices out for the products (muon_gemm.hip), the last of which writes
+// the parameters.  The matrices of a launch are part of its arguments, so that nothing is
+// copied to the device beforehand and a captured step replays.
+//
+// Steps may be joined: with A = X X^T, the next step's is B A B, so that a few steps need X
+// only for the first A and for X = (... B2 B1) X, and square products in between, which are
+// symmetric since all are polynomials of A.  Of m by 4 m that is 19 / 32 of the single steps'
+// operations, of squares the same.  But what rounds in A grows by B B where B A B is formed
+// and not from X: a joined run ends before its B's product may exceed 48 (three usual steps;
+// all five lose a digit or two where a gradient has a few strong directions, these none).
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -158,7 +164,9 @@ double most_of_step(double a, double b, double c, double t) {
 
 constexpr double kUsual[3] = {3.4445, -4.7750, 2.0315};
 constexpr double kMostSingular = 1.75;
-constexpr unsigned kMuonFill = 512;  // tiles of 128 that a launch needs to go by them
+constexpr double kMostJoined = 48.0;  // of a joined run's B's product
+// Tiles that a launch needs to go by larger ones.
+constexpr unsigned kFillSquare = 512, kFill128 = 256, kFill256 = 1024;
 
 bl_status_t run(const bl_muon_plan_s* p, void* const* out, const void* const* grads, MuonArgs a, void* ws, hipStream_t s) {
   a.ws = static_cast<char*>(ws);
@@ -219,42 +227,77 @@ bl_status_t run(const bl_muon_plan_s* p, void* const* out, const void* const* gr
         hipExtLaunchKernelGGL(k_muon_lay<decltype(g)>, dim3(blocks), dim3(kThreads), 0, s, e0, e1, 0, list, slabs, a);
       });
     });
-    for (size_t k = 0; st == BL_OK && k < p->steps.size(); ++k) {
-      const auto& step = p->steps[k];
-      MuonProduct q{};
-      q.ws = a.ws;
-      q.turn = (int)(k % 2);
-      q.scale = kHoldA / (kHoldX * kHoldX);
-      auto triangle = [&](int side) {
-        return lay(shapes.first, [&](int i) {
-          const unsigned m = (shapes.m[i] * 64u + side - 1) / side;
-          return m * (m + 1) / 2;
-        });
+    auto triangle = [&](int side) {
+      return lay(shapes.first, [&](int i) {
+        const unsigned m = (shapes.m[i] * 64u + side - 1) / side;
+        return m * (m + 1) / 2;
+      });
+    };
+    auto all = [&](unsigned* first, int side) {
+      return lay(first, [&](int i) {
+        return (shapes.m[i] * 64u + side - 1) / side * ((shapes.n[i] * 64u + side - 1) / side);
+      });
+    };
+    const int square_side = triangle(128) >= kFillSquare ? 128 : 64;
+    const int apply_side = all(shapes.first, 256) >= kFill256 ? 256 : all(shapes.first, 128) >= kFill128 ? 128 : 64;
+    const auto& steps = batch.joined ? p->joined : p->single;
+    MuonProduct q{};
+    q.ws = a.ws;
+    q.q2 = -1;
+    int product = kSlotB;  // of the joined steps
+    for (size_t k = 0; st == BL_OK && k < steps.size(); ++k) {
+      const auto& step = steps[k];
+      const bool end = k + 1 == steps.size();
+      auto go = [&](int mode, double flops) {
+        if (st == BL_OK) st = muon_product(mode, square_side, shapes, blocks, flops, q, s);
       };
-      auto all = [&](unsigned* first, int side) {
-        return lay(first, [&](int i) {
-          return (shapes.m[i] * 64u + side - 1) / side * ((shapes.n[i] * 64u + side - 1) / side);
-        });
-      };
-      int side = triangle(128) >= kMuonFill ? 128 : 64;
-      blocks = triangle(side);
-      st = muon_product(kGram, side, shapes, blocks, gram, q, s);
-      if (st != BL_OK) return st;
-      q.a = (float)(step.a * step.scale_b);
-      q.b = (float)(step.b * step.scale_b / kHoldA);
-      q.c = (float)(step.c * step.scale_b / ((double)kHoldA * kHoldA));
-      st = muon_product(kPoly, side, shapes, blocks, poly, q, s);
-      if (st != BL_OK) return st;
-      const bool last = k + 1 == p->steps.size();
-      q.scale = 1.f / step.scale_b;  // (X keeps its power of two)
-      side = all(shapes.first, 128) >= kMuonFill ? 128 : 64;
-      if (last) {
+      blocks = triangle(square_side);
+      if (step.first) {
+        q.out = kSlotA;
+        q.scale = kHoldA / (kHoldX * kHoldX);
+        go(kGram, gram);
+      }
+      const int b = step.first && !step.last ? kSlotQ0 : kSlotB;
+      q.p = kSlotA;
+      q.out = b;
+      q.a = (float)(step.a * step.hold_b);
+      q.b = (float)(step.b * step.hold_b / kHoldA);
+      q.c = (float)(step.c * step.hold_b / ((double)kHoldA * kHoldA));
+      go(kPoly, poly);
+      q.p = b;
+      // the product so far times B, and A B, then B (A B)
+      const int next = step.first ? b : product == kSlotQ0 ? kSlotQ1 : kSlotQ0;
+      const float scale = step.first ? 0.f : step.hold_q / (step.hold_b * steps[k - 1].hold_q);
+      if (!step.last) {
+        q.q = kSlotA;
+        q.out = kSlotAB;
+        q.scale = 1.f / step.hold_b;
+        q.q2 = step.first ? -1 : product;
+        q.out2 = next;
+        q.scale2 = scale;
+        go(kSquare, q.q2 < 0 ? poly : 2.0 * poly);
+        q.q = kSlotAB;
+        q.out = kSlotA;
+        q.q2 = -1;
+        go(kSquare, poly);
+      } else if (!step.first) {
+        q.q = product;
+        q.out = next;
+        q.scale = scale;
+        go(kSquare, poly);
+      }
+      product = next;
+      if (!step.last || st != BL_OK) continue;
+      q.p = product;
+      q.scale = 1.f / step.hold_q;  // (X keeps its power of two)
+      if (end) {
         q.scale /= kHoldX;
-        blocks = all(list.first, side);
-        st = muon_update(p->param_dtype, side, list, blocks, apply, q, a, s);
+        blocks = all(list.first, apply_side);
+        st = muon_update(p->param_dtype, apply_side, list, blocks, apply, q, a, s);
       } else {
-        blocks = all(shapes.first, side);
-        st = muon_product(kApply, side, shapes, blocks, apply, q, s);
+        blocks = all(shapes.first, apply_side);
+        st = muon_product(kApply, apply_side, shapes, blocks, apply, q, s);
+        q.turn ^= 1;
       }
     }
     if (st != BL_OK) return st;
@@ -284,6 +327,7 @@ extern "C" bl_status_t bl_muon_plan_create(bl_muon_plan_t* out, const bl_muon_de
   p->param_dtype = d->param_dtype;
   p->grad_dtype = d->grad_dtype;
   try {
+    auto hold = [](double most) { return (float)std::exp2(std::min(14.0, std::floor(std::log2(60000.0 / most)))); };
     double most = 1.0;
     for (int k = 0; k < d->steps; ++k) {
       const double* c = d->coef ? d->coef + 3 * k : kUsual;
@@ -294,8 +338,17 @@ extern "C" bl_status_t bl_muon_plan_create(bl_muon_plan_t* out, const bl_muon_de
         delete p;
         return BL_ERR_INVALID_ARG;
       }
-      // the largest power of two that keeps B below fp16's largest value, up to 2^14
-      p->steps.push_back({c[0], c[1], c[2], (float)std::exp2(std::min(14.0, std::floor(std::log2(60000.0 / poly))))});
+      p->single.push_back({c[0], c[1], c[2], hold(poly), poly, true, true, hold(poly)});
+    }
+    double run = 1.0;
+    for (size_t k = 0; k < p->single.size(); ++k) {
+      auto step = p->single[k];
+      step.first = k == 0 || run * step.most_b > kMostJoined;
+      if (step.first && k) p->joined.back().last = true;
+      run = step.first ? step.most_b : run * step.most_b;
+      step.last = k + 1 == p->single.size();
+      step.hold_q = hold(run);
+      p->joined.push_back(step);
     }
     std::vector<int> order;  // of those that are not empty: the longest sums first
     for (int i = 0; i < d->count; ++i) {
@@ -310,13 +363,41 @@ extern "C" bl_status_t bl_muon_plan_create(bl_muon_plan_t* out, const bl_muon_de
       return std::max(x.rows, x.cols) > std::max(y.rows, y.cols);
     };
     std::stable_sort(order.begin(), order.end(), longer);
+    auto sides = [&](int i, unsigned& m, unsigned& n) {
+      const auto& x = p->matrices[i];
+      m = (unsigned)((std::min(x.rows, x.cols) + kMuonPad - 1) / kMuonPad);
+      n = (unsigned)((std::max(x.rows, x.cols) + kMuonPad - 1) / kMuonPad);
+    };
+    // joined steps for matrices at least twice as long as high, single ones for the others; where
+    // either are too few to fill the GPU, what takes fewer operations for all
+    double single = 0.0, joined = 0.0;
+    unsigned long long tiles[2] = {0, 0};
+    for (int i : order) {
+      unsigned m, n;
+      sides(i, m, n);
+      const double runs = std::count_if(p->joined.begin(), p->joined.end(), [](auto& x) { return x.first; });
+      const double count = (double)p->single.size(), mm = 0.5 * m * m;
+      single += count * mm * (3.0 * n + m);
+      joined += runs * mm * 3.0 * n + mm * m * (count + 3.0 * (count - runs));
+      tiles[n >= 2 * m] += (unsigned long long)((m + 1) / 2) * ((m + 1) / 2 + 1) / 2;
+    }
+    const bool apart = tiles[0] >= kFillSquare && tiles[1] >= kFillSquare;
+    if (apart)
+      std::stable_partition(order.begin(), order.end(), [&](int i) {
+        unsigned m, n;
+        sides(i, m, n);
+        return n >= 2 * m;
+      });
     for (int i : order) {
       const long long r = d->rows[i], c = d->cols[i];
-      const unsigned m = (unsigned)((std::min(r, c) + kMuonPad - 1) / kMuonPad);
-      const unsigned n = (unsigned)((std::max(r, c) + kMuonPad - 1) / kMuonPad);
-      if (p->batches.empty() || p->batches.back().of.size() == kMuonList ||
-          p->batches.back().bytes + muon_places(m, n).bytes > kMuonBytes)
+      unsigned m, n;
+      sides(i, m, n);
+      const bool join = apart ? n >= 2 * m : joined < single;
+      if (p->batches.empty() || p->batches.back().of.size() == kMuonList || p->batches.back().joined != join ||
+          p->batches.back().bytes + muon_places(m, n).bytes > kMuonBytes) {
         p->batches.emplace_back();
+        p->batches.back().joined = join;
+      }
       auto& b = p->batches.back();
       b.of.push_back(i);
       b.off.push_back((unsigned)(b.bytes / 256));

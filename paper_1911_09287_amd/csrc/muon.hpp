@@ -52,13 +52,15 @@ struct MuonArgs {
   unsigned key, seed;
 };
 
-// One product of a Newton-Schulz step: powers of two that its operands hold and its result
-// is stored with, and the step's coefficients.
+// A product's launch.  Square matrices [m][m] are kept in slots of a matrix's part.
 struct MuonProduct {
   char* ws;
-  float scale;    // of the accumulated sum
-  float a, b, c;  // (poly: of I, A, A A, with the powers of two)
-  int turn;       // which of the two transposes is read
+  int p, q, out;     // slots of the operands and the result (gram: out; poly: p, out; apply: p)
+  float scale;       // of the accumulated sum
+  int q2, out2;      // square: a second product p q2 in the same launch, or q2 < 0
+  float scale2;
+  float a, b, c;     // poly: of I, A and A A, with the powers of two
+  int turn;          // apply: which of X's two transposes is read
 };
 
 }  // namespace blc
@@ -71,7 +73,10 @@ struct bl_muon_plan_s {
   };
   struct Step {
     double a, b, c;
-    float scale_b;  // power of two that B is stored with
+    float hold_b;   // power of two that B is held with
+    double most_b;  // its largest singular value's bound
+    bool first, last;  // of the steps that X is multiplied by at once
+    float hold_q;   // power of two that their product up to this step is held with
   };
   // Matrices that are taken together, by their numbers.
   struct Batch {
@@ -79,9 +84,10 @@ struct bl_muon_plan_s {
     std::vector<unsigned> off;
     size_t bytes;
     long slabs;
+    bool joined;  // by joined steps, not single ones
   };
   std::vector<Matrix> matrices;
-  std::vector<Step> steps;
+  std::vector<Step> single, joined;
   std::vector<Batch> batches;
   int param_dtype, grad_dtype;
   long long total;
@@ -92,20 +98,22 @@ namespace blc {
 
 // Values are held as two fp16 parts, high and low, 32 of a row's high parts and then their
 // low ones side by side.  X is held times 2^15 (no singular value of it is above 1.75),
-// A = X X^T times 2^14.
+// A = X X^T and A B (no singular value above 1.75^2) times 2^14.
 constexpr float kHoldX = 32768.f, kHoldA = 16384.f;
+// Slots of square matrices: A, B, A B and the product of a few steps' B, in turn.
+enum MuonSlot { kSlotA, kSlotB, kSlotAB, kSlotQ0, kSlotQ1, kSlots };
 
 // Bytes of a row of n 64s.
 __host__ __device__ inline size_t muon_row(unsigned n) { return (size_t)n * kMuonPad * 4; }
-// Byte offsets in a matrix's part: X [m][n], its transpose twice, A and B [m][m].
+// Byte offsets in a matrix's part: X [m][n], its transpose twice and the slots [m][m].
 struct MuonPlaces {
-  size_t x, t0, t1, a, b, bytes;
+  size_t x, t0, t1, square, each, bytes;
   __host__ __device__ size_t t(int turn) const { return turn ? t1 : t0; }
+  __host__ __device__ size_t slot(int s) const { return square + s * each; }
 };
 __host__ __device__ inline MuonPlaces muon_places(unsigned m, unsigned n) {
-  const size_t x = (size_t)m * kMuonPad * muon_row(n), t = (size_t)n * kMuonPad * muon_row(m),
-               s = (size_t)m * kMuonPad * muon_row(m);
-  return MuonPlaces{0, x, x + t, x + 2 * t, x + 2 * t + s, x + 2 * t + 2 * s};
+  const size_t x = (size_t)m * kMuonPad * muon_row(n), s = (size_t)m * kMuonPad * muon_row(m);
+  return MuonPlaces{0, x, 2 * x, 3 * x, s, 3 * x + kSlots * s};
 }
 
 __device__ __forceinline__ unsigned muon_find(const unsigned* first, int count, unsigned block) {
@@ -126,7 +134,7 @@ __device__ __forceinline__ unsigned muon_dither(unsigned long long place, unsign
   return (x * 0x6A09E667u) >> 16;
 }
 
-enum MuonMode { kGram, kPoly, kApply };
+enum MuonMode { kGram, kPoly, kSquare, kApply };
 // side: of the tiles, 64 or 128.
 bl_status_t muon_product(int mode, int side, const MuonShapes& shapes, unsigned blocks, double flops, const MuonProduct& q,
                          hipStream_t s);

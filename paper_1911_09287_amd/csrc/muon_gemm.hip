@@ -1,13 +1,14 @@
-// The products of a Newton-Schulz step, A = X X^T, B = a I + b A + c A A and X = B X, of many
-// matrices in one launch each.
+// The products of Newton-Schulz steps of many matrices, in one launch each: A = X X^T, B =
+// a I + b A + c A A, products of the square matrices (which commute, being polynomials of
+// one, so that they are symmetric) and X = B X.
 //
-// Both operands of each lie with the summed index side by side: A and B are symmetric, and X
-// is held together with its transpose.  Values are two fp16 parts, v = high + low to 22 bits;
-// a product takes high high + high low + low high on the matrix cores (the last, low low, is
-// below 2^-22) and sums in fp32.  One fp16 part alone leaves errors of 1 % in the result where a
-// gradient has a few strong directions: rounding is noise in all directions, and the steps
-// raise the weak ones by up to 3.44 each.  Symmetric products are taken for tiles on and
-// below the diagonal only and stored twice.
+// Both operands of each lie with the summed index side by side: square matrices are
+// symmetric, and X is held together with its transpose.  Values are two fp16 parts, v = high +
+// low to 22 bits; a product takes high high + high low + low high on the matrix cores (the
+// last, low low, is below 2^-22) and sums in fp32.  One fp16 part alone leaves errors of 1 %
+// in the result where a gradient has a few strong directions: rounding is noise in all
+// directions, and the steps raise the weak ones by up to 3.44 each.  Symmetric products
+// are taken for tiles on and below the diagonal only and stored twice.
 #include "muon.hpp"
 
 namespace blc {
@@ -228,21 +229,24 @@ __global__ __launch_bounds__(MuonShape<SIDE>::kThreads, MuonShape<SIDE>::kBlocks
   // 32 rows of each wave at a time are turned by way of LDS
   static_assert(S::kLds >= S::kGrid * 32 * SIDE * 4 * (S::kGroups > 1 ? 2 : 1), "room for them");
   extern __shared__ __align__(16) char lds[];
-  const MuonTilePlace p = MuonTilePlace::make<SIDE, MODE != kApply>(list.first, list.count, list.m, list.n,
-                                                                              near_tile<SIDE>(blockIdx.x, gridDim.x));
+  const unsigned blocks = MODE == kSquare ? list.first[kMuonList] : gridDim.x;
+  const bool second = MODE == kSquare && blockIdx.x >= blocks;
+  const MuonTilePlace p = MuonTilePlace::make<SIDE, MODE != kApply>(
+      list.first, list.count, list.m, list.n, near_tile<SIDE>(second ? blockIdx.x - blocks : blockIdx.x, blocks));
   const MuonPlaces w = muon_places(p.m, p.n);
   char* part = q.ws + (size_t)list.off[p.at] * 256;
   const unsigned sum = MODE == kGram ? p.n : p.m;  // of the summed index
   const size_t stride = muon_row(sum), mm = muon_row(p.m), nn = muon_row(p.n);
-  const char* P = part + (MODE == kGram ? w.x : MODE == kPoly ? w.a : w.b);
-  const char* Q = MODE == kApply ? part + w.t(q.turn) : P;
+  const char* P = part + (MODE == kGram ? w.x : w.slot(q.p));
+  const char* Q = MODE == kApply ? part + w.t(q.turn) : MODE == kSquare ? part + w.slot(second ? q.q2 : q.q) : P;
   MuonSums<SIDE> sums;
   sums.product(fetched<SIDE>(P, Q, stride, p), stride, (int)sum * 2, lds);
   float* tiled = reinterpret_cast<float*>(lds + (S::kGroups > 1 ? S::kLds / 2 : 0));
   // columns of the tile are rows of the transpose: four of a lane's values lie side by side
-  char* across = part + (MODE == kGram ? w.a : MODE == kPoly ? w.b : w.t(q.turn ^ 1));
-  char* along = part + (MODE == kGram ? w.a : MODE == kPoly ? w.b : w.x);
+  char* across = part + (MODE == kApply ? w.t(q.turn ^ 1) : w.slot(second ? q.out2 : q.out));
+  char* along = MODE == kApply ? part + w.x : across;
   const size_t along_row = MODE == kApply ? nn : mm;
+  const float scale = second ? q.scale2 : q.scale;
   const bool both = MODE == kApply || p.ti != p.tj, there = wave_there<SIDE>(p);
 #pragma unroll
   for (int tp = 0; tp < S::kSub; ++tp) {
@@ -250,7 +254,7 @@ __global__ __launch_bounds__(MuonShape<SIDE>::kThreads, MuonShape<SIDE>::kBlocks
       sums.each_four(tp, [&](int row, int col, float (&v)[4]) {
         const size_t place = held_at((size_t)p.tj * SIDE + col, mm, p.ti * SIDE + row);
         if (MODE == kPoly) {
-          const char* from = part + w.a + place;
+          const char* from = P + place;
           const Pack<f16_t, 4> hi = load_pack<f16_t, 4>(reinterpret_cast<const f16_t*>(from)),
                                lo = load_pack<f16_t, 4>(reinterpret_cast<const f16_t*>(from + 64));
 #pragma unroll
@@ -260,7 +264,7 @@ __global__ __launch_bounds__(MuonShape<SIDE>::kThreads, MuonShape<SIDE>::kBlocks
           }
         } else {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] *= q.scale;
+          for (int k = 0; k < 4; ++k) v[k] *= scale;
         }
         hold<4>(across + place, v);
         if (both)
@@ -293,7 +297,7 @@ __global__ __launch_bounds__(MuonShape<SIDE>::kThreads, MuonShape<SIDE>::kBlocks
   const char* part = q.ws + (size_t)it.off * 256;
   const size_t stride = muon_row(p.m);
   MuonSums<SIDE> sums;
-  sums.product(fetched<SIDE>(part + w.b, part + w.t(q.turn), stride, p), stride, (int)p.m * 2, lds);
+  sums.product(fetched<SIDE>(part + w.slot(q.p), part + w.t(q.turn), stride, p), stride, (int)p.m * 2, lds);
   if (!wave_there<SIDE>(p)) return;
   float keep = 1.f, rate = 1.f;
   unsigned key = a.key;
@@ -356,11 +360,13 @@ bl_status_t with_side(int side, Go&& go) {
 
 bl_status_t muon_product(int mode, int side, const MuonShapes& shapes, unsigned blocks, double flops,
                          const MuonProduct& q, hipStream_t s) {
-  const char* names[] = {"muon_gram", "muon_poly", "muon_apply"};
+  const char* names[] = {"muon_gram", "muon_poly", "muon_square", "muon_apply"};
+  if (mode == kSquare && q.q2 >= 0) blocks *= 2;
   return with_side(side, [&](auto n) {
     using S = MuonShape<decltype(n)::value>;
-    auto kernel = mode == kGram ? k_muon_product<kGram, decltype(n)::value>
-                                : mode == kPoly ? k_muon_product<kPoly, decltype(n)::value> : k_muon_product<kApply, decltype(n)::value>;
+    constexpr int N = decltype(n)::value;
+    auto kernel = mode == kGram ? k_muon_product<kGram, N> : mode == kPoly ? k_muon_product<kPoly, N>
+                  : mode == kSquare ? k_muon_product<kSquare, N> : k_muon_product<kApply, N>;
     const bl_status_t st = lds_opt_in(reinterpret_cast<const void*>(kernel), S::kLds);
     if (st != BL_OK) return st;
     return timed_launch(names[mode], 0.0, flops, s, [&](hipEvent_t e0, hipEvent_t e1) {

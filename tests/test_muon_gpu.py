@@ -3,14 +3,15 @@
 Tolerances come from the arithmetic, before any run, in the Frobenius norm.  U = 2^-24.  A
 value held in two fp16 parts is off by 2^-22 = 4 U, a product of such values by two of those
 and what the third product leaves out (2^-22), their sum by 16 U of the magnitudes: together
-32 U |P| |Q|^T, whose norm is at most 32 U |P| |Q|.  A step of singular values t -> f(t), odd,
-moves an error by at most max |f'| over the range that they have, L, so that
+32 U |P| |Q|^T, whose norm is at most 32 U |P| |Q|, |.| being Frobenius norms of the 64-bit
+reference.  So a product R = P Q, held again, of operands that are off by dP and dQ is off by
 
-  E' = L E + |X|_2 dB + 32 U |B| |X| + 4 U |X'|,   dB = |b| dA + |c| (2 |A|_2 dA + 32 U |A|^2) + 4 U |B|,
-  dA = 36 U |X|^2,
+  dR = ||P|| dQ + ||Q|| dP + 32 U |P| |Q| + 4 U |R|,   ||.|| the largest singular value.
 
-with |.| the Frobenius norms of the 64-bit reference.  What X holds below 2^-14 of the
-largest power of two is off by 2^-39: 2^-39 sqrt(m n) at each step.
+Steps may be taken one by one or joined, X = Q X with Q = ... B2 B1 and A' = B (A B) in place of
+X X^T of the next X.  An error of X itself at a run's start is moved by the run's map of
+singular values t -> f(t), odd, by at most the product of max |f'|.  What X holds below 2^-14
+of the largest power of two is off by 2^-39: 2^-39 sqrt(m n) each time X is held.
 """
 import math
 
@@ -24,24 +25,58 @@ pytestmark = pytest.mark.gpu
 USUAL = ((3.4445, -4.7750, 2.0315),) * 5
 
 
+def error_bound(t, x, coefficients, most):
+    """Of the result's Frobenius norm where runs end before the bound of their B's product passes `most`."""
+    places = 2.0 ** -39 * math.sqrt(x.numel())
+    err, top, k = 6 * U * x.norm().item() + places, 1.0, 0
+    eye = t.eye(x.shape[0], dtype=x.dtype, device=x.device)
+    while k < len(coefficients):
+        gram = x @ x.t()
+        size_a, top_a = gram.norm().item(), top ** 2
+        da = 36 * U * x.norm().item() ** 2
+        q, size_q, top_q, dq, slope, start = None, 0.0, 1.0, 0.0, 1.0, top
+        while True:
+            a, b, c = coefficients[k]
+            s = t.linspace(0, top + 0.01, 2001, dtype=t.float64)
+            top_b = (a + b * s ** 2 + c * s ** 4).abs().max().item()
+            if q is not None and top_q * top_b > most:
+                break
+            slope *= (a + 3 * b * s ** 2 + 5 * c * s ** 4).abs().max().item()
+            top = (s * (a + b * s ** 2 + c * s ** 4)).abs().max().item()
+            poly = a * eye + b * gram + c * gram @ gram
+            size_b = poly.norm().item()
+            db = abs(b) * da + abs(c) * (2 * top_a * da + 32 * U * size_a ** 2) + 4 * U * size_b
+            if q is None:
+                q, dq = poly, db
+            else:
+                new = poly @ q
+                dq = top_b * dq + top_q * db + 32 * U * size_b * size_q + 4 * U * new.norm().item()
+                q = new
+            size_q, top_q = q.norm().item(), top_q * top_b
+            ab = poly @ gram
+            size_ab, top_ab = ab.norm().item(), top_a * top_b
+            dab = top_b * da + top_a * db + 32 * U * size_b * size_a + 4 * U * size_ab
+            gram = poly @ ab
+            size_a, top_a = gram.norm().item(), top ** 2
+            da = top_b * dab + top_ab * db + 32 * U * size_b * size_ab + 4 * U * size_a
+            k += 1
+            if k == len(coefficients):
+                break
+        following = q @ x
+        err = slope * err + start * dq + 32 * U * size_q * x.norm().item() + 4 * U * following.norm().item() + places
+        x = following
+    return err
+
+
 def reference(t, u, eps, coefficients=USUAL):
     """X in 64 bits and the bound of the error in the Frobenius norm."""
     tall = u.shape[0] > u.shape[1]
     x = (u.t() if tall else u).double()
     x = x / (x.norm() + eps)
-    places = 2.0 ** -39 * math.sqrt(x.numel())
-    err, top = 6 * U * x.norm().item() + places, 1.0
+    err = max(error_bound(t, x, coefficients, most) for most in (0.0, 50.0))
     for a, b, c in coefficients:
         gram = x @ x.t()
-        poly = a * t.eye(x.shape[0], dtype=x.dtype, device=x.device) + b * gram + c * gram @ gram
-        s = t.linspace(0, top + 0.01, 2001, dtype=t.float64)
-        slope = (a + 3 * b * s ** 2 + 5 * c * s ** 4).abs().max().item()
-        following = poly @ x
-        da = 36 * U * x.norm().item() ** 2
-        db = abs(b) * da + abs(c) * (2 * top ** 2 * da + 32 * U * gram.norm().item() ** 2) + 4 * U * poly.norm().item()
-        err = slope * err + top * db + 32 * U * poly.norm().item() * x.norm().item() + 4 * U * following.norm().item() + places
-        top = (s * (a + b * s ** 2 + c * s ** 4)).abs().max().item()
-        x = following
+        x = a * x + (b * gram + c * gram @ gram) @ x
     return (x.t() if tall else x), err
 
 
