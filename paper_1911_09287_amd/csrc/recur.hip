@@ -23,48 +23,60 @@ __global__ __launch_bounds__(WAVES* kWave) void k_recur_fwd(RecurArgs r) {
   const RecurPlace<T, LAYOUT, WAVES> p(r);
   const long chunk = blockIdx.y, begin = chunk * r.chunk, end = min(r.length, begin + r.chunk);
   const long sites = r.outer * r.inner, at = p.o * r.inner + p.i;
-  const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer + p.i;
-  const T* x = static_cast<const T*>(r.x) + p.o * r.in_outer + p.i;
-  T* y = static_cast<T*>(r.y) + p.o * r.out_outer + p.i;
+  const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer;
+  const T* x = static_cast<const T*>(r.x) + p.o * r.in_outer;
+  T* y = static_cast<T*>(r.y) + p.o * r.out_outer;
   const unsigned char* resets = RESETS ? r.resets + p.o * r.length : nullptr;
   float h[N];  // before the tile
-  if (gridDim.y > 1) {
-    state_at<N, RESETS>(r, p.o, p.i, p.n, 0, 1, chunk, h);
+  if (WAVES > 1 && gridDim.y > 1) {
+    state_at<N, S::kLanes, RESETS, true>(r, p, chunk, gridDim.y, h);
   } else {
 #pragma unroll
-    for (int j = 0; j < N; ++j) h[j] = r.h0 && j < p.n ? r.h0[at + j] : 0.f;
+    for (int j = 0; j < N; ++j) h[j] = r.h0 ? r.h0[at + j] : 0.f;
   }
-  const long mine = begin + p.slice * EACH;  // this thread's steps of the first tile
-  RecurRaw<T, LAYOUT, EACH> g, v;
-  g.load(gate + mine * r.in_step, r.in_step, end - mine, p.n);
-  v.load(x + mine * r.in_step, r.in_step, end - mine, p.n);
-  unsigned bits = reset_bits<EACH, RESETS>(resets + mine, end - mine);
+  // a tile's loads are in flight while the one before it is worked on
+  struct Raw {
+    RecurRaw<T, LAYOUT, EACH> g, v;
+    RecurResets<EACH, RESETS> z;
+  } raw[2];
+  const long mine = p.slice * EACH;  // this thread's steps of a tile
+  const unsigned in_off = (unsigned)((mine * r.in_step + p.i) * sizeof(T)), out_off = (unsigned)((mine * r.out_step + p.i) * sizeof(T));
+  auto load = [&](auto full, Raw& w, long tile) {
+    constexpr bool FULL = decltype(full)::value;
+    const long t = tile + mine;
+    if constexpr (FULL) {
+      w.g.load_all(gate + tile * r.in_step, r.in_step, in_off);
+      w.v.load_all(x + tile * r.in_step, r.in_step, in_off);
+    } else {
+      w.g.load(gate + t * r.in_step + p.i, r.in_step, end - t);
+      w.v.load(x + t * r.in_step + p.i, r.in_step, end - t);
+    }
+    w.z.template load<FULL>(resets + t, end - t);
+  };
   int turn = 0;
-  for (long t = mine; t - mine + begin < end; t += TILE, turn ^= 1) {
-    const long there = end - t;
+  // a tile from w while the following one is loaded; full: both have all their steps
+  auto work = [&](auto full, Raw& w, Raw& following, long tile) {
+    constexpr bool FULL = decltype(full)::value;
+    const long t = tile + mine, there = end - t;
+    load(full, following, tile + TILE);
+    const unsigned bits = w.z.bits();
     float a[EACH][N], b[EACH][N];
     Stretch<N> own = stretch_none<N>();
-    g.refresh();
-    v.refresh();
+    w.g.refresh();
+    w.v.refresh();
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         float rest;
-        gate_of<GATE>(g.at(k, j), a[k][j], rest);
-        b[k][j] = rest * v.at(k, j);
-        if (k >= there) a[k][j] = 1.f, b[k][j] = 0.f;
-        const bool drop = RESETS && (bits >> k & 1);
-        own.b[j] = drop ? b[k][j] : fmaf(a[k][j], own.b[j], b[k][j]);
+        gate_of<GATE>(w.g.at(k, j), a[k][j], rest);
+        b[k][j] = rest * w.v.at(k, j);
+        if (!FULL && k >= there) a[k][j] = 1.f, b[k][j] = 0.f;
+        own.b[j] = RESETS && (bits >> k & 1) ? b[k][j] : fmaf(a[k][j], own.b[j], b[k][j]);
         own.a[j] *= a[k][j];
       }
     }
     own.drop = RESETS && bits;
-    const unsigned now = bits;
-    // the next tile's loads are in flight while this one's state is found
-    g.load(gate + (t + TILE) * r.in_step, r.in_step, there - TILE, p.n);
-    v.load(x + (t + TILE) * r.in_step, r.in_step, there - TILE, p.n);
-    bits = reset_bits<EACH, RESETS>(resets + t + TILE, there - TILE);
     Stretch<N> all;
     const Stretch<N> before = wave_others<N, S::kLanes, RESETS, true>(own, all);
     float s[N];  // this thread's state
@@ -78,7 +90,7 @@ __global__ __launch_bounds__(WAVES* kWave) void k_recur_fwd(RecurArgs r) {
         for (int j = 0; j < N; ++j) sa[turn][p.wave][p.lane][j] = all.a[j], sb[turn][p.wave][p.lane][j] = all.b[j];
         if (p.lane == 0) sd[turn][p.wave] = all.drop;
       }
-      __syncthreads();  // (the other half is written before the next one)
+      block_sync();  // (the other half is written before the next one)
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) {
         Stretch<N> o;
@@ -92,25 +104,42 @@ __global__ __launch_bounds__(WAVES* kWave) void k_recur_fwd(RecurArgs r) {
       }
     }
     stretch_apply<N, RESETS>(before, s);
-    if (r.states && there > 0 && t % r.every == 0) {
+    if (r.states && there > 0 && (t & (r.every - 1)) == 0) {
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (j < p.n) r.states[t / r.every * sites + at + j] = s[j];
+      for (int j = 0; j < N; ++j) r.states[(t >> r.every_log2) * sites + at + j] = s[j];
     }
     RecurOut<T, LAYOUT, EACH> out;
 #pragma unroll
     for (int k = 0; k < EACH; ++k)
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        s[j] = RESETS && (now >> k & 1) ? b[k][j] : fmaf(a[k][j], s[j], b[k][j]);
+        s[j] = RESETS && (bits >> k & 1) ? b[k][j] : fmaf(a[k][j], s[j], b[k][j]);
         out.set(k, j, s[j]);
       }
-    out.store(y + t * r.out_step, r.out_step, there, p.n);
+    if constexpr (FULL) out.store_all(y + tile * r.out_step, r.out_step, out_off);
+    else out.store(y + t * r.out_step + p.i, r.out_step, there);
+    turn ^= 1;
+  };
+  constexpr std::true_type full;
+  constexpr std::false_type any;
+  long t = begin;
+  load(any, raw[0], t);
+  if (r.near && t + 2 * TILE <= end) {
+    // (the first one apart, so that each wait of the loop finds the same accesses behind it)
+    work(full, raw[0], raw[1], t);
+    for (t += TILE; t + 3 * TILE <= end; t += 2 * TILE) {
+      work(full, raw[1], raw[0], t);
+      work(full, raw[0], raw[1], t + TILE);
+    }
+    raw[0] = raw[1];
+  }
+  for (; t < end; t += TILE) {
+    work(any, raw[0], raw[1], t);
+    raw[0] = raw[1];
   }
   if (r.last && end == r.length && p.slice == 0) {
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (j < p.n) r.last[at + j] = h[j];
+    for (int j = 0; j < N; ++j) r.last[at + j] = h[j];
   }
 }
 
@@ -123,14 +152,17 @@ __global__ __launch_bounds__(8 * kWave) void k_recur_fwd_part(RecurArgs r) {
   const long begin = chunk * r.chunk + p.slice * stretch, end = min(r.length, begin + stretch);
   const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer + p.i;
   const T* x = static_cast<const T*>(r.x) + p.o * r.in_outer + p.i;
+  const unsigned char* resets = RESETS ? r.resets + p.o * r.length : nullptr;
   Stretch<N> own = stretch_none<N>();
   for (long t = begin; t < end; t += EACH) {
     RecurRaw<T, LAYOUT, EACH> g, v;
-    g.load(gate + t * r.in_step, r.in_step, end - t, p.n);
-    v.load(x + t * r.in_step, r.in_step, end - t, p.n);
-    const unsigned bits = reset_bits<EACH, RESETS>(RESETS ? r.resets + p.o * r.length + t : nullptr, end - t);
+    RecurResets<EACH, RESETS> z;
+    g.load(gate + t * r.in_step, r.in_step, end - t);
+    v.load(x + t * r.in_step, r.in_step, end - t);
+    z.template load<false>(resets + t, end - t);
     g.refresh();
     v.refresh();
+    const unsigned bits = z.bits();
 #pragma unroll
     for (int k = 0; k < EACH; ++k)
       if (k < end - t) {
@@ -166,10 +198,10 @@ __global__ __launch_bounds__(kThreads) void k_recur_serial(RecurArgs r, int vec_
     g.load(gate + t * r.in_step, n);
     v.load(x + t * r.in_step, n);
     const bool drop = RESETS && r.resets[o * r.length + t];
-    if (r.states && t % r.every == 0) {
+    if (r.states && (t & (r.every - 1)) == 0) {
 #pragma unroll
       for (int j = 0; j < N; ++j)
-        if (j < n) r.states[t / r.every * sites + at + j] = h[j];
+        if (j < n) r.states[(t >> r.every_log2) * sites + at + j] = h[j];
     }
     g.refresh();
     v.refresh();
@@ -199,11 +231,6 @@ __global__ void k_recur_none(const float* from, float* to, long n) {
 // Up to this many steps a thread walks them alone.
 constexpr long kSerialSteps = 8;
 
-long blocks_of(const bl_recurrence_desc_t& d, int layout) {
-  const long lanes = layout == kWide ? 16 * (8 / dtype_bytes(d.dtype)) : layout == kNarrow ? 4 : 1;
-  return d.outer * ((d.inner + lanes - 1) / lanes);
-}
-
 template <typename T>
 bl_status_t forward(const bl_recurrence_plan_s* p, RecurArgs r, hipStream_t s) {
   const bl_recurrence_desc_t& d = p->d;
@@ -219,11 +246,11 @@ bl_status_t forward(const bl_recurrence_plan_s* p, RecurArgs r, hipStream_t s) {
       });
     });
   }
-  const dim3 grid((unsigned)blocks_of(d, p->layout), (unsigned)p->chunks[0]);
+  const dim3 grid((unsigned)recur_blocks(d, p->layout[0]), (unsigned)p->chunks[0]);
   r.chunk = p->chunk[0];
   if (p->chunks[0] > 1) {
     const bl_status_t st = timed_launch("recur_fwd_part", bytes * 2 / 3, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-      recur_dispatch(d.gate, p->layout, 8, r.resets, [&](auto g, auto l, auto, auto z) {
+      recur_dispatch(d.gate, p->layout[0], 8, r.resets, [&](auto g, auto l, auto, auto z) {
         hipExtLaunchKernelGGL((k_recur_fwd_part<T, decltype(g)::value, decltype(l)::value, decltype(z)::value>), grid,
                               dim3(8 * kWave), 0, s, e0, e1, 0, r);
       });
@@ -231,7 +258,7 @@ bl_status_t forward(const bl_recurrence_plan_s* p, RecurArgs r, hipStream_t s) {
     if (st != BL_OK) return st;
   }
   return timed_launch("recur_fwd", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-    recur_dispatch(d.gate, p->layout, p->waves[0], r.resets, [&](auto g, auto l, auto w, auto z) {
+    recur_dispatch(d.gate, p->layout[0], p->waves[0], r.resets, [&](auto g, auto l, auto w, auto z) {
       hipExtLaunchKernelGGL((k_recur_fwd<T, decltype(g)::value, decltype(l)::value, decltype(w)::value, decltype(z)::value>),
                             grid, dim3(decltype(w)::value * kWave), 0, s, e0, e1, 0, r);
     });
@@ -249,6 +276,9 @@ RecurArgs args_of(const bl_recurrence_plan_s* p, void* ws) {
   r.out_outer = d.out_outer;
   r.out_step = d.out_step;
   r.every = p->every;
+  while (1L << r.every_log2 < r.every) ++r.every_log2;
+  const long tile = 8L * kWave * 8;  // (steps of any tile, at most)
+  r.near = (tile * std::max(d.in_step, d.out_step) + d.inner) * dtype_bytes(d.dtype) < 1LL << 32;
   const long parts = std::max(p->chunks[0], p->chunks[1]) + 1, sites = d.outer * d.inner;
   r.part_a = static_cast<float*>(ws);
   r.part_b = r.part_a + parts * sites;
@@ -300,25 +330,29 @@ extern "C" bl_status_t bl_recurrence_plan_create(bl_recurrence_plan_t* out, cons
   if (!p) return BL_ERR_OOM;
   p->d = d;
   const bool row = d.inner == 1 && d.in_step == 1 && d.out_step == 1;
-  p->layout = row ? kRow : d.inner <= 4 ? kNarrow : kWide;
-  const long slices = row ? kWave : p->layout == kNarrow ? 16 : 4, blocks = std::max(blocks_of(d, p->layout), 1L);
-  const long each[2] = {row ? 16 / dtype_bytes(d.dtype) : 8, row ? 16 / dtype_bytes(d.dtype) : 4};
+  const long slices = row ? kWave : d.inner <= 4 ? 16 : 4;
+  long most_threads = 0;
   for (int i = 0; i < 2; ++i) {
-    const long tile = slices * each[i];  // of one wave
+    // lines of 128 bytes where they leave a block for each compute unit
+    p->layout[i] = row ? kRow : d.inner <= 4 ? kNarrow : recur_blocks(d, kWide) >= 256 ? kWide : kHalf;
+    const long blocks = std::max(recur_blocks(d, p->layout[i]), 1L), tile = slices * recur_each(p->layout[i], dtype_bytes(d.dtype), i);
+    // (tile: of one wave)
     // one wave a block: rows in such a number that they fill the GPU, or sequences of one tile
-    p->waves[i] = p->layout != kNarrow && (d.length <= tile || (row && blocks >= 2048)) ? 1 : 8;
-    // as many chunks as bring 512 blocks onto the GPU, each of four tiles at least
+    p->waves[i] = p->layout[i] != kNarrow && (d.length <= tile || (row && blocks >= 2048)) ? 1 : 8;
+    // fewer blocks than compute units: as many chunks as bring 512 blocks onto the GPU, each
+    // of four tiles at least
     const long part = 8 * tile;
-    const long want = p->waves[i] == 1 ? 1 : std::max(1L, std::min<long>(512 / blocks, d.length / (4 * part)));
+    const long want = p->waves[i] == 1 || blocks >= 256 ? 1 : std::max(1L, std::min<long>(512 / blocks, d.length / (4 * part)));
     p->chunk[i] = want > 1 ? ((d.length + want - 1) / want + part - 1) / part * part : std::max<long>(d.length, 1);
     p->chunks[i] = want > 1 ? (d.length + p->chunk[i] - 1) / p->chunk[i] : 1;
+    most_threads = std::max(most_threads, blocks * p->waves[i] * kWave);
   }
-  if (blocks >= (1LL << 32) / kWave / std::max(p->waves[0], p->waves[1])) {  // (a launch has fewer threads)
+  if (most_threads >= 1LL << 32) {  // (a launch has fewer)
     delete p;
     return BL_ERR_UNSUPPORTED;
   }
   // a state at every tile of the backward pass
-  p->every = slices * each[1] * p->waves[1];
+  p->every = slices * recur_each(p->layout[1], dtype_bytes(d.dtype), true) * p->waves[1];
   const size_t parts = std::max(p->chunks[0], p->chunks[1]);
   p->bytes = parts > 1 ? (parts + 1) * ((size_t)d.outer * d.inner * 8 + d.outer) : 0;
   *out = p;

@@ -24,71 +24,79 @@ __global__ __launch_bounds__(WAVES* kWave) void k_recur_bwd(RecurArgs r) {
   const RecurPlace<T, LAYOUT, WAVES> p(r);
   const long chunk = blockIdx.y, begin = chunk * r.chunk, end = min(r.length, begin + r.chunk);
   const long sites = r.outer * r.inner, at = p.o * r.inner + p.i;
-  const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer + p.i;
-  const T* x = static_cast<const T*>(r.x) + p.o * r.in_outer + p.i;
-  const T* dy = static_cast<const T*>(r.dy) + p.o * r.out_outer + p.i;
-  T* dgate = static_cast<T*>(r.dgate) + p.o * r.in_outer + p.i;
-  T* dx = static_cast<T*>(r.dx) + p.o * r.in_outer + p.i;
+  const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer;
+  const T* x = static_cast<const T*>(r.x) + p.o * r.in_outer;
+  const T* dy = static_cast<const T*>(r.dy) + p.o * r.out_outer;
+  T* dgate = static_cast<T*>(r.dgate) + p.o * r.in_outer;
+  T* dx = static_cast<T*>(r.dx) + p.o * r.in_outer;
   const unsigned char* resets = RESETS ? r.resets + p.o * r.length : nullptr;
   float back[N];  // what the tiles behind pass back
-  if (gridDim.y > 1) {
-    state_at<N, RESETS>(r, p.o, p.i, p.n, gridDim.y - 1, -1, gridDim.y - 1 - chunk, back);
+  if (WAVES > 1 && gridDim.y > 1) {
+    state_at<N, S::kLanes, RESETS, false>(r, p, chunk, gridDim.y, back);
   } else {
 #pragma unroll
-    for (int j = 0; j < N; ++j) back[j] = r.dlast && j < p.n ? r.dlast[at + j] : 0.f;
+    for (int j = 0; j < N; ++j) back[j] = r.dlast ? r.dlast[at + j] : 0.f;
   }
-  const long tiles = (end - begin + TILE - 1) / TILE;
-  long t = begin + (tiles - 1) * TILE + p.slice * EACH;
-  RecurRaw<T, LAYOUT, EACH> g, v, d;
-  unsigned bits;
-  float h[N];  // the state at the tile's start
-  auto load = [&](long from, long there) {
-    g.load(gate + from * r.in_step, r.in_step, there, p.n);
-    v.load(x + from * r.in_step, r.in_step, there, p.n);
-    d.load(dy + from * r.out_step, r.out_step, there, p.n);
-    bits = reset_bits<EACH, RESETS>(resets + from, there);
-    const long tile = (from - p.slice * EACH) / TILE;
+  // a tile's loads are in flight while the one behind it is worked on
+  struct Raw {
+    RecurRaw<T, LAYOUT, EACH> g, v, d;
+    RecurResets<EACH, RESETS> z;
+    float h[N];  // the state at the tile's start
+  } raw[2];
+  const long mine = p.slice * EACH;  // this thread's steps of a tile
+  const unsigned in_off = (unsigned)((mine * r.in_step + p.i) * sizeof(T)), out_off = (unsigned)((mine * r.out_step + p.i) * sizeof(T));
+  auto load = [&](auto full, Raw& w, long tile) {
+    constexpr bool FULL = decltype(full)::value;
+    const long t = tile + mine;
+    if constexpr (FULL) {
+      w.g.load_all(gate + tile * r.in_step, r.in_step, in_off);
+      w.v.load_all(x + tile * r.in_step, r.in_step, in_off);
+      w.d.load_all(dy + tile * r.out_step, r.out_step, out_off);
+    } else {
+      w.g.load(gate + t * r.in_step + p.i, r.in_step, end - t);
+      w.v.load(x + t * r.in_step + p.i, r.in_step, end - t);
+      w.d.load(dy + t * r.out_step + p.i, r.out_step, end - t);
+    }
+    w.z.template load<FULL>(resets + t, end - t);
+    const float* state = r.states + tile / TILE * sites + at;
 #pragma unroll
-    for (int j = 0; j < N; ++j) h[j] = there > -TILE && j < p.n ? r.states[tile * sites + at + j] : 0.f;
+    for (int j = 0; j < N; ++j) w.h[j] = state[j];
   };
-  load(t, end - t);
   int turn = 0;
-  for (long tile = tiles - 1; tile >= 0; --tile, t -= TILE, turn ^= 1) {
-    const long there = end - t;
-    float a[EACH][N], rest[EACH][N], xs[EACH][N], ds[EACH][N];
+  // a tile from w while the one before it is loaded; full: both are there, with all their steps
+  auto work = [&](auto full, Raw& w, Raw& following, bool more, long tile) {
+    constexpr bool FULL = decltype(full)::value;
+    const long t = tile + mine, there = end - t;
+    if (FULL || more) load(full, following, tile - TILE);
+    const unsigned bits = w.z.bits();
+    float a[EACH][N], rest[EACH][N];
     Stretch<N> own = stretch_none<N>(), rev = stretch_none<N>();
-    g.refresh();
-    v.refresh();
-    d.refresh();
+    w.g.refresh();
+    w.v.refresh();
+    w.d.refresh();
 #pragma unroll
     for (int k = 0; k < EACH; ++k)
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        gate_of<GATE>(g.at(k, j), a[k][j], rest[k][j]);
-        xs[k][j] = v.at(k, j);
-        ds[k][j] = d.at(k, j);
-        if (k >= there) a[k][j] = 1.f, rest[k][j] = 0.f, xs[k][j] = 0.f, ds[k][j] = 0.f;
-        const float b = rest[k][j] * xs[k][j];
+        gate_of<GATE>(w.g.at(k, j), a[k][j], rest[k][j]);
+        if (!FULL && k >= there) a[k][j] = 1.f, rest[k][j] = 0.f;  // (x and dy are 0 there)
+        const float b = rest[k][j] * w.v.at(k, j);
         own.b[j] = RESETS && (bits >> k & 1) ? b : fmaf(a[k][j], own.b[j], b);
         own.a[j] *= a[k][j];
       }
 #pragma unroll
     for (int k = EACH - 1; k >= 0; --k)
 #pragma unroll
-      for (int j = 0; j < N; ++j) rev.b[j] = RESETS && (bits >> k & 1) ? 0.f : a[k][j] * (ds[k][j] + rev.b[j]);
+      for (int j = 0; j < N; ++j) rev.b[j] = RESETS && (bits >> k & 1) ? 0.f : a[k][j] * (w.d.at(k, j) + rev.b[j]);
 #pragma unroll
     for (int j = 0; j < N; ++j) rev.a[j] = own.a[j];
     own.drop = rev.drop = RESETS && bits;
-    const unsigned now = bits;
     float s[N], back_now[N];  // this thread's state, and what is passed back to it
-#pragma unroll
-    for (int j = 0; j < N; ++j) s[j] = h[j];
-    if (tile > 0) load(t - TILE, there + TILE);
     Stretch<N> all, all_rev;
     const Stretch<N> before = wave_others<N, S::kLanes, RESETS, true>(own, all);
     const Stretch<N> behind = wave_others<N, S::kLanes, RESETS, false>(rev, all_rev);
 #pragma unroll
-    for (int j = 0; j < N; ++j) back_now[j] = back[j];
+    for (int j = 0; j < N; ++j) s[j] = w.h[j], back_now[j] = back[j];
     if constexpr (WAVES == 1) {
       stretch_apply<N, RESETS>(all_rev, back);
     } else {
@@ -102,7 +110,7 @@ __global__ __launch_bounds__(WAVES* kWave) void k_recur_bwd(RecurArgs r) {
         }
         if (p.lane == 0) sd[turn][p.wave] = all.drop;
       }
-      __syncthreads();  // (the other half is written before the next one)
+      block_sync();  // (the other half is written before the next one)
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) {
         Stretch<N> o;
@@ -130,32 +138,54 @@ __global__ __launch_bounds__(WAVES* kWave) void k_recur_bwd(RecurArgs r) {
     for (int k = 0; k < EACH; ++k)
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        hs[k][j] = RESETS && (now >> k & 1) ? 0.f : s[j];
-        s[j] = RESETS && (now >> k & 1) ? rest[k][j] * xs[k][j] : fmaf(a[k][j], s[j], rest[k][j] * xs[k][j]);
+        const float b = rest[k][j] * w.v.at(k, j);
+        hs[k][j] = RESETS && (bits >> k & 1) ? 0.f : s[j];
+        s[j] = RESETS && (bits >> k & 1) ? b : fmaf(a[k][j], s[j], b);
       }
     RecurOut<T, LAYOUT, EACH> og, ox;
 #pragma unroll
     for (int k = EACH - 1; k >= 0; --k)
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const float dh = ds[k][j] + back_now[j], ah = a[k][j] * dh;
+        const float dh = w.d.at(k, j) + back_now[j], ah = a[k][j] * dh;
         if (GATE == BL_GATE_SIGMOID) {
-          og.set(k, j, ah * rest[k][j] * (hs[k][j] - xs[k][j]));
+          og.set(k, j, ah * rest[k][j] * (hs[k][j] - w.v.at(k, j)));
           ox.set(k, j, dh * rest[k][j]);
         } else {
           og.set(k, j, ah * hs[k][j]);
           ox.set(k, j, dh);
         }
-        back_now[j] = RESETS && (now >> k & 1) ? 0.f : ah;
-        if (k >= there) back_now[j] = dh;
+        back_now[j] = RESETS && (bits >> k & 1) ? 0.f : ah;
       }
-    og.store(dgate + t * r.in_step, r.in_step, there, p.n);
-    ox.store(dx + t * r.in_step, r.in_step, there, p.n);
+    if constexpr (FULL) {
+      og.store_all(dgate + tile * r.in_step, r.in_step, in_off);
+      ox.store_all(dx + tile * r.in_step, r.in_step, in_off);
+    } else {
+      og.store(dgate + t * r.in_step + p.i, r.in_step, there);
+      ox.store(dx + t * r.in_step + p.i, r.in_step, there);
+    }
+    turn ^= 1;
+  };
+  constexpr std::true_type full;
+  constexpr std::false_type any;
+  long tile = begin + (end - begin - 1) / TILE * TILE;
+  load(any, raw[0], tile);
+  for (bool last = true; tile >= begin; last = false) {
+    work(any, raw[0], raw[1], tile > begin, tile);
+    raw[0] = raw[1];
+    tile -= TILE;
+    if (!last || !r.near || tile < begin + TILE) continue;
+    // (one apart, so that each wait of the loop finds the same accesses behind it)
+    work(full, raw[0], raw[1], true, tile);
+    for (tile -= TILE; tile >= begin + 2 * TILE; tile -= 2 * TILE) {
+      work(full, raw[1], raw[0], true, tile);
+      work(full, raw[0], raw[1], true, tile - TILE);
+    }
+    raw[0] = raw[1];
   }
   if (r.dh0 && chunk == 0 && p.slice == 0) {
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (j < p.n) r.dh0[at + j] = back[j];
+    for (int j = 0; j < N; ++j) r.dh0[at + j] = back[j];
   }
 }
 
@@ -168,15 +198,18 @@ __global__ __launch_bounds__(8 * kWave) void k_recur_bwd_part(RecurArgs r) {
   const long begin = chunk * r.chunk + p.slice * stretch, end = min(r.length, begin + stretch);
   const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer + p.i;
   const T* dy = static_cast<const T*>(r.dy) + p.o * r.out_outer + p.i;
+  const unsigned char* resets = RESETS ? r.resets + p.o * r.length : nullptr;
   Stretch<N> own = stretch_none<N>();
   for (long t = begin + (stretch - EACH); t >= begin; t -= EACH) {
     if (t >= end) continue;
     RecurRaw<T, LAYOUT, EACH> g, d;
-    g.load(gate + t * r.in_step, r.in_step, end - t, p.n);
-    d.load(dy + t * r.out_step, r.out_step, end - t, p.n);
-    const unsigned bits = reset_bits<EACH, RESETS>(RESETS ? r.resets + p.o * r.length + t : nullptr, end - t);
+    RecurResets<EACH, RESETS> z;
+    g.load(gate + t * r.in_step, r.in_step, end - t);
+    d.load(dy + t * r.out_step, r.out_step, end - t);
+    z.template load<false>(resets + t, end - t);
     g.refresh();
     d.refresh();
+    const unsigned bits = z.bits();
 #pragma unroll
     for (int k = EACH - 1; k >= 0; --k)
       if (k < end - t) {
@@ -197,12 +230,11 @@ template <typename T>
 bl_status_t backward(const bl_recurrence_plan_s* p, RecurArgs r, hipStream_t s) {
   const bl_recurrence_desc_t& d = p->d;
   const double bytes = 5.0 * d.outer * d.length * d.inner * sizeof(T);
-  const long lanes = p->layout == kWide ? 16 * (8 / (int)sizeof(T)) : p->layout == kNarrow ? 4 : 1;
-  const dim3 grid((unsigned)(d.outer * ((d.inner + lanes - 1) / lanes)), (unsigned)p->chunks[1]);
+  const dim3 grid((unsigned)recur_blocks(d, p->layout[1]), (unsigned)p->chunks[1]);
   r.chunk = p->chunk[1];
   if (p->chunks[1] > 1) {
     const bl_status_t st = timed_launch("recur_bwd_part", bytes * 2 / 5, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-      recur_dispatch(d.gate, p->layout, 8, r.resets, [&](auto g, auto l, auto, auto z) {
+      recur_dispatch(d.gate, p->layout[1], 8, r.resets, [&](auto g, auto l, auto, auto z) {
         hipExtLaunchKernelGGL((k_recur_bwd_part<T, decltype(g)::value, decltype(l)::value, decltype(z)::value>), grid,
                               dim3(8 * kWave), 0, s, e0, e1, 0, r);
       });
@@ -210,7 +242,7 @@ bl_status_t backward(const bl_recurrence_plan_s* p, RecurArgs r, hipStream_t s) 
     if (st != BL_OK) return st;
   }
   return timed_launch("recur_bwd", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-    recur_dispatch(d.gate, p->layout, p->waves[1], r.resets, [&](auto g, auto l, auto w, auto z) {
+    recur_dispatch(d.gate, p->layout[1], p->waves[1], r.resets, [&](auto g, auto l, auto w, auto z) {
       hipExtLaunchKernelGGL((k_recur_bwd<T, decltype(g)::value, decltype(l)::value, decltype(w)::value, decltype(z)::value>),
                             grid, dim3(decltype(w)::value * kWave), 0, s, e0, e1, 0, r);
     });
