@@ -21,7 +21,7 @@ __global__ __launch_bounds__(WAVES* kWave) void k_recur_fwd(RecurArgs r) {
   __shared__ float sa[2][WAVES][S::kLanes][N], sb[2][WAVES][S::kLanes][N];
   __shared__ int sd[2][WAVES];
   const RecurPlace<T, LAYOUT, WAVES> p(r);
-  const long chunk = blockIdx.y, begin = chunk * r.chunk, end = min(r.length, begin + r.chunk);
+  const long chunk = p.chunk, begin = chunk * r.chunk, end = min(r.length, begin + r.chunk);
   const long sites = r.outer * r.inner, at = p.o * r.inner + p.i;
   const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer;
   const T* x = static_cast<const T*>(r.x) + p.o * r.in_outer;
@@ -148,34 +148,57 @@ __global__ __launch_bounds__(8 * kWave) void k_recur_fwd_part(RecurArgs r) {
   using S = RecurShape<T, LAYOUT>;
   constexpr int N = S::kVec, EACH = recur_each<T, LAYOUT, false>(), SLICES = S::kSlices * 8;
   const RecurPlace<T, LAYOUT, 8> p(r);
-  const long chunk = blockIdx.y, stretch = r.chunk / SLICES;  // (a multiple of EACH)
-  const long begin = chunk * r.chunk + p.slice * stretch, end = min(r.length, begin + stretch);
-  const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer + p.i;
-  const T* x = static_cast<const T*>(r.x) + p.o * r.in_outer + p.i;
+  const long chunk = p.chunk, stretch = r.chunk / SLICES;  // (a multiple of EACH)
+  const long first = chunk * r.chunk, begin = first + p.slice * stretch, end = min(r.length, begin + stretch);
+  const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer;
+  const T* x = static_cast<const T*>(r.x) + p.o * r.in_outer;
   const unsigned char* resets = RESETS ? r.resets + p.o * r.length : nullptr;
-  Stretch<N> own = stretch_none<N>();
-  for (long t = begin; t < end; t += EACH) {
+  struct Raw {
     RecurRaw<T, LAYOUT, EACH> g, v;
     RecurResets<EACH, RESETS> z;
-    g.load(gate + t * r.in_step, r.in_step, end - t);
-    v.load(x + t * r.in_step, r.in_step, end - t);
-    z.template load<false>(resets + t, end - t);
-    g.refresh();
-    v.refresh();
-    const unsigned bits = z.bits();
+  } raw[2];
+  Stretch<N> own = stretch_none<N>();
+  auto work = [&](Raw& w, long there) {
+    w.g.refresh();
+    w.v.refresh();
+    const unsigned bits = w.z.bits();
 #pragma unroll
     for (int k = 0; k < EACH; ++k)
-      if (k < end - t) {
+      if (k < there) {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           float a, rest;
-          gate_of<GATE>(g.at(k, j), a, rest);
-          const float b = rest * v.at(k, j);
+          gate_of<GATE>(w.g.at(k, j), a, rest);
+          const float b = rest * w.v.at(k, j);
           own.b[j] = RESETS && (bits >> k & 1) ? b : fmaf(a, own.b[j], b);
           own.a[j] *= a;
         }
       }
     own.drop |= RESETS && bits;
+  };
+  if (first + r.chunk <= r.length && (r.chunk * r.in_step + r.inner) * (long)sizeof(T) < 1L << 32) {
+    // the chunk is whole: the following steps' loads are in flight while these are worked on
+    const unsigned off = (unsigned)((p.slice * stretch * r.in_step + p.i) * sizeof(T));
+    auto load = [&](Raw& w, long t) {
+      w.g.load_all(gate + (first + t) * r.in_step, r.in_step, off);
+      w.v.load_all(x + (first + t) * r.in_step, r.in_step, off);
+      w.z.template load<true>(resets + begin + t, EACH);
+    };
+    load(raw[0], 0);
+    for (long t = 0; t < stretch; t += 2 * EACH) {
+      if (t + EACH < stretch) load(raw[1], t + EACH);
+      work(raw[0], EACH);
+      if (t + EACH >= stretch) break;
+      if (t + 2 * EACH < stretch) load(raw[0], t + 2 * EACH);
+      work(raw[1], EACH);
+    }
+  } else {
+    for (long t = begin; t < end; t += EACH) {
+      raw[0].g.load(gate + t * r.in_step + p.i, r.in_step, end - t);
+      raw[0].v.load(x + t * r.in_step + p.i, r.in_step, end - t);
+      raw[0].z.template load<false>(resets + t, end - t);
+      work(raw[0], end - t);
+    }
   }
   chunk_part<N, S::kLanes, 8, RESETS, true>(r, p, own, chunk, r.h0, chunk == 0);
 }
@@ -333,8 +356,8 @@ extern "C" bl_status_t bl_recurrence_plan_create(bl_recurrence_plan_t* out, cons
   const long slices = row ? kWave : d.inner <= 4 ? 16 : 4;
   long most_threads = 0;
   for (int i = 0; i < 2; ++i) {
-    // lines of 128 bytes where they leave a block for each compute unit
-    p->layout[i] = row ? kRow : d.inner <= 4 ? kNarrow : recur_blocks(d, kWide) >= 256 ? kWide : kHalf;
+    // lines of 64 bytes where those of 128 leave compute units without a block, and they do not
+    p->layout[i] = row ? kRow : d.inner <= 4 ? kNarrow : recur_blocks(d, kWide) < 256 && recur_blocks(d, kHalf) >= 256 ? kHalf : kWide;
     const long blocks = std::max(recur_blocks(d, p->layout[i]), 1L), tile = slices * recur_each(p->layout[i], dtype_bytes(d.dtype), i);
     // (tile: of one wave)
     // one wave a block: rows in such a number that they fill the GPU, or sequences of one tile
@@ -342,7 +365,7 @@ extern "C" bl_status_t bl_recurrence_plan_create(bl_recurrence_plan_t* out, cons
     // fewer blocks than compute units: as many chunks as bring 512 blocks onto the GPU, each
     // of four tiles at least
     const long part = 8 * tile;
-    const long want = p->waves[i] == 1 || blocks >= 256 ? 1 : std::max(1L, std::min<long>(512 / blocks, d.length / (4 * part)));
+    const long want = p->waves[i] == 1 || blocks >= 256 ? 1 : std::max(1L, std::min<long>(1024 / blocks, d.length / (4 * part)));
     p->chunk[i] = want > 1 ? ((d.length + want - 1) / want + part - 1) / part * part : std::max<long>(d.length, 1);
     p->chunks[i] = want > 1 ? (d.length + p->chunk[i] - 1) / p->chunk[i] : 1;
     most_threads = std::max(most_threads, blocks * p->waves[i] * kWave);

@@ -102,26 +102,29 @@ struct RecurShape {
   static constexpr int kSlices = kWave / kLanes;  // of a wave, along steps
 };
 
-// Where a thread stands: its sequence, first channel and slice of the tile's steps.  Lanes that
+// Where a thread stands: its sequence and chunk of it, first channel and slice of the tile's steps.  Lanes that
 // would reach over the last channel (of which there are at least a lane's) take the last
 // ones, as another lane of their wave does too: both read the same before either writes, and
 // write the same.
 template <typename T, int LAYOUT, int WAVES>
 struct RecurPlace {
   using S = RecurShape<T, LAYOUT>;
-  long o, i;
+  long o, chunk, i;
   int wave, lane, slice;
   __device__ __forceinline__ explicit RecurPlace(const RecurArgs& r) {
     const long tiles = (r.inner + S::kLanes * S::kVec - 1) / (S::kLanes * S::kVec);
     // blocks go to the GPU's eight dies in turn, each with caches of its own: a die takes
-    // neighbouring channels of a sequence
-    const unsigned die = blockIdx.x % 8, each = gridDim.x / 8, more = gridDim.x % 8;
-    const long block = (long)die * each + min(die, more) + blockIdx.x / 8;
-    o = block / tiles;
+    // neighbouring channels of a sequence's chunk
+    const unsigned index = blockIdx.y * gridDim.x + blockIdx.x, all = gridDim.x * gridDim.y;
+    const unsigned die = index % 8, at = die * (all / 8) + min(die, all % 8) + index / 8;
+    const unsigned q = at / (unsigned)tiles;  // chunks of a sequence, then sequences
+    o = q / gridDim.y;
+    chunk = q - (unsigned)o * gridDim.y;
+    const unsigned block = at - q * (unsigned)tiles;
     wave = WAVES == 1 ? 0 : threadIdx.x / kWave;
     lane = threadIdx.x % kWave;
     slice = wave * S::kSlices + lane / S::kLanes;
-    i = min((block % tiles * S::kLanes + lane % S::kLanes) * S::kVec, r.inner - S::kVec);
+    i = min(((long)block * S::kLanes + lane % S::kLanes) * S::kVec, r.inner - S::kVec);
   }
 };
 

@@ -22,7 +22,7 @@ __global__ __launch_bounds__(WAVES* kWave) void k_recur_bwd(RecurArgs r) {
   __shared__ float sa[2][WAVES][S::kLanes][N], sb[2][WAVES][S::kLanes][N], sr[2][WAVES][S::kLanes][N];
   __shared__ int sd[2][WAVES];
   const RecurPlace<T, LAYOUT, WAVES> p(r);
-  const long chunk = blockIdx.y, begin = chunk * r.chunk, end = min(r.length, begin + r.chunk);
+  const long chunk = p.chunk, begin = chunk * r.chunk, end = min(r.length, begin + r.chunk);
   const long sites = r.outer * r.inner, at = p.o * r.inner + p.i;
   const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer;
   const T* x = static_cast<const T*>(r.x) + p.o * r.in_outer;
@@ -194,34 +194,59 @@ __global__ __launch_bounds__(8 * kWave) void k_recur_bwd_part(RecurArgs r) {
   using S = RecurShape<T, LAYOUT>;
   constexpr int N = S::kVec, EACH = recur_each<T, LAYOUT, true>(), SLICES = S::kSlices * 8;
   const RecurPlace<T, LAYOUT, 8> p(r);
-  const long chunk = blockIdx.y, stretch = r.chunk / SLICES;  // (a multiple of EACH)
-  const long begin = chunk * r.chunk + p.slice * stretch, end = min(r.length, begin + stretch);
-  const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer + p.i;
-  const T* dy = static_cast<const T*>(r.dy) + p.o * r.out_outer + p.i;
+  const long chunk = p.chunk, stretch = r.chunk / SLICES;  // (a multiple of EACH)
+  const long first = chunk * r.chunk, begin = first + p.slice * stretch, end = min(r.length, begin + stretch);
+  const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer;
+  const T* dy = static_cast<const T*>(r.dy) + p.o * r.out_outer;
   const unsigned char* resets = RESETS ? r.resets + p.o * r.length : nullptr;
-  Stretch<N> own = stretch_none<N>();
-  for (long t = begin + (stretch - EACH); t >= begin; t -= EACH) {
-    if (t >= end) continue;
+  struct Raw {
     RecurRaw<T, LAYOUT, EACH> g, d;
     RecurResets<EACH, RESETS> z;
-    g.load(gate + t * r.in_step, r.in_step, end - t);
-    d.load(dy + t * r.out_step, r.out_step, end - t);
-    z.template load<false>(resets + t, end - t);
-    g.refresh();
-    d.refresh();
-    const unsigned bits = z.bits();
+  } raw[2];
+  Stretch<N> own = stretch_none<N>();
+  auto work = [&](Raw& w, long there) {
+    w.g.refresh();
+    w.d.refresh();
+    const unsigned bits = w.z.bits();
 #pragma unroll
     for (int k = EACH - 1; k >= 0; --k)
-      if (k < end - t) {
+      if (k < there) {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           float a, rest;
-          gate_of<GATE>(g.at(k, j), a, rest);
-          own.b[j] = RESETS && (bits >> k & 1) ? 0.f : a * (d.at(k, j) + own.b[j]);
+          gate_of<GATE>(w.g.at(k, j), a, rest);
+          own.b[j] = RESETS && (bits >> k & 1) ? 0.f : a * (w.d.at(k, j) + own.b[j]);
           own.a[j] *= a;
         }
       }
     own.drop |= RESETS && bits;
+  };
+  const long widest = max(r.in_step, r.out_step);
+  if (first + r.chunk <= r.length && (r.chunk * widest + r.inner) * (long)sizeof(T) < 1L << 32) {
+    // the chunk is whole: the loads of the steps before are in flight while these are worked on
+    const unsigned in_off = (unsigned)((p.slice * stretch * r.in_step + p.i) * sizeof(T));
+    const unsigned out_off = (unsigned)((p.slice * stretch * r.out_step + p.i) * sizeof(T));
+    auto load = [&](Raw& w, long t) {
+      w.g.load_all(gate + (first + t) * r.in_step, r.in_step, in_off);
+      w.d.load_all(dy + (first + t) * r.out_step, r.out_step, out_off);
+      w.z.template load<true>(resets + begin + t, EACH);
+    };
+    load(raw[0], stretch - EACH);
+    for (long t = stretch - EACH; t >= 0; t -= 2 * EACH) {
+      if (t > 0) load(raw[1], t - EACH);
+      work(raw[0], EACH);
+      if (t <= 0) break;
+      if (t > EACH) load(raw[0], t - 2 * EACH);
+      work(raw[1], EACH);
+    }
+  } else {
+    for (long t = begin + (stretch - EACH); t >= begin; t -= EACH) {
+      if (t >= end) continue;
+      raw[0].g.load(gate + t * r.in_step + p.i, r.in_step, end - t);
+      raw[0].d.load(dy + t * r.out_step + p.i, r.out_step, end - t);
+      raw[0].z.template load<false>(resets + t, end - t);
+      work(raw[0], end - t);
+    }
   }
   chunk_part<N, S::kLanes, 8, RESETS, false>(r, p, own, chunk, r.dlast, chunk == (long)gridDim.y - 1);
 }
