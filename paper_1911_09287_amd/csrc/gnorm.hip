@@ -218,6 +218,11 @@ extern "C" bl_status_t bl_group_norm_plan_create(bl_group_norm_plan_t* out, cons
                                    : std::max<long>((d.sites + blocks - 1) / blocks, kThreads * most_vec * 4);
     p->chunk = (p->chunk + most_vec - 1) / most_vec * most_vec;
   }
+  d.layout == BL_CHANNELS_LAST ? gnorm_last_whole(p) : gnorm_first_whole(p);
+  // (few groups that are large go over more of the GPU in parts)
+  const __int128 wholes = (__int128)d.batch * p->whole_tiles;
+  for (int i = 0; i < 2; ++i)
+    if (wholes >= 1LL << 22 || (wholes < 128 && p->whole_threads[i] > kThreads)) p->whole_threads[i] = 0;
   p->chunk = std::min<long>(p->chunk, d.sites);
   p->chunks = (int)((d.sites + p->chunk - 1) / p->chunk);
   const size_t groups = (size_t)d.batch * d.groups, channels = (size_t)d.batch * d.channels;

@@ -12,6 +12,10 @@ struct bl_group_norm_plan_s {
   int tiles;       // channels last: blocks along channels
   long chunk;      // sites of a block
   int chunks;      // of them
+  // a block keeps whole groups of a sample in registers (threads 0: no block can)
+  int whole_threads[2], whole_each[2];  // forward and backward: threads, accesses of one
+  int whole_lanes;  // channels last: accesses of a site (`tile` channels); first: lanes of a channel
+  int whole_tiles;  // channels last: blocks of a sample
   size_t off_part, off_sums, off_own, bytes;
 };
 
@@ -37,7 +41,13 @@ struct GroupNormArgs {
 __device__ __forceinline__ float norm_z(float x, float mean, float rstd, float w, float b) {
   return fmaf((x - mean) * rstd, w, b);
 }
-__device__ __forceinline__ float logistic(float z) { return 1.f / (1.f + expf(-z)); }
+// By the hardware's power of two and reciprocal, an ulp each; rounding z log2(e) moves the
+// exponential by |z| ulps more, which z / (1 + exp(-z)) and its slope have at most 0.3 of.  (The
+// library's exponential and division took 30 of 45 instructions a value, and these bound
+// 16-bit passes: 128 x 3136 x 64 bf16 36 us against 22.)
+__device__ __forceinline__ float logistic(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -0x1.715476p+0f));
+}
 template <int ACT>
 __device__ __forceinline__ float act_of(float z) {
   if (ACT == BL_ACT_RELU) return z > 0.f ? z : z != z ? z : 0.f;
@@ -69,6 +79,28 @@ __device__ __forceinline__ float weight_at(const void* w, bool wide, long c, flo
   return !w ? one : wide ? static_cast<const float*>(w)[c] : to_f32(static_cast<const T*>(w)[c]);
 }
 
+constexpr int kMostThreads = 512;  // of a block that keeps whole groups: 256 registers a thread
+
+// Sum over a block of up to 16 waves, in each thread; red: 16 values that nobody else uses.
+__device__ __forceinline__ float block_sum(float x, float* red) {
+  x = wave_sum(x);
+  if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = x;
+  __syncthreads();
+  x = 0.f;
+  for (unsigned w = 0; w < blockDim.x / kWave; ++w) x += red[w];
+  return x;
+}
+
+// go(E) for the least of 1, 2, 4 and 8 that is at least `each`.
+template <typename Go>
+void with_each(int each, Go&& go) {
+  if (each <= 1) go(std::integral_constant<int, 1>());
+  else if (each <= 2) go(std::integral_constant<int, 2>());
+  else if (each <= 4) go(std::integral_constant<int, 4>());
+  else go(std::integral_constant<int, 8>());
+}
+constexpr int kMostEach = 8;
+
 // Mean and sum of squares about it, of values that come in tiles: each tile's own are
 // taken in registers and joined (Chan, Golub and LeVeque, "Updating formulae and a
 // pairwise algorithm for computing sample variances", 1979), so that no square of a
@@ -87,6 +119,9 @@ bl_status_t gnorm_last_forward(const bl_group_norm_plan_s* p, const GroupNormArg
 bl_status_t gnorm_last_backward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
 bl_status_t gnorm_first_forward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
 bl_status_t gnorm_first_backward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
+// How a plan's blocks keep whole groups, if they can.
+void gnorm_last_whole(bl_group_norm_plan_s* p);
+void gnorm_first_whole(bl_group_norm_plan_s* p);
 // Statistics from the parts; backward: means over groups and sums over samples from theirs.
 bl_status_t gnorm_join_forward(const GroupNormArgs& a, hipStream_t s);
 bl_status_t gnorm_join_backward(const GroupNormArgs& a, int dtype, hipStream_t s);

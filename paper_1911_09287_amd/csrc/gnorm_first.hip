@@ -191,6 +191,163 @@ __global__ __launch_bounds__(kThreads) void k_first_bwd_apply(GroupNormArgs a) {
   }
 }
 
+// A block keeps a group of a sample: each channel's sites on `lanes` lanes of a wave, so that
+// a thread has accesses k of the channels pass rows + its row (entry e = pass per + k of E).
+// x (and dy) are read once, and no sums cross blocks but the weights' gradients.
+template <int V>
+struct WholePlace {
+  long n, g, c, site;  // of an entry: its channel in the group and its first site
+  int lanes, rows, row, lane, per;
+  __device__ __forceinline__ WholePlace(const GroupNormArgs& a, int on) : lanes(on) {
+    n = (long)blockIdx.x / a.groups;
+    g = (long)blockIdx.x - n * a.groups;
+    rows = blockDim.x / lanes;
+    row = threadIdx.x / lanes;
+    lane = threadIdx.x % lanes;
+    per = (int)((a.sites + lanes * V - 1) / (lanes * V));
+  }
+  // entry e: values of it that there are (<= 0: none)
+  __device__ __forceinline__ long at(const GroupNormArgs& a, int e) {
+    const int pass = e / per;
+    c = (long)pass * rows + row;
+    site = (long)((e - pass * per) * lanes + lane) * V;
+    return c < a.each ? a.sites - site : 0;
+  }
+  __device__ __forceinline__ long offset(const GroupNormArgs& a) const { return (g * a.each + c) * a.sites + site; }
+};
+
+template <typename T, int V, int ACT, int E>
+__global__ __launch_bounds__(kMostThreads) void k_first_whole_fwd(GroupNormArgs a, int lanes) {
+  __shared__ float red[2][kMostThreads / kWave];
+  WholePlace<V> p(a, lanes);
+  const T* x = static_cast<const T*>(a.x) + p.n * a.x_stride;
+  T* y = static_cast<T*>(a.y) + p.n * a.y_stride;
+  Held<T, V> v[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const long there = p.at(a, e);
+    v[e].load(x + p.offset(a), there);
+  }
+  float w[E], b[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const bool there = p.at(a, e) > 0;
+    w[e] = there ? weight_at<T>(a.w, a.wide, p.g * a.each + p.c, 1.f) : 0.f;
+    b[e] = there ? weight_at<T>(a.b, a.wide, p.g * a.each + p.c, 0.f) : 0.f;
+  }
+  const float size = (float)a.sites * (float)a.each;
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    v[e].refresh();
+#pragma unroll
+    for (int j = 0; j < V; ++j) s += v[e][j];  // (0 where there is none)
+  }
+  const float mean = block_sum(s, red[0]) / size;
+  s = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const long there = p.at(a, e);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float d = j < there ? v[e][j] - mean : 0.f;
+      s = fmaf(d, d, s);
+    }
+  }
+  const float rstd = 1.f / sqrtf(block_sum(s, red[1]) * (1.f / size) + a.eps);
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const long there = p.at(a, e);
+    Pack<T, V> o;
+#pragma unroll
+    for (int j = 0; j < V; ++j) o.v[j] = (T)act_of<ACT>(norm_z(v[e][j], mean, rstd, w[e], b[e]));
+    store_part(y + p.offset(a), there, o);
+  }
+  if (a.stats && threadIdx.x == 0) {
+    a.stats[blockIdx.x] = mean;
+    a.stats[a.batch * a.groups + blockIdx.x] = rstd;
+  }
+}
+
+template <typename T, int V, int ACT, int E>
+__global__ __launch_bounds__(kMostThreads) void k_first_whole_bwd(GroupNormArgs a, int lanes) {
+  extern __shared__ float chan[];  // [each][2]: sums of dz and of dz h
+  __shared__ float both[2];
+  WholePlace<V> p(a, lanes);
+  const T* x = static_cast<const T*>(a.x) + p.n * a.x_stride;
+  const T* dy = static_cast<const T*>(a.dy) + p.n * a.y_stride;
+  T* dx = static_cast<T*>(a.dx) + p.n * a.x_stride;
+  Held<T, V> v[E], d[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const long there = p.at(a, e);
+    v[e].load(x + p.offset(a), there);
+    d[e].load(dy + p.offset(a), there);
+  }
+  const float mean = a.stats[blockIdx.x], rstd = a.stats[a.batch * a.groups + blockIdx.x];
+  float w[E], b[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const bool there = p.at(a, e) > 0;
+    w[e] = there ? weight_at<T>(a.w, a.wide, p.g * a.each + p.c, 1.f) : 0.f;
+    b[e] = there ? weight_at<T>(a.b, a.wide, p.g * a.each + p.c, 0.f) : 0.f;
+  }
+  float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const long there = p.at(a, e);
+    v[e].refresh();
+    d[e].refresh();
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float dz = act_grad<ACT>(norm_z(v[e][j], mean, rstd, w[e], b[e]), d[e][j]), h = (v[e][j] - mean) * rstd;
+      s1 += j < there ? dz : 0.f;
+      s2 = j < there ? fmaf(dz, h, s2) : s2;
+    }
+    v[e].refresh();
+    d[e].refresh();
+    if ((e + 1) % p.per == 0) {  // the channel's last
+      s1 = wave_sum(s1, lanes);
+      s2 = wave_sum(s2, lanes);
+      if (p.lane == 0 && p.c < a.each) chan[2 * p.c] = s1, chan[2 * p.c + 1] = s2;
+      s1 = s2 = 0.f;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < kWave) {
+#pragma clang fp contract(off)
+    float c1 = 0.f, c2 = 0.f;
+    for (long c = threadIdx.x; c < a.each; c += kWave) {
+      const long at = p.g * a.each + c;
+      a.own[(p.n * a.channels + at) * 2] = chan[2 * c];
+      a.own[(p.n * a.channels + at) * 2 + 1] = chan[2 * c + 1];
+      const float wc = weight_at<T>(a.w, a.wide, at, 1.f);
+      c1 += wc * chan[2 * c];
+      c2 += wc * chan[2 * c + 1];
+    }
+    c1 = wave_sum(c1);
+    c2 = wave_sum(c2);
+    if (threadIdx.x == 0) {
+      const float size = (float)a.sites * (float)a.each;
+      both[0] = c1 / size;
+      both[1] = c2 / size;
+    }
+  }
+  __syncthreads();
+  const float c1 = both[0], c2 = both[1];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const long there = p.at(a, e);
+    Pack<T, V> o;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float dz = act_grad<ACT>(norm_z(v[e][j], mean, rstd, w[e], b[e]), d[e][j]);
+      o.v[j] = (T)norm_grad(dz, w[e], c1, (v[e][j] - mean) * rstd, c2, rstd);
+    }
+    store_part(dx + p.offset(a), there, o);
+  }
+}
+
 // go(T, V) of a plan.
 template <typename Go>
 void dispatch(const bl_group_norm_plan_s* p, Go&& go) {
@@ -206,9 +363,38 @@ dim3 grid_of(const GroupNormArgs& a) {
 
 }  // namespace
 
+void gnorm_first_whole(bl_group_norm_plan_s* p) {
+  const bl_group_norm_desc_t& d = p->d;
+  const long vec = 16 / dtype_bytes(d.dtype);
+  int lanes = kWave;
+  while (lanes > 1 && lanes / 2 * vec >= d.sites) lanes /= 2;
+  const long per = (d.sites + lanes * vec - 1) / (lanes * vec);
+  p->whole_lanes = lanes;
+  p->whole_tiles = (int)d.groups;
+  for (int i = 0; i < 2; ++i) {
+    // the fewest threads that have a few accesses each
+    for (int threads = kWave; threads <= kMostThreads && !p->whole_threads[i]; threads *= 2) {
+      const long rows = threads / lanes, each = (p->each + rows - 1) / rows * per;
+      if (each <= (threads < kMostThreads ? 4 : kMostEach)) p->whole_threads[i] = threads, p->whole_each[i] = (int)each;
+    }
+  }
+}
+
 bl_status_t gnorm_first_forward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s) {
   const dim3 grid = grid_of(a), block(kThreads);
   const double bytes = (double)a.batch * a.sites * a.channels * dtype_bytes(p->d.dtype);
+  if (p->whole_threads[0])
+    return timed_launch("gnorm_fwd", 2.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+      with_act(p->d.act, [&](auto act) {
+        with_each(p->whole_each[0], [&](auto e) {
+          dispatch(p, [&](auto t, auto v) {
+            hipExtLaunchKernelGGL((k_first_whole_fwd<decltype(t), decltype(v)::value, decltype(act)::value, decltype(e)::value>),
+                                  dim3((unsigned)(a.batch * a.groups)), dim3(p->whole_threads[0]), 0, s, e0, e1, 0, a,
+                                  p->whole_lanes);
+          });
+        });
+      });
+    });
   bl_status_t st = timed_launch("gnorm_part", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
     dispatch(p, [&](auto t, auto v) {
       hipExtLaunchKernelGGL((k_first_part<decltype(t), decltype(v)::value>), grid, block, 0, s, e0, e1, 0, a);
@@ -229,6 +415,20 @@ bl_status_t gnorm_first_forward(const bl_group_norm_plan_s* p, const GroupNormAr
 bl_status_t gnorm_first_backward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s) {
   const dim3 grid = grid_of(a), block(kThreads);
   const double bytes = (double)a.batch * a.sites * a.channels * dtype_bytes(p->d.dtype);
+  if (p->whole_threads[1]) {
+    const bl_status_t st = timed_launch("gnorm_bwd", 3.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+      with_act(p->d.act, [&](auto act) {
+        with_each(p->whole_each[1], [&](auto e) {
+          dispatch(p, [&](auto t, auto v) {
+            hipExtLaunchKernelGGL((k_first_whole_bwd<decltype(t), decltype(v)::value, decltype(act)::value, decltype(e)::value>),
+                                  dim3((unsigned)(a.batch * a.groups)), dim3(p->whole_threads[1]),
+                                  (unsigned)(p->each * 2 * sizeof(float)), s, e0, e1, 0, a, p->whole_lanes);
+          });
+        });
+      });
+    });
+    return st == BL_OK ? gnorm_weights(a, p->d.dtype, s) : st;
+  }
   bl_status_t st = timed_launch("gnorm_bwd_part", 2.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
     with_act(p->d.act, [&](auto act) {
       dispatch(p, [&](auto t, auto v) {

@@ -3,12 +3,15 @@
 // A thread keeps an access of channels (`vec` of them, a divisor of their number) and walks
 // sites, so that neighbouring threads read neighbouring memory whatever the channels'
 // number, and what belongs to its channels (weights, statistics) stays in registers.
+#include <algorithm>
+
 #include "gnorm.hpp"
 
 namespace blc {
 namespace {
 
-constexpr int kAhead = 4;  // sites of a thread whose loads are in flight together
+constexpr int kAhead = 8;      // sites of a thread whose loads are in flight together
+constexpr int kAheadBoth = 4;  // backward, of x and dy
 
 // Where a thread stands: sample, chunk, its first channel and its sites begin, begin +
 // slices, ...
@@ -141,16 +144,16 @@ __global__ __launch_bounds__(kThreads) void k_last_bwd_part(GroupNormArgs a) {
   LastChannels<T, V> own;
   own.load(a, p);
   float s[2 * V] = {};
-  for (long t = p.begin; t < p.end; t += (long)kAhead * p.slices) {
-    Held<T, V> v[kAhead], g[kAhead];
+  for (long t = p.begin; t < p.end; t += (long)kAheadBoth * p.slices) {
+    Held<T, V> v[kAheadBoth], g[kAheadBoth];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
+    for (int k = 0; k < kAheadBoth; ++k) {
       const long site = t + (long)k * p.slices;
       v[k].load(x + site * a.channels, site < p.end ? V : 0);
       g[k].load(dy + site * a.channels, site < p.end ? V : 0);
     }
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
+    for (int k = 0; k < kAheadBoth; ++k) {
       v[k].refresh();
       g[k].refresh();
       if (t + (long)k * p.slices >= p.end) continue;
@@ -194,16 +197,16 @@ __global__ __launch_bounds__(kThreads) void k_last_bwd_apply(GroupNormArgs a) {
     c1[j] = a.sums[2 * q];
     c2[j] = a.sums[2 * q + 1];
   }
-  for (long t = p.begin; t < p.end; t += (long)kAhead * p.slices) {
-    Held<T, V> v[kAhead], g[kAhead];
+  for (long t = p.begin; t < p.end; t += (long)kAheadBoth * p.slices) {
+    Held<T, V> v[kAheadBoth], g[kAheadBoth];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
+    for (int k = 0; k < kAheadBoth; ++k) {
       const long site = t + (long)k * p.slices;
       v[k].load(x + site * a.channels, site < p.end ? V : 0);
       g[k].load(dy + site * a.channels, site < p.end ? V : 0);
     }
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
+    for (int k = 0; k < kAheadBoth; ++k) {
       const long site = t + (long)k * p.slices;
       v[k].refresh();
       g[k].refresh();
@@ -216,6 +219,221 @@ __global__ __launch_bounds__(kThreads) void k_last_bwd_apply(GroupNormArgs a) {
       if (site < p.end) store_pack(dx + site * a.channels, o);
     }
   }
+}
+
+// A block keeps all sites of a tile of whole groups of a sample: accesses of V channels on
+// `lanes` lanes (any number), sites on the other threads' slices, E of them each.  x (and dy)
+// are read once, and no sums cross blocks but the weights' gradients.
+template <int V>
+struct WholePlace {
+  long n, first, c;  // sample, tile's first channel, this thread's in the tile
+  int width, lanes, slices, slice;  // width: channels of the tile that there are
+  bool there;
+  __device__ __forceinline__ WholePlace(const GroupNormArgs& a, int on, int tiles) : lanes(on) {
+    n = (long)blockIdx.x / tiles;
+    first = ((long)blockIdx.x - n * tiles) * lanes * V;
+    width = (int)min((long)lanes * V, a.channels - first);
+    slices = blockDim.x / lanes;
+    slice = threadIdx.x / lanes;
+    c = (threadIdx.x - slice * lanes) * V;
+    there = slice < slices && c < width;
+  }
+  __device__ __forceinline__ bool site(const GroupNormArgs& a, int e, long& at) const {
+    at = (long)e * slices + slice;
+    return there && at < a.sites;
+  }
+};
+// Sums over slices and a group's channels of what each thread has for its channels, a wave a
+// group: sums[g] of the tile's groups.  all: [slices][lanes V].
+template <int V>
+__device__ __forceinline__ void group_sums(const GroupNormArgs& a, const WholePlace<V>& p, const float (&x)[V], float* all,
+                                           float* sums) {
+  const int row = p.lanes * V, each = (int)a.each;
+  __syncthreads();  // (what was there has been read)
+  if (p.slice < p.slices)
+#pragma unroll
+    for (int j = 0; j < V; ++j) all[p.slice * row + p.c + j] = p.there ? x[j] : 0.f;
+  __syncthreads();
+  const unsigned lane = threadIdx.x % kWave, waves = blockDim.x / kWave;
+  for (unsigned g = threadIdx.x / kWave; g < (unsigned)(p.width / each); g += waves) {
+    float s = 0.f;
+    for (unsigned i = lane; i < (unsigned)(p.slices * each); i += kWave) {
+      const unsigned k = i / (unsigned)each;
+      s += all[k * row + g * each + (i - k * each)];
+    }
+    s = wave_sum(s);
+    if (lane == 0) sums[g] = s;
+  }
+  __syncthreads();
+}
+
+template <typename T, int V, int ACT, int E>
+__global__ __launch_bounds__(kMostThreads) void k_last_whole_fwd(GroupNormArgs a, int lanes, int tiles) {
+  extern __shared__ float all[];  // [slices][lanes V], then the groups' sums
+  const WholePlace<V> p(a, lanes, tiles);
+  float* sums = all + p.slices * lanes * V;
+  const T* x = static_cast<const T*>(a.x) + p.n * a.x_stride + p.first + p.c;
+  T* y = static_cast<T*>(a.y) + p.n * a.y_stride + p.first + p.c;
+  Held<T, V> v[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    long at;
+    const bool there = p.site(a, e, at);
+    v[e].load(x + at * a.channels, there ? V : 0);
+  }
+  float w[V], b[V], s[V] = {};
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const long c = p.first + (p.there ? p.c + j : 0);
+    w[j] = weight_at<T>(a.w, a.wide, c, 1.f);
+    b[j] = weight_at<T>(a.b, a.wide, c, 0.f);
+  }
+  int group[V];  // of the tile
+#pragma unroll
+  for (int j = 0; j < V; ++j) group[j] = p.there ? (int)(p.c + j) / (int)a.each : 0;
+  const float size = (float)a.sites * (float)a.each, inv = 1.f / size;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    v[e].refresh();
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] += v[e][j];  // (0 where there is none)
+  }
+  group_sums<V>(a, p, s, all, sums);
+  float mean[V], rstd[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) mean[j] = sums[group[j]] / size, s[j] = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    long at;
+    const bool there = p.site(a, e, at);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float d = there ? v[e][j] - mean[j] : 0.f;
+      s[j] = fmaf(d, d, s[j]);
+    }
+  }
+  group_sums<V>(a, p, s, all, sums);
+#pragma unroll
+  for (int j = 0; j < V; ++j) rstd[j] = 1.f / sqrtf(sums[group[j]] * inv + a.eps);
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    long at;
+    if (!p.site(a, e, at)) continue;
+    Pack<T, V> o;
+#pragma unroll
+    for (int j = 0; j < V; ++j) o.v[j] = (T)act_of<ACT>(norm_z(v[e][j], mean[j], rstd[j], w[j], b[j]));
+    store_pack(y + at * a.channels, o);
+  }
+  if (a.stats && p.slice == 0 && p.there)
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const long q = p.n * a.groups + (p.first + p.c + j) / a.each;
+      if ((p.c + j) % a.each == 0) a.stats[q] = mean[j], a.stats[a.batch * a.groups + q] = rstd[j];
+    }
+}
+
+template <typename T, int V, int ACT, int E>
+__global__ __launch_bounds__(kMostThreads) void k_last_whole_bwd(GroupNormArgs a, int lanes, int tiles) {
+  extern __shared__ float all[];  // [slices][lanes V], then [lanes V][2] of channels and [groups][2]
+  const WholePlace<V> p(a, lanes, tiles);
+  const int row = lanes * V, each = (int)a.each;
+  float *chan = all + p.slices * row, *sums = chan + 2 * row;
+  const T* x = static_cast<const T*>(a.x) + p.n * a.x_stride + p.first + p.c;
+  const T* dy = static_cast<const T*>(a.dy) + p.n * a.y_stride + p.first + p.c;
+  T* dx = static_cast<T*>(a.dx) + p.n * a.x_stride + p.first + p.c;
+  Held<T, V> v[E], d[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    long at;
+    const bool there = p.site(a, e, at);
+    v[e].load(x + at * a.channels, there ? V : 0);
+    d[e].load(dy + at * a.channels, there ? V : 0);
+  }
+  float w[V], b[V], mean[V], rstd[V], s[2][V] = {};
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const long c = p.first + (p.there ? p.c + j : 0), q = p.n * a.groups + c / a.each;
+    mean[j] = a.stats[q];
+    rstd[j] = a.stats[a.batch * a.groups + q];
+    w[j] = weight_at<T>(a.w, a.wide, c, 1.f);
+    b[j] = weight_at<T>(a.b, a.wide, c, 0.f);
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    v[e].refresh();
+    d[e].refresh();
+    long at;
+    const bool there = p.site(a, e, at);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float h = (v[e][j] - mean[j]) * rstd[j];
+      const float dz = act_grad<ACT>(norm_z(v[e][j], mean[j], rstd[j], w[j], b[j]), d[e][j]);
+      s[0][j] += there ? dz : 0.f;
+      s[1][j] = there ? fmaf(dz, h, s[1][j]) : s[1][j];
+    }
+    v[e].refresh();
+    d[e].refresh();
+  }
+  // over the slices: a thread a channel
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (k) __syncthreads();
+    if (p.slice < p.slices)
+#pragma unroll
+      for (int j = 0; j < V; ++j) all[p.slice * row + p.c + j] = p.there ? s[k][j] : 0.f;
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.width; c += blockDim.x) {
+      float sum = 0.f;
+      for (int i = 0; i < p.slices; ++i) sum += all[i * row + c];
+      chan[2 * c + k] = sum;
+      a.own[(p.n * a.channels + p.first + c) * 2 + k] = sum;
+    }
+  }
+  __syncthreads();
+  {
+#pragma clang fp contract(off)
+    const unsigned lane = threadIdx.x % kWave, waves = blockDim.x / kWave;
+    const float size = (float)a.sites * (float)a.each;
+    for (unsigned g = threadIdx.x / kWave; g < (unsigned)(p.width / each); g += waves) {
+      float c1 = 0.f, c2 = 0.f;
+      for (int c = lane; c < each; c += kWave) {
+        const int at = g * each + c;
+        const float wc = weight_at<T>(a.w, a.wide, p.first + at, 1.f);
+        c1 += wc * chan[2 * at];
+        c2 += wc * chan[2 * at + 1];
+      }
+      c1 = wave_sum(c1);
+      c2 = wave_sum(c2);
+      if (lane == 0) sums[2 * g] = c1 / size, sums[2 * g + 1] = c2 / size;
+    }
+  }
+  __syncthreads();
+  float c1[V], c2[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int g = p.there ? (int)(p.c + j) / each : 0;
+    c1[j] = sums[2 * g];
+    c2[j] = sums[2 * g + 1];
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    long at;
+    if (!p.site(a, e, at)) continue;
+    Pack<T, V> o;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float dz = act_grad<ACT>(norm_z(v[e][j], mean[j], rstd[j], w[j], b[j]), d[e][j]);
+      o.v[j] = (T)norm_grad(dz, w[j], c1[j], (v[e][j] - mean[j]) * rstd[j], c2[j], rstd[j]);
+    }
+    store_pack(dx + at * a.channels, o);
+  }
+}
+
+// Bytes of LDS of a block.
+unsigned whole_lds(const bl_group_norm_plan_s* p, bool backward) {
+  const long row = (long)p->whole_lanes * p->vec, slices = p->whole_threads[backward] / p->whole_lanes;
+  const long groups = std::max<long>(1, row / p->each);
+  return (unsigned)((slices * row + (backward ? 2 * row + 2 * groups : groups)) * sizeof(float));
 }
 
 // go(T, V) of a plan.
@@ -237,9 +455,42 @@ void dispatch(const bl_group_norm_plan_s* p, Go&& go) {
 
 }  // namespace
 
+void gnorm_last_whole(bl_group_norm_plan_s* p) {
+  const bl_group_norm_desc_t& d = p->d;
+  // whole groups and whole accesses, in lines of 128 bytes where there are as many
+  long step = p->each;
+  while (step % p->vec) step += p->each;
+  long width = step;
+  while (width < d.channels && (width + step) * dtype_bytes(d.dtype) <= 128) width += step;
+  const long lanes = width / p->vec;
+  if (lanes > kThreads) return;
+  p->whole_lanes = (int)lanes;
+  p->whole_tiles = (int)((d.channels + width - 1) / width);
+  for (int i = 0; i < 2; ++i) {
+    // the fewest threads that have a few accesses each
+    for (int threads = kWave; threads <= kMostThreads && !p->whole_threads[i]; threads *= 2) {
+      if (lanes > threads) continue;
+      const long slices = threads / lanes, each = (d.sites + slices - 1) / slices;
+      if (each <= (threads < kMostThreads ? 4 : kMostEach)) p->whole_threads[i] = threads, p->whole_each[i] = (int)each;
+    }
+  }
+}
+
 bl_status_t gnorm_last_forward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(a.batch * a.chunks * a.tiles)), block(kThreads);
   const double bytes = (double)a.batch * a.sites * a.channels * dtype_bytes(p->d.dtype);
+  if (p->whole_threads[0])
+    return timed_launch("gnorm_fwd", 2.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+      with_act(p->d.act, [&](auto act) {
+        with_each(p->whole_each[0], [&](auto e) {
+          dispatch(p, [&](auto t, auto v) {
+            hipExtLaunchKernelGGL((k_last_whole_fwd<decltype(t), decltype(v)::value, decltype(act)::value, decltype(e)::value>),
+                                  dim3((unsigned)(a.batch * p->whole_tiles)), dim3(p->whole_threads[0]),
+                                  whole_lds(p, false), s, e0, e1, 0, a, p->whole_lanes, p->whole_tiles);
+          });
+        });
+      });
+    });
   bl_status_t st = timed_launch("gnorm_part", bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
     dispatch(p, [&](auto t, auto v) {
       hipExtLaunchKernelGGL((k_last_part<decltype(t), decltype(v)::value>), grid, block, 0, s, e0, e1, 0, a);
@@ -260,6 +511,20 @@ bl_status_t gnorm_last_forward(const bl_group_norm_plan_s* p, const GroupNormArg
 bl_status_t gnorm_last_backward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(a.batch * a.chunks * a.tiles)), block(kThreads);
   const double bytes = (double)a.batch * a.sites * a.channels * dtype_bytes(p->d.dtype);
+  if (p->whole_threads[1]) {
+    const bl_status_t st = timed_launch("gnorm_bwd", 3.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+      with_act(p->d.act, [&](auto act) {
+        with_each(p->whole_each[1], [&](auto e) {
+          dispatch(p, [&](auto t, auto v) {
+            hipExtLaunchKernelGGL((k_last_whole_bwd<decltype(t), decltype(v)::value, decltype(act)::value, decltype(e)::value>),
+                                  dim3((unsigned)(a.batch * p->whole_tiles)), dim3(p->whole_threads[1]),
+                                  whole_lds(p, true), s, e0, e1, 0, a, p->whole_lanes, p->whole_tiles);
+          });
+        });
+      });
+    });
+    return st == BL_OK ? gnorm_weights(a, p->d.dtype, s) : st;
+  }
   bl_status_t st = timed_launch("gnorm_bwd_part", 2.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
     with_act(p->d.act, [&](auto act) {
       dispatch(p, [&](auto t, auto v) {
