@@ -28,12 +28,14 @@ __global__ __launch_bounds__(kThreads) void k_gnorm_join_fwd(GroupNormArgs a) {
   const unsigned entries = (unsigned)(a.each * a.chunks), lane = threadIdx.x % kWave;
   const float inv = 1.f / ((float)a.sites * (float)a.each);
   float sum = 0.f, m2 = 0.f;
+#pragma unroll 4
   for (unsigned i = lane; i < entries; i += kWave) {
     float sites;
     const float* v = part_at(a, n, g, i, sites);
     sum = fmaf(sites, v[0], sum);
   }
   const float mean = wave_sum(sum) / ((float)a.sites * (float)a.each);
+#pragma unroll 4
   for (unsigned i = lane; i < entries; i += kWave) {
     float sites;
     const float* v = part_at(a, n, g, i, sites);
@@ -64,10 +66,11 @@ __global__ __launch_bounds__(kThreads) void k_gnorm_join_bwd(GroupNormArgs a) {
     const unsigned c = first + lane / on;
     float dz = 0.f, dh = 0.f;
     if (c < (unsigned)a.each)
+#pragma unroll 8
       for (unsigned k = lane % on; k < (unsigned)a.chunks; k += on) {
-        const float* v = a.part + (((n * a.chunks + k) * a.channels) + g * a.each + c) * 2;
-        dz += v[0];
-        dh += v[1];
+        const Pack<float, 2> v = load_pack<float, 2>(a.part + (((n * a.chunks + k) * a.channels) + g * a.each + c) * 2);
+        dz += v.v[0];
+        dh += v.v[1];
       }
     dz = wave_sum(dz, (int)on);
     dh = wave_sum(dh, (int)on);
@@ -88,34 +91,9 @@ __global__ __launch_bounds__(kThreads) void k_gnorm_join_bwd(GroupNormArgs a) {
   a.sums[2 * q + 1] = s2 / size;
 }
 
-// dw and db: 64 channels and four slices of the samples a block.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_gnorm_weights(GroupNormArgs a) {
-  constexpr int kSlices = kThreads / kWave;
-  __shared__ float red[2][kSlices][kWave];
-  const int col = threadIdx.x % kWave, slice = threadIdx.x / kWave;
-  const long c = (long)blockIdx.x * kWave + col;
-  float db = 0.f, dw = 0.f;
-  if (c < a.channels)
-    for (long n = slice; n < a.batch; n += kSlices) {
-      db += a.own[(n * a.channels + c) * 2];
-      dw += a.own[(n * a.channels + c) * 2 + 1];
-    }
-  red[0][slice][col] = db;
-  red[1][slice][col] = dw;
-  __syncthreads();
-  if (slice || c >= a.channels) return;
-  db = dw = 0.f;
-#pragma unroll
-  for (int k = 0; k < kSlices; ++k) db += red[0][k][col], dw += red[1][k][col];
-  if (a.dw) {
-    if (a.wide) static_cast<float*>(a.dw)[c] = dw;
-    else static_cast<T*>(a.dw)[c] = (T)dw;
-  }
-  if (a.db) {
-    if (a.wide) static_cast<float*>(a.db)[c] = db;
-    else static_cast<T*>(a.db)[c] = (T)db;
-  }
+  gnorm_weights_block<T>(a, blockIdx.x);
 }
 
 unsigned blocks_for(long n, long each) { return (unsigned)((n + each - 1) / each); }
@@ -163,7 +141,7 @@ bl_status_t gnorm_join_backward(const GroupNormArgs& a, int dtype, hipStream_t s
 bl_status_t gnorm_weights(const GroupNormArgs& a, int dtype, hipStream_t s) {
   if (!a.dw && !a.db) return BL_OK;
   return timed_launch("gnorm_weights", 8.0 * a.batch * a.channels, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
-    const dim3 grid(blocks_for(a.channels, kWave));
+    const dim3 grid(gnorm_weights_blocks(a));
     if (dtype == BL_F16) hipExtLaunchKernelGGL(k_gnorm_weights<f16_t>, grid, dim3(kThreads), 0, s, e0, e1, 0, a);
     else hipExtLaunchKernelGGL(k_gnorm_weights<bf16_t>, grid, dim3(kThreads), 0, s, e0, e1, 0, a);
   });

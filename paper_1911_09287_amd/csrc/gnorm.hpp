@@ -109,7 +109,8 @@ struct Moments {
   float n, mean, m2;
 };
 __device__ __forceinline__ void moments_join(Moments& a, const Moments& b) {
-  const float n = a.n + b.n, d = b.mean - a.mean, share = n > 0.f ? b.n / n : 0.f;
+  // (joined to nothing b stays as it is: a group of one value is its own mean)
+  const float n = a.n + b.n, d = b.mean - a.mean, share = a.n == 0.f ? 1.f : b.n * __builtin_amdgcn_rcpf(n);
   a.mean = fmaf(d, share, a.mean);
   a.m2 += fmaf(d * d, a.n * share, b.m2);
   a.n = n;
@@ -125,7 +126,43 @@ void gnorm_first_whole(bl_group_norm_plan_s* p);
 // Statistics from the parts; backward: means over groups and sums over samples from theirs.
 bl_status_t gnorm_join_forward(const GroupNormArgs& a, hipStream_t s);
 bl_status_t gnorm_join_backward(const GroupNormArgs& a, int dtype, hipStream_t s);
-// dw and db from the samples' sums (batch = 0: zeros).
+// dw and db from the samples' sums (batch = 0: zeros); as a launch of its own, or by the blocks
+// of another one past its own, of kThreads threads.
+constexpr int kWeightSlices = kThreads / kWave;
+template <typename T>
+__device__ __forceinline__ void gnorm_weights_block(const GroupNormArgs& a, unsigned block) {
+  __shared__ float red[2][kWeightSlices][kWave];
+  const int col = threadIdx.x % kWave, slice = threadIdx.x / kWave;
+  const long c = (long)block * kWave + col;
+  float db = 0.f, dw = 0.f;
+  if (c < a.channels) {
+    const float* from = a.own + c * 2;
+#pragma unroll 8
+    for (long n = slice; n < a.batch; n += kWeightSlices) {
+      const Pack<float, 2> v = load_pack<float, 2>(from + n * a.channels * 2);
+      db += v.v[0];
+      dw += v.v[1];
+    }
+  }
+  red[0][slice][col] = db;
+  red[1][slice][col] = dw;
+  __syncthreads();
+  if (slice || c >= a.channels) return;
+  db = dw = 0.f;
+#pragma unroll
+  for (int k = 0; k < kWeightSlices; ++k) db += red[0][k][col], dw += red[1][k][col];
+  if (a.dw) {
+    if (a.wide) static_cast<float*>(a.dw)[c] = dw;
+    else static_cast<T*>(a.dw)[c] = (T)dw;
+  }
+  if (a.db) {
+    if (a.wide) static_cast<float*>(a.db)[c] = db;
+    else static_cast<T*>(a.db)[c] = (T)db;
+  }
+}
+inline unsigned gnorm_weights_blocks(const GroupNormArgs& a) {
+  return a.dw || a.db ? (unsigned)((a.channels + kWave - 1) / kWave) : 0;
+}
 bl_status_t gnorm_weights(const GroupNormArgs& a, int dtype, hipStream_t s);
 
 // go(act) as a constant.

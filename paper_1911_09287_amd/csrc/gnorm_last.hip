@@ -183,7 +183,11 @@ __global__ __launch_bounds__(kThreads) void k_last_bwd_part(GroupNormArgs a) {
 }
 
 template <typename T, int V, int ACT>
-__global__ __launch_bounds__(kThreads) void k_last_bwd_apply(GroupNormArgs a) {
+__global__ __launch_bounds__(kThreads) void k_last_bwd_apply(GroupNormArgs a, unsigned blocks) {
+  if (blockIdx.x >= blocks) {
+    gnorm_weights_block<T>(a, blockIdx.x - blocks);
+    return;
+  }
   const LastPlace p = LastPlace::make<V>(a);
   const T* x = static_cast<const T*>(a.x) + p.n * a.x_stride + p.c;
   const T* dy = static_cast<const T*>(a.dy) + p.n * a.y_stride + p.c;
@@ -535,15 +539,15 @@ bl_status_t gnorm_last_backward(const bl_group_norm_plan_s* p, const GroupNormAr
   });
   if (st == BL_OK) st = gnorm_join_backward(a, p->d.dtype, s);
   if (st != BL_OK) return st;
-  st = timed_launch("gnorm_bwd", 3.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+  // (the blocks past the values' own sum the weights' gradients)
+  return timed_launch("gnorm_bwd", 3.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
     with_act(p->d.act, [&](auto act) {
       dispatch(p, [&](auto t, auto v) {
-        hipExtLaunchKernelGGL((k_last_bwd_apply<decltype(t), decltype(v)::value, decltype(act)::value>), grid, block, 0,
-                              s, e0, e1, 0, a);
+        hipExtLaunchKernelGGL((k_last_bwd_apply<decltype(t), decltype(v)::value, decltype(act)::value>),
+                              dim3(grid.x + gnorm_weights_blocks(a)), block, 0, s, e0, e1, 0, a, grid.x);
       });
     });
   });
-  return st == BL_OK ? gnorm_weights(a, p->d.dtype, s) : st;
 }
 
 }  // namespace blc
