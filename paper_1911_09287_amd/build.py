@@ -15,7 +15,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["plan.cpp", "api.hip", "tables.hip", "direct.hip", "bluestein.hip", "fft2d.hip", "mdft.hip", "pgemm.hip", "contract.hip", "thin.hip", "energy.hip", "topk.hip", "small.hip",
            "norm.hip", "norm_rows.hip", "norm_maps.hip", "logprob.hip", "adamw.hip",
-           "gnorm.hip", "gnorm_last.hip", "gnorm_first.hip", "recur.hip", "recur_bwd.hip", "muon.hip", "muon_gemm.hip"]
+           "gnorm.hip", "gnorm_last.hip", "gnorm_first.hip", "recur.hip", "recur_bwd.hip", "muon.hip", "muon_gemm.hip",
+           "muon_small.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950",

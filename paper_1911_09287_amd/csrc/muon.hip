@@ -20,11 +20,6 @@
 namespace blc {
 namespace {
 
-// u of four elements from their gradients and (new) momenta.
-__device__ __forceinline__ float update_of(float g, float m, float gs, const MuonArgs& a) {
-  return !a.momentum ? gs * g : a.nesterov ? fmaf(a.beta, m, gs * g) : m;
-}
-
 // Sum over a block, in each thread.
 __device__ __forceinline__ double block_sum(double sum, double (&red)[kThreads / kWave]) {
   for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
@@ -64,7 +59,7 @@ __global__ __launch_bounds__(kThreads) void k_muon_momentum(MuonList list, MuonA
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       next.v[j] = fmaf(a.beta, mv[k][j], gs * gv[k][j]);
-      const double u = update_of(gv[k][j], next.v[j], gs, a);  // (0 where there is none)
+      const double u = muon_update_of(gv[k][j], next.v[j], gs, a);  // (0 where there is none)
       sum = fma(u, u, sum);
     }
     if (m) store_part(m + k * kThreads * 4, size - from - k * kThreads * 4, next);
@@ -124,7 +119,7 @@ __global__ __launch_bounds__(kThreads) void k_muon_lay(MuonList list, MuonSlabs 
     for (int j = 0; j < 4; ++j) {
       const int r = k * 16 + threadIdx.x / 16;
       const bool there = r0 + r < it.rows && c + j < cols;
-      tile[r * kLayRow + threadIdx.x % 16 * 4 + j] = there ? (float)((double)update_of(gv[k][j], mv[k][j], gs, a) * inv) : 0.f;
+      tile[r * kLayRow + threadIdx.x % 16 * 4 + j] = there ? (float)((double)muon_update_of(gv[k][j], mv[k][j], gs, a) * inv) : 0.f;
     }
   }
   __syncthreads();
@@ -197,6 +192,18 @@ bl_status_t run(const bl_muon_plan_s* p, void* const* out, const void* const* gr
       poly += 3.0 * m * m * m;
       apply += 6.0 * m * m * n;
       values += (double)m * n;
+    }
+    if (p->small) {
+      MuonSmallSteps small{};
+      small.count = (int)p->joined.size();
+      for (int k = 0; k < small.count; ++k) {
+        const auto& step = p->joined[k];
+        small.step[k] = {(float)(step.a * step.hold_b), (float)(step.b * step.hold_b / kHoldA),
+                         (float)(step.c * step.hold_b / ((double)kHoldA * kHoldA)), step.hold_b, step.hold_q, step.first, step.last};
+      }
+      const bl_status_t st = muon_small(p->param_dtype, p->grad_dtype, list, small, a, 5.0 * (gram + poly + apply), s);
+      if (st != BL_OK) return st;
+      continue;
     }
     // first[] of a launch whose blocks of matrix k are blocks(k); how many there are
     auto lay = [&](unsigned* first, auto&& blocks) {
@@ -380,6 +387,11 @@ extern "C" bl_status_t bl_muon_plan_create(bl_muon_plan_t* out, const bl_muon_de
       single += count * mm * (3.0 * n + m);
       joined += runs * mm * 3.0 * n + mm * m * (count + 3.0 * (count - runs));
       tiles[n >= 2 * m] += (unsigned long long)((m + 1) / 2) * ((m + 1) / 2 + 1) / 2;
+    }
+    p->small = true;
+    for (int i : order) {
+      const auto& x = p->matrices[i];
+      p->small &= std::min(x.rows, x.cols) <= kSmallShort && std::max(x.rows, x.cols) <= kSmallLong;
     }
     const bool apart = tiles[0] >= kFillSquare && tiles[1] >= kFillSquare;
     if (apart)

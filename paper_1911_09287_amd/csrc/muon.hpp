@@ -63,6 +63,17 @@ struct MuonProduct {
   int turn;          // apply: which of X's two transposes is read
 };
 
+// The steps of a launch that takes whole matrices (a, b, c as in a product's launch).
+struct MuonSmallSteps {
+  struct Step {
+    float a, b, c, hold_b, hold_q;
+    int first, last;
+  };
+  int count;
+  Step step[kMuonSteps];
+};
+constexpr long long kSmallShort = 64, kSmallLong = 1024;  // sides of the matrices it takes
+
 }  // namespace blc
 
 struct bl_muon_plan_s {
@@ -88,6 +99,7 @@ struct bl_muon_plan_s {
   };
   std::vector<Matrix> matrices;
   std::vector<Step> single, joined;
+  bool small;  // a block takes a matrix
   std::vector<Batch> batches;
   int param_dtype, grad_dtype;
   long long total;
@@ -133,6 +145,34 @@ __device__ __forceinline__ unsigned muon_dither(unsigned long long place, unsign
   x ^= x >> 16;
   return (x * 0x6A09E667u) >> 16;
 }
+
+// u of an element from its gradient and (new) momentum.
+__device__ __forceinline__ float muon_update_of(float g, float m, float gs, const MuonArgs& a) {
+  return !a.momentum ? gs * g : a.nesterov ? fmaf(a.beta, m, gs * g) : m;
+}
+// The parameter from its old value and x of X, or x itself (set).
+template <typename P>
+__device__ __forceinline__ P muon_next(float old, float x, unsigned long long place, float keep, float rate, unsigned key,
+                                       bool set) {
+  if (set) return (P)x;
+  const float next = fmaf(-rate, x, old * keep);
+  if constexpr (sizeof(P) == 4) {
+    return next;
+  } else {
+    const unsigned bits = __float_as_uint(next);
+    const bool finite = (bits & 0x7F800000u) != 0x7F800000u;
+    const unsigned up = finite ? bits + muon_dither(place, key) : bits | (next != next ? 0x400000u : 0u);
+    return __builtin_bit_cast(bf16_t, (unsigned short)(up >> 16));
+  }
+}
+template <typename P>
+__device__ __forceinline__ void muon_put(P* p, size_t e, float x, unsigned long long start, float keep, float rate,
+                                         unsigned key, bool set) {
+  p[e] = muon_next<P>(set ? 0.f : to_f32(p[e]), x, start + e, keep, rate, key, set);
+}
+
+bl_status_t muon_small(int param_dtype, int grad_dtype, const MuonList& list, const MuonSmallSteps& steps,
+                       const MuonArgs& a, double flops, hipStream_t s);
 
 enum MuonMode { kGram, kPoly, kSquare, kApply };
 // side: of the tiles, 64 or 128.

@@ -316,7 +316,7 @@ __global__ __launch_bounds__(MuonShape<SIDE>::kThreads, MuonShape<SIDE>::kBlocks
   const unsigned long long start = (unsigned long long)it.start;
 #pragma unroll
   for (int tp = 0; tp < S::kSub; ++tp) {
-    P old[S::kSub * 16 / S::kGroups];
+    P old[S::kSub * 16 / S::kGroups] = {};
     auto each = [&](auto&& go) {  // go(old value, element, v) for all that there are
       int n = 0;
       sums.each_four(tp, [&](int row, int col, const float (&v)[4]) {
@@ -330,20 +330,7 @@ __global__ __launch_bounds__(MuonShape<SIDE>::kThreads, MuonShape<SIDE>::kBlocks
     // all old values are in flight before the first is used
     if (!a.set) each([&](P& o, size_t e, float) { o = param[e]; });
     each([&](P& o, size_t e, float v) {
-      const float x = v * q.scale;
-      if (a.set) {
-        param[e] = (P)x;
-        return;
-      }
-      const float next = fmaf(-rate, x, to_f32(o) * keep);
-      if constexpr (sizeof(P) == 4) {
-        param[e] = next;
-      } else {
-        const unsigned bits = __float_as_uint(next);
-        const bool finite = (bits & 0x7F800000u) != 0x7F800000u;
-        const unsigned up = finite ? bits + muon_dither(start + e, key) : bits | (next != next ? 0x400000u : 0u);
-        param[e] = __builtin_bit_cast(bf16_t, (unsigned short)(up >> 16));
-      }
+      param[e] = muon_next<P>(to_f32(o), v * q.scale, start + e, keep, rate, key, a.set);
     });
   }
 }

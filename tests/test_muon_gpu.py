@@ -113,6 +113,24 @@ def test_orthogonalize(torch, param, grad):
         within(out, want, err + half_ulp(param) * (want.norm().item() + err), f"{s} {param} {grad}")
 
 
+SMALL = [s for s in SHAPES if min(s) <= 64] + [(64, 1024), (1000, 63), (17, 16), (16, 64), (31, 33), (1, 1024), (2, 65)]
+
+
+@pytest.mark.parametrize("grad", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("param", ["f32", "bf16"])
+def test_orthogonalize_small(torch, param, grad):
+    # none has sides over 64 and 1024: a block takes a matrix
+    us = [gradient(torch, s, 100 + k).to(tdtype(torch, grad)) for k, s in enumerate(SMALL)]
+    plan = bltrain.MuonPlan(SMALL, param_dtype=tdtype(torch, param), grad_dtype=tdtype(torch, grad))
+    outs = [torch.full(s, float("nan"), dtype=tdtype(torch, param), device="cuda") for s in SMALL]
+    ws = plan.workspace()
+    ws.fill_(255)
+    plan.orthogonalize(plan.bind(outs, [u.cuda() for u in us]), ws, eps=1e-7)
+    for s, u, out in zip(SMALL, us, outs):
+        want, err = reference(torch, u, 1e-7)
+        within(out, want, err + half_ulp(param) * (want.norm().item() + err), f"{s} {param} {grad}")
+
+
 @pytest.mark.parametrize("shape", [(1024, 1030), (2000, 300), (64, 4097), (700, 1)])
 def test_orthogonalize_larger(torch, shape):
     u = gradient(torch, shape, 1)
@@ -205,10 +223,13 @@ def step_reference(t, p, g, m, shapes, starts, a, decay, scales, gs):
     return new_p, new_m, err
 
 
+@pytest.mark.parametrize("small", [False, True])
 @pytest.mark.parametrize("nesterov", [True, False])
 @pytest.mark.parametrize("param,grad", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f16")])
-def test_step(torch, param, grad, nesterov):
+def test_step(torch, param, grad, nesterov, small):
     shapes = [(1, 1), (64, 27), (130, 140), (5, 300), (300, 90), (128, 256)]
+    if small:
+        shapes = [(1, 1), (64, 27), (63, 64), (5, 300), (300, 9), (32, 256)]
     decay, scales = [True, False, True, True, False, True], None if nesterov else [1.0, 0.5, 2.0, 0.0, 1.5, 0.1]
     a = {"lr": 0.02, "momentum": 0.95, "eps": 1e-7, "weight_decay": 0.1, "nesterov": nesterov}
     plan = bltrain.MuonPlan(shapes, param_dtype=tdtype(torch, param), grad_dtype=tdtype(torch, grad), decay=decay,
@@ -262,9 +283,9 @@ def test_rounding_of_bfloat16_parameters_is_right_on_average(torch):
     assert (again != p).any()
 
 
+@pytest.mark.parametrize("shapes", [[(70, 30), (128, 200), (3, 3)], [(70, 30), (3, 3)]])
 @pytest.mark.parametrize("param", ["f32", "bf16"])
-def test_live_rate_and_step_and_a_graph(torch, param):
-    shapes = [(70, 30), (128, 200), (3, 3)]
+def test_live_rate_and_step_and_a_graph(torch, param, shapes):
     plan = bltrain.MuonPlan(shapes, param_dtype=tdtype(torch, param))
     gen = torch.Generator().manual_seed(9)
     start = [(0.05 * torch.randn(s, generator=gen)).to(tdtype(torch, param)).cuda() for s in shapes]
