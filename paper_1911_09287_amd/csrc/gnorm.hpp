@@ -99,7 +99,7 @@ void with_each(int each, Go&& go) {
   else if (each <= 4) go(std::integral_constant<int, 4>());
   else go(std::integral_constant<int, 8>());
 }
-constexpr int kMostEach = 8;
+constexpr long kMostEach = 8;
 
 // Mean and sum of squares about it, of values that come in tiles: each tile's own are
 // taken in registers and joined (Chan, Golub and LeVeque, "Updating formulae and a
@@ -120,6 +120,18 @@ bl_status_t gnorm_last_forward(const bl_group_norm_plan_s* p, const GroupNormArg
 bl_status_t gnorm_last_backward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
 bl_status_t gnorm_first_forward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
 bl_status_t gnorm_first_backward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
+// The fewest threads of a block that keeps all with at most eight accesses each, and more while
+// that leaves them over four and fewer; none (0) where it cannot.  each(threads): accesses.
+template <typename Each>
+void gnorm_whole_threads(Each&& each, int& threads, int& found) {
+  threads = 0;
+  int n = kWave;
+  while (n <= kMostThreads && each(n) > kMostEach) n *= 2;
+  if (n > kMostThreads) return;
+  while (n < kMostThreads && each(n) > 4 && each(2 * n) < each(n)) n *= 2;
+  threads = n;
+  found = (int)each(n);
+}
 // How a plan's blocks keep whole groups, if they can.
 void gnorm_last_whole(bl_group_norm_plan_s* p);
 void gnorm_first_whole(bl_group_norm_plan_s* p);

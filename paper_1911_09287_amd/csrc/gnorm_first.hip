@@ -376,11 +376,8 @@ void gnorm_first_whole(bl_group_norm_plan_s* p) {
   p->whole_lanes = lanes;
   p->whole_tiles = (int)d.groups;
   for (int i = 0; i < 2; ++i) {
-    // the fewest threads that have a few accesses each
-    for (int threads = kWave; threads <= kMostThreads && !p->whole_threads[i]; threads *= 2) {
-      const long rows = threads / lanes, each = (p->each + rows - 1) / rows * per;
-      if (each <= (threads < kMostThreads ? 4 : kMostEach)) p->whole_threads[i] = threads, p->whole_each[i] = (int)each;
-    }
+    const auto each = [&](int threads) { return (p->each + threads / lanes - 1) / (threads / lanes) * per; };
+    gnorm_whole_threads(each, p->whole_threads[i], p->whole_each[i]);
   }
 }
 

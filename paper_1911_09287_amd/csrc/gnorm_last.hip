@@ -471,12 +471,11 @@ void gnorm_last_whole(bl_group_norm_plan_s* p) {
   p->whole_lanes = (int)lanes;
   p->whole_tiles = (int)((d.channels + width - 1) / width);
   for (int i = 0; i < 2; ++i) {
-    // the fewest threads that have a few accesses each
-    for (int threads = kWave; threads <= kMostThreads && !p->whole_threads[i]; threads *= 2) {
-      if (lanes > threads) continue;
-      const long slices = threads / lanes, each = (d.sites + slices - 1) / slices;
-      if (each <= (threads < kMostThreads ? 4 : kMostEach)) p->whole_threads[i] = threads, p->whole_each[i] = (int)each;
-    }
+    const auto each = [&](int threads) {
+      const long slices = threads / lanes;
+      return slices ? (d.sites + slices - 1) / slices : kMostEach + 1L;
+    };
+    gnorm_whole_threads(each, p->whole_threads[i], p->whole_each[i]);
   }
 }
 
