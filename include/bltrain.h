@@ -122,8 +122,8 @@ typedef struct {
 typedef struct bl_group_norm_plan_s* bl_group_norm_plan_t;
 
 /* BL_ERR_UNSUPPORTED: sites channels >= 2^31, batch channels >= 2^31, batch groups >= 2^26;
- * samples in such a number that a launch would take 2^24 blocks (with channels last batch >=
- * 2^24); strides that reach over 2^60 elements. */
+ * samples or channels in such a number that a launch would take 2^24 blocks (batch with
+ * channels last, or channels / 64); strides that reach over 2^60 elements. */
 bl_status_t bl_group_norm_plan_create(bl_group_norm_plan_t* out, const bl_group_norm_desc_t* desc);
 bl_status_t bl_group_norm_plan_destroy(bl_group_norm_plan_t plan);
 /* Workspace bytes of either call (0: ws may be NULL). */
@@ -185,8 +185,9 @@ typedef struct {
 typedef struct bl_recurrence_plan_s* bl_recurrence_plan_t;
 
 /* BL_ERR_UNSUPPORTED: outer inner >= 2^31, length >= 2^31; 2^26 sequences or more of one
- * channel with steps side by side (inner = 1), else 2^23 or more times inner in lines of 128
- * bytes; strides that reach over 2^60 elements. */
+ * channel with steps side by side (inner = 1), else so many that a launch would take 2^23
+ * blocks of some 128 bytes of channels (or four channels) each; strides that reach over 2^60
+ * elements. */
 bl_status_t bl_recurrence_plan_create(bl_recurrence_plan_t* out, const bl_recurrence_desc_t* desc);
 bl_status_t bl_recurrence_plan_destroy(bl_recurrence_plan_t plan);
 /* Workspace bytes of either call (0: ws may be NULL), and elements (fp32) of `states`. */

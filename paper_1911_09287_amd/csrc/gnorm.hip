@@ -219,7 +219,8 @@ extern "C" bl_status_t bl_group_norm_plan_create(bl_group_norm_plan_t* out, cons
   const __int128 blocks = d.layout == BL_CHANNELS_LAST
                               ? (__int128)d.batch * p->chunks * p->tiles
                               : ((__int128)d.batch * d.channels + kThreads / p->lanes - 1) / (kThreads / p->lanes) * p->chunks;
-  if (blocks >= 1LL << 24 || (__int128)d.batch * d.groups >= (1LL << 24) * 4 || (__int128)p->each * p->chunks >= 1LL << 31) {
+  const long sums = (d.channels + kWave - 1) / kWave;  // (blocks that sum the weights' gradients)
+  if (blocks + sums >= 1LL << 24 || (__int128)d.batch * d.groups >= (1LL << 24) * 4 || (__int128)p->each * p->chunks >= 1LL << 31) {
     delete p;
     return BL_ERR_UNSUPPORTED;
   }

@@ -271,6 +271,7 @@ bl_status_t forward(const bl_recurrence_plan_s* p, RecurArgs r, hipStream_t s) {
   }
   const dim3 grid((unsigned)recur_blocks(d, p->layout[0]), (unsigned)p->chunks[0]);
   r.chunk = p->chunk[0];
+  r.lanes = p->lanes[0];
   if (p->chunks[0] > 1) {
     const bl_status_t st = timed_launch("recur_fwd_part", bytes * 2 / 3, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
       recur_dispatch(d.gate, p->layout[0], 8, r.resets, [&](auto g, auto l, auto, auto z) {
@@ -353,11 +354,13 @@ extern "C" bl_status_t bl_recurrence_plan_create(bl_recurrence_plan_t* out, cons
   if (!p) return BL_ERR_OOM;
   p->d = d;
   const bool row = d.inner == 1 && d.in_step == 1 && d.out_step == 1;
-  const long slices = row ? kWave : d.inner <= 4 ? 16 : 4;
   long most_threads = 0;
   for (int i = 0; i < 2; ++i) {
     // lines of 64 bytes where those of 128 leave compute units without a block, and they do not
-    p->layout[i] = row ? kRow : d.inner <= 4 ? kNarrow : recur_blocks(d, kWide) < 256 && recur_blocks(d, kHalf) >= 256 ? kHalf : kWide;
+    const bool half = recur_lanes(d, kHalf) && (!recur_lanes(d, kWide) || (recur_blocks(d, kWide) < 256 && recur_blocks(d, kHalf) >= 256));
+    p->layout[i] = row ? kRow : d.inner <= 4 ? kNarrow : half ? kHalf : recur_lanes(d, kWide) ? kWide : kNarrow;
+    p->lanes[i] = recur_lanes(d, p->layout[i]);
+    const long slices = row ? kWave : p->layout[i] == kNarrow ? 16 : 4;
     const long blocks = std::max(recur_blocks(d, p->layout[i]), 1L), tile = slices * recur_each(p->layout[i], dtype_bytes(d.dtype), i);
     // (tile: of one wave)
     // one wave a block: rows in such a number that they fill the GPU, or sequences of one tile
@@ -375,7 +378,7 @@ extern "C" bl_status_t bl_recurrence_plan_create(bl_recurrence_plan_t* out, cons
     return BL_ERR_UNSUPPORTED;
   }
   // a state at every tile of the backward pass
-  p->every = slices * recur_each(p->layout[1], dtype_bytes(d.dtype), true) * p->waves[1];
+  p->every = (row ? kWave : p->layout[1] == kNarrow ? 16 : 4) * recur_each(p->layout[1], dtype_bytes(d.dtype), true) * p->waves[1];
   const size_t parts = std::max(p->chunks[0], p->chunks[1]);
   p->bytes = parts > 1 ? (parts + 1) * ((size_t)d.outer * d.inner * 8 + d.outer) : 0;
   *out = p;

@@ -7,6 +7,7 @@
 struct bl_recurrence_plan_s {
   bl_recurrence_desc_t d;
   int layout[2];    // RecurLayout, forward and backward, as all that follow
+  int lanes[2];     // of channels that a block takes
   int waves[2];     // of a block
   long every;       // steps between two saved states, a multiple of both directions' thread's steps
   long chunk[2];    // steps that a block takes (>= length: all)
@@ -34,6 +35,7 @@ struct RecurArgs {
   long every, chunk;  // every: a power of two
   int every_log2;
   bool near;          // a tile's bytes count in 32 bits
+  int lanes;          // of channels that a block takes
   float *part_a, *part_b;    // chunks: [1 + chunk][outer][inner] products and sums, entry 0 the state from outside
   unsigned char* part_drop;  // [1 + chunk][outer]: the state from outside does not reach the chunk's end
 };
@@ -94,25 +96,27 @@ __device__ __forceinline__ void gate_of(float g, float& a, float& rest) {
   }
 }
 
+// Channels of a lane.
+constexpr int recur_vec(int layout, int wide) { return layout == kWide ? 8 / wide : layout == kHalf ? 4 / wide : 1; }
 // Lanes of channels, channels of a lane and steps of a thread.
 template <typename T, int LAYOUT>
 struct RecurShape {
   static constexpr int kLanes = LAYOUT == kNarrow ? 4 : LAYOUT == kRow ? 1 : 16;
-  static constexpr int kVec = LAYOUT == kWide ? 8 / (int)sizeof(T) : LAYOUT == kHalf ? 4 / (int)sizeof(T) : 1;
+  static constexpr int kVec = recur_vec(LAYOUT, (int)sizeof(T));
   static constexpr int kSlices = kWave / kLanes;  // of a wave, along steps
 };
 
-// Where a thread stands: its sequence and chunk of it, first channel and slice of the tile's steps.  Lanes that
-// would reach over the last channel (of which there are at least a lane's) take the last
-// ones, as another lane of their wave does too: both read the same before either writes, and
-// write the same.
+// Where a thread stands: its sequence and chunk of it, first channel and slice of the tile's
+// steps.  Lanes that would reach over the block's channels (which are a lane's at least, see
+// recur_lanes) take its last ones, as another lane of their wave does too: both read the same
+// before either writes, and write the same.
 template <typename T, int LAYOUT, int WAVES>
 struct RecurPlace {
   using S = RecurShape<T, LAYOUT>;
   long o, chunk, i;
   int wave, lane, slice;
   __device__ __forceinline__ explicit RecurPlace(const RecurArgs& r) {
-    const long tiles = (r.inner + S::kLanes * S::kVec - 1) / (S::kLanes * S::kVec);
+    const long tiles = (r.inner + r.lanes * S::kVec - 1) / (r.lanes * S::kVec);
     // blocks go to the GPU's eight dies in turn, each with caches of its own: a die takes
     // neighbouring channels of a sequence's chunk
     const unsigned index = blockIdx.y * gridDim.x + blockIdx.x, all = gridDim.x * gridDim.y;
@@ -124,7 +128,7 @@ struct RecurPlace {
     wave = WAVES == 1 ? 0 : threadIdx.x / kWave;
     lane = threadIdx.x % kWave;
     slice = wave * S::kSlices + lane / S::kLanes;
-    i = min(((long)block * S::kLanes + lane % S::kLanes) * S::kVec, r.inner - S::kVec);
+    i = min(((long)block * r.lanes + min(lane % S::kLanes, r.lanes - 1)) * S::kVec, r.inner - S::kVec);
   }
 };
 
@@ -405,11 +409,22 @@ constexpr int recur_each() {
   return recur_each(LAYOUT, (int)sizeof(T), BACKWARD);
 }
 
-// Blocks along sequences and channels.
+// Lanes of channels that a block takes: as many as there are, or a few less, so that the last
+// block is not left with fewer channels than a lane has (it would share them with the block
+// before); 0 where no number does it.
+inline int recur_lanes(const bl_recurrence_desc_t& d, int layout) {
+  const int all = layout == kRow ? 1 : layout == kNarrow ? 4 : 16, vec = recur_vec(layout, dtype_bytes(d.dtype));
+  if (vec == 1) return all;
+  for (int lanes = all; lanes >= all / 2; --lanes) {
+    const long rest = d.inner % (lanes * vec);
+    if (!rest || rest >= vec) return lanes;
+  }
+  return 0;
+}
+// Blocks along sequences and channels (0: the layout does not do).
 inline long recur_blocks(const bl_recurrence_desc_t& d, int layout) {
-  const long wide = dtype_bytes(d.dtype);
-  const long lanes = layout == kWide ? 128 / wide : layout == kHalf ? 64 / wide : layout == kNarrow ? 4 : 1;
-  return d.outer * ((d.inner + lanes - 1) / lanes);
+  const long channels = (long)recur_lanes(d, layout) * recur_vec(layout, dtype_bytes(d.dtype));
+  return channels ? d.outer * ((d.inner + channels - 1) / channels) : 0;
 }
 
 bl_status_t recur_backward(const bl_recurrence_plan_s* p, const RecurArgs& r, hipStream_t s);

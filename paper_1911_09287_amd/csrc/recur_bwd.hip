@@ -257,6 +257,7 @@ bl_status_t backward(const bl_recurrence_plan_s* p, RecurArgs r, hipStream_t s) 
   const double bytes = 5.0 * d.outer * d.length * d.inner * sizeof(T);
   const dim3 grid((unsigned)recur_blocks(d, p->layout[1]), (unsigned)p->chunks[1]);
   r.chunk = p->chunk[1];
+  r.lanes = p->lanes[1];
   if (p->chunks[1] > 1) {
     const bl_status_t st = timed_launch("recur_bwd_part", bytes * 2 / 5, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
       recur_dispatch(d.gate, p->layout[1], 8, r.resets, [&](auto g, auto l, auto, auto z) {

@@ -28,7 +28,8 @@ def _code(call, *args, **kw):
     ((2, 4, 8, 2), {"wdtype": torch.bfloat16}, INVALID),
     ((1, 1 << 16, 1 << 15, 2), {}, UNSUPPORTED), ((1 << 20, 1, 1 << 11, 2), {}, UNSUPPORTED),
     ((1 << 31, 1, 1, 1), {}, UNSUPPORTED), ((1, BIG, 1, 1), {}, UNSUPPORTED), ((1, 1, BIG, 1), {}, UNSUPPORTED),
-    ((1 << 25, 1, 1, 1), {"channels_last": True}, UNSUPPORTED), ((2, 4, 8, 2), {"x_stride": 1 << 61}, UNSUPPORTED),
+    ((1 << 25, 1, 1, 1), {"channels_last": True}, UNSUPPORTED), ((1, 1, 1 << 30, 1), {}, UNSUPPORTED),
+    ((1, 1, 1 << 30, 1 << 20), {"channels_last": True}, UNSUPPORTED), ((0, 1, 1 << 30, 1 << 20), {}, UNSUPPORTED), ((2, 4, 8, 2), {"x_stride": 1 << 61}, UNSUPPORTED),
 ])
 def test_group_norm_plan_refusals(args, kw, code):
     assert _code(bltrain.GroupNormPlan, *args, **kw) == code
@@ -67,6 +68,13 @@ def test_recurrence_plans_of_interleaved_layouts():
 ])
 def test_muon_plan_refusals(shapes, kw, code):
     assert _code(bltrain.MuonPlan, shapes, **kw) == code
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_recurrence_plans_of_any_number_of_channels(dtype):
+    # among them numbers that leave one channel over whatever lanes a block takes (4 lcm(1 ... 16) + 1)
+    for inner in list(range(1, 300)) + [2882881, 2882882, 2882883]:
+        bltrain.RecurrencePlan(1, 50, inner, dtype=dtype)
 
 
 def test_muon_layout():

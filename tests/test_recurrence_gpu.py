@@ -114,7 +114,7 @@ def check(t, shape, kind, dtype, seed, resets, **kw):
 
 SHAPES = [(1, 1, 1), (3, 1, 5), (2, 7, 3), (2, 8, 70), (2, 9, 1), (5, 16, 70), (3, 17, 64), (2, 100, 33), (4, 257, 130),
           (1, 1000, 4), (2, 1029, 2), (3, 300, 1), (2100, 70, 1), (1, 5000, 40), (1, 20000, 1), (1, 9000, 3),
-          (2, 2500, 32), (600, 33, 17), (1, 4097, 256)]
+          (2, 2500, 32), (600, 33, 17), (1, 4097, 256), (2, 200, 65), (3, 150, 66), (300, 20, 67)]
 
 
 @pytest.mark.parametrize("resets", [False, True])
@@ -230,11 +230,14 @@ def test_token_by_token_and_in_parts(torch, kind):
         near(state, r["last"], most["last"])
 
 
-@pytest.mark.parametrize("shape", [(2, 900, 24), (1, 6000, 24), (3, 700, 1)])
-def test_in_place(torch, shape):
-    v = inputs(torch, shape, "sigmoid", "f32", 9, True)
-    want = run(torch, shape, "sigmoid", "f32", v)
-    plan = bltrain.RecurrencePlan(*shape)
+# (channels one to three over those of a whole number of blocks among them: no two blocks may share one)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 900, 24), (1, 6000, 24), (3, 700, 1), (2, 900, 33), (2, 900, 65), (40, 300, 66),
+                                   (40, 300, 67), (1, 9000, 129), (300, 40, 65), (300, 6, 65)])
+def test_in_place(torch, shape, dtype):
+    v = inputs(torch, shape, "sigmoid", dtype, 9, True)
+    want = run(torch, shape, "sigmoid", dtype, v)
+    plan = bltrain.RecurrencePlan(*shape, dtype=tdtype(torch, dtype))
     ws, states = plan.workspace(), plan.states()
     gate, x, dy, resets = (v[k].cuda() for k in ("gate", "x", "dy", "resets"))
     state, y = v["h0"].cuda(), x.clone()
