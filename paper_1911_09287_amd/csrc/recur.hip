@@ -251,6 +251,7 @@ __global__ void k_recur_none(const float* from, float* to, long n) {
   if (i < n) to[i] = from ? from[i] : 0.f;
 }
 
+constexpr long kUnits = 256;  // compute units
 // Up to this many steps a thread walks them alone.
 constexpr long kSerialSteps = 8;
 
@@ -273,9 +274,11 @@ bl_status_t forward(const bl_recurrence_plan_s* p, RecurArgs r, hipStream_t s) {
   r.chunk = p->chunk[0];
   r.lanes = p->lanes[0];
   if (p->chunks[0] > 1) {
+    // (nothing follows the last chunk)
+    const dim3 parts(grid.x, grid.y - 1);
     const bl_status_t st = timed_launch("recur_fwd_part", bytes * 2 / 3, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
       recur_dispatch(d.gate, p->layout[0], 8, r.resets, [&](auto g, auto l, auto, auto z) {
-        hipExtLaunchKernelGGL((k_recur_fwd_part<T, decltype(g)::value, decltype(l)::value, decltype(z)::value>), grid,
+        hipExtLaunchKernelGGL((k_recur_fwd_part<T, decltype(g)::value, decltype(l)::value, decltype(z)::value>), parts,
                               dim3(8 * kWave), 0, s, e0, e1, 0, r);
       });
     });
@@ -356,21 +359,41 @@ extern "C" bl_status_t bl_recurrence_plan_create(bl_recurrence_plan_t* out, cons
   const bool row = d.inner == 1 && d.in_step == 1 && d.out_step == 1;
   long most_threads = 0;
   for (int i = 0; i < 2; ++i) {
-    // lines of 64 bytes where those of 128 leave compute units without a block, and they do not
-    const bool half = recur_lanes(d, kHalf) && (!recur_lanes(d, kWide) || (recur_blocks(d, kWide) < 256 && recur_blocks(d, kHalf) >= 256));
-    p->layout[i] = row ? kRow : d.inner <= 4 ? kNarrow : half ? kHalf : recur_lanes(d, kWide) ? kWide : kNarrow;
-    p->lanes[i] = recur_lanes(d, p->layout[i]);
-    const long slices = row ? kWave : p->layout[i] == kNarrow ? 16 : 4;
-    const long blocks = std::max(recur_blocks(d, p->layout[i]), 1L), tile = slices * recur_each(p->layout[i], dtype_bytes(d.dtype), i);
-    // (tile: of one wave)
-    // one wave a block: rows in such a number that they fill the GPU, or sequences of one tile
-    p->waves[i] = p->layout[i] != kNarrow && (d.length <= tile || (row && blocks >= 2048)) ? 1 : 8;
-    // fewer blocks than compute units: as many chunks as bring 512 blocks onto the GPU, each
-    // of four tiles at least
-    const long part = 8 * tile;
-    const long want = p->waves[i] == 1 || blocks >= 256 ? 1 : std::max(1L, std::min<long>(1024 / blocks, d.length / (4 * part)));
-    p->chunk[i] = want > 1 ? ((d.length + want - 1) / want + part - 1) / part * part : std::max<long>(d.length, 1);
-    p->chunks[i] = want > 1 ? (d.length + p->chunk[i] - 1) / p->chunk[i] : 1;
+    double best = 0.0;
+    auto consider = [&](int layout, double rate) {
+      const long lanes = recur_lanes(d, layout), blocks = std::max(recur_blocks(d, layout), 1L);
+      if (!lanes) return;
+      const long slices = layout == kRow ? kWave : layout == kNarrow ? 16 : 4;
+      const long tile = slices * recur_each(layout, dtype_bytes(d.dtype), i), part = 8 * tile;  // of a wave, of eight
+      // one wave a block: rows in such a number that they fill the GPU, or sequences of one tile
+      const int waves = layout != kNarrow && (d.length <= tile || (layout == kRow && blocks >= 2048)) ? 1 : 8;
+      // fewer blocks than compute units (each has registers for one): chunks of four tiles at
+      // least, whose loads of a part more (all but one chunk's gates and values or dy) are
+      // weighed against the units that have none
+      const long most = waves == 1 || blocks >= kUnits ? 1 : std::max(1L, std::min<long>(4 * kUnits / blocks, d.length / (4 * part)));
+      for (long n = 1; n <= most; ++n) {
+        const long all = n * blocks, turns = (all + kUnits - 1) / kUnits;
+        const double full = most > 1 ? (double)all / (double)(turns * kUnits) : std::min(1.0, (double)blocks / kUnits);
+        const double more = (i ? 2.0 / 5.0 : 2.0 / 3.0) * (double)(n - 1) / (double)n;
+        const double speed = rate * full / (1.0 + more);
+        if (speed <= best * 1.02) continue;
+        best = speed;
+        p->layout[i] = layout;
+        p->lanes[i] = (int)lanes;
+        p->waves[i] = waves;
+        p->chunk[i] = n > 1 ? ((d.length + n - 1) / n + part - 1) / part * part : std::max<long>(d.length, 1);
+        p->chunks[i] = n > 1 ? (d.length + p->chunk[i] - 1) / p->chunk[i] : 1;
+      }
+    };
+    if (row) consider(kRow, 1.0);
+    if (!row && d.inner > 4) {
+      // lines of 64 bytes against 128: bf16, 8 x 4096 x 1024 forward 3.4 TB/s, twice the channels
+      // 4.2, backward (which is short of registers with 128) 3.5 and 4.0
+      consider(kWide, 1.0);
+      consider(kHalf, i ? 0.9 : 0.8);
+    }
+    if (!row && (d.inner <= 4 || best == 0.0)) consider(kNarrow, 1.0);
+    const long blocks = std::max(recur_blocks(d, p->layout[i]), 1L);
     most_threads = std::max(most_threads, blocks * p->waves[i] * kWave);
   }
   if (most_threads >= 1LL << 32) {  // (a launch has fewer)

@@ -194,7 +194,7 @@ __global__ __launch_bounds__(8 * kWave) void k_recur_bwd_part(RecurArgs r) {
   using S = RecurShape<T, LAYOUT>;
   constexpr int N = S::kVec, EACH = recur_each<T, LAYOUT, true>(), SLICES = S::kSlices * 8;
   const RecurPlace<T, LAYOUT, 8> p(r);
-  const long chunk = p.chunk, stretch = r.chunk / SLICES;  // (a multiple of EACH)
+  const long chunk = p.chunk + 1, stretch = r.chunk / SLICES;  // (a multiple of EACH)
   const long first = chunk * r.chunk, begin = first + p.slice * stretch, end = min(r.length, begin + stretch);
   const T* gate = static_cast<const T*>(r.gate) + p.o * r.in_outer;
   const T* dy = static_cast<const T*>(r.dy) + p.o * r.out_outer;
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(8 * kWave) void k_recur_bwd_part(RecurArgs r) {
       work(raw[0], end - t);
     }
   }
-  chunk_part<N, S::kLanes, 8, RESETS, false>(r, p, own, chunk, r.dlast, chunk == (long)gridDim.y - 1);
+  chunk_part<N, S::kLanes, 8, RESETS, false>(r, p, own, chunk, r.dlast, chunk == (long)gridDim.y);
 }
 
 template <typename T>
@@ -259,9 +259,11 @@ bl_status_t backward(const bl_recurrence_plan_s* p, RecurArgs r, hipStream_t s) 
   r.chunk = p->chunk[1];
   r.lanes = p->lanes[1];
   if (p->chunks[1] > 1) {
+    // (nothing is passed back from the first chunk to another)
+    const dim3 parts(grid.x, grid.y - 1);
     const bl_status_t st = timed_launch("recur_bwd_part", bytes * 2 / 5, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
       recur_dispatch(d.gate, p->layout[1], 8, r.resets, [&](auto g, auto l, auto, auto z) {
-        hipExtLaunchKernelGGL((k_recur_bwd_part<T, decltype(g)::value, decltype(l)::value, decltype(z)::value>), grid,
+        hipExtLaunchKernelGGL((k_recur_bwd_part<T, decltype(g)::value, decltype(l)::value, decltype(z)::value>), parts,
                               dim3(8 * kWave), 0, s, e0, e1, 0, r);
       });
     });
