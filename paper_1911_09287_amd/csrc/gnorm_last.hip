@@ -10,11 +10,15 @@
 namespace blc {
 namespace {
 
-constexpr int kAhead = 8;      // sites of a thread whose loads are in flight together
-constexpr int kAheadBoth = 4;  // backward, of x and dy
+// Sites of a thread whose loads are in flight while as many are worked on; backward, of x and dy.
+template <typename T, int V>
+constexpr int kAhead = V * sizeof(T) >= 16 ? 4 : 8;
+template <typename T, int V>
+constexpr int kAheadBoth = kAhead<T, V> / 2;
+constexpr int kMostParts = 8;  // of a channel's slices, which threads sum side by side
 
-// Where a thread stands: sample, chunk, its first channel and its sites begin, begin +
-// slices, ...
+// Where a thread stands: sample, chunk, its first channel and its sites begin + slice, begin +
+// slice + slices, ... below end.
 struct LastPlace {
   long n, chunk, c, begin, end;
   int lane, slice, slices;
@@ -30,65 +34,107 @@ struct LastPlace {
     p.lane = threadIdx.x - p.slice * a.lanes;
     p.c = (tile * kThreads + p.lane) * V;
     p.there = p.slice < p.slices && p.c < a.channels;
-    p.begin = p.chunk * a.chunk + p.slice;
-    p.end = p.there ? min(a.sites, (p.chunk + 1) * a.chunk) : 0;
+    p.begin = p.chunk * a.chunk;
+    p.end = min(a.sites, p.begin + a.chunk);
     return p;
   }
+  // COUNT sites of a thread at a time: load(held, site) for them while work(held, site, the
+  // sites that there are) goes through those before.  Sites behind the last one are read as the
+  // last one, so that loads have no branch around them and can be told from those after.
+  template <int COUNT, typename H, typename Load, typename Work>
+  __device__ __forceinline__ void walk(Load&& load, Work&& work) const {
+    const long step = (long)COUNT * slices;
+    H now[COUNT], next[COUNT];
+    auto fetch = [&](H (&to)[COUNT], long from) {
+#pragma unroll
+      for (int k = 0; k < COUNT; ++k) load(to[k], min(from + (long)k * slices + slice, end - 1));
+    };
+    long t = begin;
+    fetch(now, t);
+    for (; t + step <= end; t += step) {
+      fetch(next, t + step);
+      work(now, t + slice, std::integral_constant<int, COUNT>());
+#pragma unroll
+      for (int k = 0; k < COUNT; ++k) now[k] = next[k];
+    }
+    const long left = end - t - slice;
+    if (left > 0) work(now, t + slice, (int)((left + slices - 1) / slices));
+  }
 };
+
+// Sums over the slices of a thread's N values, in each thread.  red: [kThreads][N].
+template <int N>
+__device__ __forceinline__ void slices_sum(float (&v)[N], float* red, const LastPlace& p, int lanes) {
+  if (p.slices == 1) return;
+  const int width = lanes * N, parts = max(1, min(min(kMostParts, p.slices), kThreads / width));
+#pragma unroll
+  for (int j = 0; j < N; ++j) red[threadIdx.x * N + j] = v[j];
+  __syncthreads();
+  // (a part's threads alone read the place that its sum goes to)
+  for (int i = threadIdx.x; i < parts * width; i += kThreads) {
+    const int q = i / width, c = i - q * width;
+    float s = 0.f;
+    for (int k = q; k < p.slices; k += parts) s += red[k * width + c];
+    red[i] = s;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < N; ++j) v[j] = 0.f;
+  for (int q = 0; q < parts; ++q)
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] += red[q * width + p.lane * N + j];
+}
 
 // Each channel's moments over the block's sites.
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void k_last_part(GroupNormArgs a) {
-  __shared__ Moments red[kThreads][V];
+  __shared__ float red[kThreads * V];
   const LastPlace p = LastPlace::make<V>(a);
   const T* x = static_cast<const T*>(a.x) + p.n * a.x_stride + p.c;
-  Moments m[V];
+  float n = 0.f, mean[V] = {}, m2[V] = {};
+  if (p.there)
+    p.walk<kAhead<T, V>, Held<T, V>>(
+        [&](Held<T, V>& to, long site) { to.load(x + site * a.channels, V); },
+        [&](Held<T, V>(&v)[kAhead<T, V>], long, auto count) {
+          const float inv = 1.f / (float)count, share = (float)count / (n + (float)count);
+          const float old = n * share;
 #pragma unroll
-  for (int j = 0; j < V; ++j) m[j] = Moments{0.f, 0.f, 0.f};
-  for (long t = p.begin; t < p.end; t += (long)kAhead * p.slices) {
-    Held<T, V> v[kAhead];
-    int count = 0;
+          for (int k = 0; k < kAhead<T, V>; ++k) v[k].refresh();
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const long site = t + (long)k * p.slices;
-      v[k].load(x + site * a.channels, site < p.end ? V : 0);
-      count += site < p.end;
-    }
-    const float inv = 1.f / (float)count;
+          for (int j = 0; j < V; ++j) {
+            float m = 0.f, s = 0.f;
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) v[k].refresh();
+            for (int k = 0; k < kAhead<T, V>; ++k) m += k < count ? v[k][j] : 0.f;
+            m *= inv;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      Moments own{(float)count, 0.f, 0.f};
+            for (int k = 0; k < kAhead<T, V>; ++k) {
+              const float d = k < count ? v[k][j] - m : 0.f;
+              s = fmaf(d, d, s);
+            }
+            const float d = m - mean[j];
+            m2[j] += fmaf(d * d, old, s);
+            mean[j] = fmaf(d, share, mean[j]);
+          }
+          n += (float)count;
+        });
+  // the block's means, then the squares about them
+  float sum[V];
+  const float inv = 1.f / (float)(p.end - p.begin);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) own.mean += v[k][j];
-      own.mean *= inv;
+  for (int j = 0; j < V; ++j) sum[j] = n * mean[j];
+  slices_sum(sum, red, p, a.lanes);
+  __syncthreads();
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const float d = k < count ? v[k][j] - own.mean : 0.f;
-        own.m2 = fmaf(d, d, own.m2);
-      }
-      moments_join(m[j], own);
-    }
+  for (int j = 0; j < V; ++j) {
+    sum[j] = p.slices == 1 ? mean[j] : sum[j] * inv;
+    const float d = mean[j] - sum[j];
+    m2[j] = fmaf(n * d, d, m2[j]);
   }
-  // over the slices, by halves
-  int span = 1;
-  while (span < p.slices) span *= 2;
-#pragma unroll
-  for (int j = 0; j < V; ++j) red[threadIdx.x][j] = m[j];
-  for (span /= 2; span; span /= 2) {
-    __syncthreads();
-    if (p.slice < span && p.slice + span < p.slices)
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        moments_join(m[j], red[threadIdx.x + span * a.lanes][j]);
-        red[threadIdx.x][j] = m[j];
-      }
-  }
+  slices_sum(m2, red, p, a.lanes);
   if (p.slice || !p.there) return;
   float* to = a.part + ((p.n * a.chunks + p.chunk) * a.channels + p.c) * 2;
 #pragma unroll
-  for (int j = 0; j < V; ++j) to[2 * j] = m[j].mean, to[2 * j + 1] = m[j].m2;
+  for (int j = 0; j < V; ++j) to[2 * j] = sum[j], to[2 * j + 1] = m2[j];
 }
 
 // What a thread's channels need: statistics and weights.
@@ -115,67 +161,64 @@ __global__ __launch_bounds__(kThreads) void k_last_apply(GroupNormArgs a) {
   T* y = static_cast<T*>(a.y) + p.n * a.y_stride + p.c;
   LastChannels<T, V> own;
   own.load(a, p);
-  for (long t = p.begin; t < p.end; t += (long)kAhead * p.slices) {
-    Held<T, V> v[kAhead];
+  if (!p.there) return;
+  p.walk<kAhead<T, V>, Held<T, V>>(
+      [&](Held<T, V>& to, long site) { to.load(x + site * a.channels, V); },
+      [&](Held<T, V>(&v)[kAhead<T, V>], long site, auto count) {
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const long site = t + (long)k * p.slices;
-      v[k].load(x + site * a.channels, site < p.end ? V : 0);
-    }
+        for (int k = 0; k < kAhead<T, V>; ++k, site += p.slices) {
+          v[k].refresh();
+          Pack<T, V> o;
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const long site = t + (long)k * p.slices;
-      v[k].refresh();
-      Pack<T, V> o;
-#pragma unroll
-      for (int j = 0; j < V; ++j) o.v[j] = (T)act_of<ACT>(norm_z(v[k][j], own.mean[j], own.rstd[j], own.w[j], own.b[j]));
-      if (site < p.end) store_pack(y + site * a.channels, o);
-    }
-  }
+          for (int j = 0; j < V; ++j)
+            o.v[j] = (T)act_of<ACT>(norm_z(v[k][j], own.mean[j], own.rstd[j], own.w[j], own.b[j]));
+          if (k < count) store_pack(y + site * a.channels, o);
+        }
+      });
 }
+
+// A site's x and dy.
+template <typename T, int V>
+struct HeldBoth {
+  Held<T, V> v, g;
+  __device__ __forceinline__ void load(const T* x, const T* dy) {
+    v.load(x, V);
+    g.load(dy, V);
+  }
+  __device__ __forceinline__ void refresh() {
+    v.refresh();
+    g.refresh();
+  }
+};
 
 // Each channel's sums of dz and of dz h over the block's sites.
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void k_last_bwd_part(GroupNormArgs a) {
-  __shared__ float red[kThreads][2 * V];
+  __shared__ float red[kThreads * 2 * V];
   const LastPlace p = LastPlace::make<V>(a);
   const T* x = static_cast<const T*>(a.x) + p.n * a.x_stride + p.c;
   const T* dy = static_cast<const T*>(a.dy) + p.n * a.y_stride + p.c;
   LastChannels<T, V> own;
   own.load(a, p);
   float s[2 * V] = {};
-  for (long t = p.begin; t < p.end; t += (long)kAheadBoth * p.slices) {
-    Held<T, V> v[kAheadBoth], g[kAheadBoth];
+  if (p.there)
+    p.walk<kAheadBoth<T, V>, HeldBoth<T, V>>(
+        [&](HeldBoth<T, V>& to, long site) { to.load(x + site * a.channels, dy + site * a.channels); },
+        [&](HeldBoth<T, V>(&at)[kAheadBoth<T, V>], long, auto count) {
 #pragma unroll
-    for (int k = 0; k < kAheadBoth; ++k) {
-      const long site = t + (long)k * p.slices;
-      v[k].load(x + site * a.channels, site < p.end ? V : 0);
-      g[k].load(dy + site * a.channels, site < p.end ? V : 0);
-    }
+          for (int k = 0; k < kAheadBoth<T, V>; ++k) {
+            at[k].refresh();
+            if (k >= count) continue;
 #pragma unroll
-    for (int k = 0; k < kAheadBoth; ++k) {
-      v[k].refresh();
-      g[k].refresh();
-      if (t + (long)k * p.slices >= p.end) continue;
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float h = (v[k][j] - own.mean[j]) * own.rstd[j];
-        const float dz = act_grad<ACT>(norm_z(v[k][j], own.mean[j], own.rstd[j], own.w[j], own.b[j]), g[k][j]);
-        s[2 * j] += dz;
-        s[2 * j + 1] = fmaf(dz, h, s[2 * j + 1]);
-      }
-    }
-  }
-  int span = 1;
-  while (span < p.slices) span *= 2;
-#pragma unroll
-  for (int j = 0; j < 2 * V; ++j) red[threadIdx.x][j] = s[j];
-  for (span /= 2; span; span /= 2) {
-    __syncthreads();
-    if (p.slice < span && p.slice + span < p.slices)
-#pragma unroll
-      for (int j = 0; j < 2 * V; ++j) red[threadIdx.x][j] = s[j] += red[threadIdx.x + span * a.lanes][j];
-  }
+            for (int j = 0; j < V; ++j) {
+              const float h = (at[k].v[j] - own.mean[j]) * own.rstd[j];
+              const float dz = act_grad<ACT>(norm_z(at[k].v[j], own.mean[j], own.rstd[j], own.w[j], own.b[j]), at[k].g[j]);
+              s[2 * j] += dz;
+              s[2 * j + 1] = fmaf(dz, h, s[2 * j + 1]);
+            }
+          }
+        });
+  slices_sum(s, red, p, a.lanes);
   if (p.slice || !p.there) return;
   float* to = a.part + ((p.n * a.chunks + p.chunk) * a.channels + p.c) * 2;
 #pragma unroll
@@ -201,28 +244,22 @@ __global__ __launch_bounds__(kThreads) void k_last_bwd_apply(GroupNormArgs a, un
     c1[j] = a.sums[2 * q];
     c2[j] = a.sums[2 * q + 1];
   }
-  for (long t = p.begin; t < p.end; t += (long)kAheadBoth * p.slices) {
-    Held<T, V> v[kAheadBoth], g[kAheadBoth];
+  if (!p.there) return;
+  p.walk<kAheadBoth<T, V>, HeldBoth<T, V>>(
+      [&](HeldBoth<T, V>& to, long site) { to.load(x + site * a.channels, dy + site * a.channels); },
+      [&](HeldBoth<T, V>(&at)[kAheadBoth<T, V>], long site, auto count) {
 #pragma unroll
-    for (int k = 0; k < kAheadBoth; ++k) {
-      const long site = t + (long)k * p.slices;
-      v[k].load(x + site * a.channels, site < p.end ? V : 0);
-      g[k].load(dy + site * a.channels, site < p.end ? V : 0);
-    }
+        for (int k = 0; k < kAheadBoth<T, V>; ++k, site += p.slices) {
+          at[k].refresh();
+          Pack<T, V> o;
 #pragma unroll
-    for (int k = 0; k < kAheadBoth; ++k) {
-      const long site = t + (long)k * p.slices;
-      v[k].refresh();
-      g[k].refresh();
-      Pack<T, V> o;
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float dz = act_grad<ACT>(norm_z(v[k][j], own.mean[j], own.rstd[j], own.w[j], own.b[j]), g[k][j]);
-        o.v[j] = (T)norm_grad(dz, own.w[j], c1[j], (v[k][j] - own.mean[j]) * own.rstd[j], c2[j], own.rstd[j]);
-      }
-      if (site < p.end) store_pack(dx + site * a.channels, o);
-    }
-  }
+          for (int j = 0; j < V; ++j) {
+            const float dz = act_grad<ACT>(norm_z(at[k].v[j], own.mean[j], own.rstd[j], own.w[j], own.b[j]), at[k].g[j]);
+            o.v[j] = (T)norm_grad(dz, own.w[j], c1[j], (at[k].v[j] - own.mean[j]) * own.rstd[j], c2[j], own.rstd[j]);
+          }
+          if (k < count) store_pack(dx + site * a.channels, o);
+        }
+      });
 }
 
 // A block keeps all sites of a tile of whole groups of a sample: accesses of V channels on
