@@ -170,13 +170,14 @@ __device__ __forceinline__ void hold(char* at, const float (&v)[N]) {
 
 // Blocks go to the GPU's eight dies in turn, each with a cache of its own: a die takes `each`
 // neighbouring tiles, which share rows, then as many further on, so that all dies work at
-// the long sums, which lie at the front, for as long.
+// the long sums, which lie at the front, for as long; the last ones go evenly over the dies
+// (products of squares up to 512: 10.4 and 10.7 us, in the order of the blocks 12.1 and 13.0).
 template <int SIDE>
 __device__ __forceinline__ unsigned near_tile(unsigned block, unsigned blocks) {
   constexpr unsigned each = SIDE == 256 ? 16 : 32, turn = 8 * each;
   const unsigned first = block / turn * turn;
-  if (first + turn > blocks) return block;
-  return first + block % 8 * each + block % turn / 8;
+  const unsigned rest = min(blocks - first, turn), die = block % 8;
+  return first + die * (rest / 8) + min(die, rest % 8) + block % turn / 8;
 }
 
 // What a block's tile is: matrix, place and the rows that this thread's wave fetches.
