@@ -3,7 +3,13 @@
 // Statistics span a sample's sites, and a group's channels may be one of 16 bits or all:
 // blocks take all channels of some sites (channels last) or sites of some channels (first),
 // leave what each channel gives there, and a launch of a wave a group joins it; a further
-// launch applies the result.  So x (backward: x and dy) is read twice.
+// launch applies the result.  So x (backward: x and dy) is read twice, which memory bounds.  Where
+// a block's registers can hold whole groups of a sample they are read once, by one launch.
+//
+// Kernels' times, bf16 (bytes as moved, with the second reading): 128 x 3136 x 64 channels last
+// forward 13.9 + 4.0 (join) + 20.6 us, 154 MB; 32 x 3136 x 256 backward 31.6 + 4.8 + 28.3 us, 257
+// MB; in one launch fp32 channels first 64 x 256 x 512 backward 26.6 us, 101 MB, and 4.1 for the
+// weights' gradients.
 #include <algorithm>
 #include <cmath>
 #include <new>

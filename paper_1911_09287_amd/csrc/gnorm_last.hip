@@ -3,6 +3,9 @@
 // A thread keeps an access of channels (`vec` of them, a divisor of their number) and walks
 // sites, so that neighbouring threads read neighbouring memory whatever the channels'
 // number, and what belongs to its channels (weights, statistics) stays in registers.
+//
+// Two blocks a compute unit with the next sites' loads in flight: the sums of 51 MB take 13.9 us
+// (3.7 TB/s, from memory) and the launch that applies them 20.6 (5.0 TB/s, x from the cache).
 #include <algorithm>
 
 #include "gnorm.hpp"
@@ -11,6 +14,7 @@ namespace blc {
 namespace {
 
 // Sites of a thread whose loads are in flight while as many are worked on; backward, of x and dy.
+// (With twice as many the sums above take 15.7 us and those of 32 x 3136 x 256 backward 35, not 32.)
 template <typename T, int V>
 constexpr int kAhead = V * sizeof(T) >= 16 ? 4 : 8;
 template <typename T, int V>
@@ -264,7 +268,8 @@ __global__ __launch_bounds__(kThreads) void k_last_bwd_apply(GroupNormArgs a, un
 
 // A block keeps all sites of a tile of whole groups of a sample: accesses of V channels on
 // `lanes` lanes (any number), sites on the other threads' slices, E of them each.  x (and dy)
-// are read once, and no sums cross blocks but the weights' gradients.
+// are read once, and no sums cross blocks but the weights' gradients.  (2 x 64 x 32 fp32 forward:
+// 5.9 us, in three launches 14.)
 template <int V>
 struct WholePlace {
   long n, first, c;  // sample, tile's first channel, this thread's in the tile

@@ -1,5 +1,5 @@
-// Device helpers of the operators around the convolution (norm.hip, logprob.hip,
-// adamw.hip): element types, vector loads of any alignment, wave reductions.
+// Device helpers of the operators around the convolution (norm.hip, logprob.hip, adamw.hip,
+// gnorm*.hip, recur*.hip, muon*.hip): element types, vector loads of any alignment, wave reductions.
 #pragma once
 
 #include <cstdint>

