@@ -397,7 +397,8 @@ bl_status_t bl_muon_state_size(bl_muon_plan_t plan, size_t* bytes, long long* to
 bl_status_t bl_muon_workspace_size(bl_muon_plan_t plan, size_t* bytes);
 
 /* params, grads: host arrays of `count` device pointers (those of empty matrices may
- * be NULL).  Parameters and state are updated in place. */
+ * be NULL).  No two parameters share memory, nor does one with another's gradient.
+ * Parameters and state are updated in place. */
 bl_status_t bl_muon_step(bl_muon_plan_t plan, void* const* params, const void* const* grads, void* state, void* ws,
                          const bl_muon_args_t* args, void* stream);
 /* X of u = grad alone, rounded to nearest, to out (matrices of the parameters' type;

@@ -9,6 +9,7 @@ GPU's current stream (or the one given).  Buffers are the caller's;
 from __future__ import annotations
 
 import ctypes
+import itertools
 
 import torch
 
@@ -606,8 +607,24 @@ class MuonPlan(_Plan):
 
     def bind(self, params, grads):
         """The list of matrices that step() and orthogonalize() take: contiguous, of the
-        plan's sizes and types."""
-        return StepTensors(self, params, grads)
+        plan's sizes and types.  No two parameters share memory, nor does one with
+        another's gradient."""
+        tensors = StepTensors(self, params, grads)
+
+        def places(of):
+            return sorted((t.data_ptr(), t.data_ptr() + t.nbytes, i) for i, t in enumerate(of) if t is not None and t.nbytes)
+        own = places(tensors.params)
+        for (_, end, i), (start, _, j) in zip(own, own[1:]):
+            if start < end:
+                raise ValueError(f"parameters {i} and {j} share memory")
+        at = 0
+        for start, end, i in places(tensors.grads):
+            while at < len(own) and own[at][1] <= start:
+                at += 1
+            # (of two that it reaches into one is another's)
+            if any(j != i for _, _, j in itertools.takewhile(lambda q: q[0] < end, own[at:at + 2])):
+                raise ValueError(f"gradient {i} shares memory with another matrix's parameter")
+        return tensors
 
     def _bound(self, tensors):
         if tensors.plan is not self:
