@@ -23,7 +23,7 @@ def problem(t, kind, seed):
         return t.randn(*shape, generator=g).to(dtype).cuda()
     if kind in ("norm_whole", "norm_parts"):
         shape = (6, 200, 64, 8) if kind == "norm_whole" else (6, 5000, 48, 8)
-        plan = bltrain.GroupNormPlan(*shape, channels_last=True, act="silu", dtype=t.bfloat16)
+        plan = bltrain.GroupNormPlan(*shape, channels_last=True, act="silu", dtype=t.bfloat16, wdtype=t.bfloat16)
         x, dy, w, b = (rand(*s, dtype=t.bfloat16) for s in (shape[:3], shape[:3], shape[2:3], shape[2:3]))
         y, dx, dw, db, stats = *(t.empty_like(v) for v in (x, x, w, b)), t.empty(plan.stats_shape(), device="cuda")
         ws = plan.workspace()
