@@ -2,12 +2,12 @@
 //
 // Statistics span a sample's sites, and a group's channels may be one of 16 bits or all:
 // blocks take all channels of some sites (channels last) or sites of some channels (first),
-// leave what each channel gives there, and a launch of a wave a group joins it; a further
-// launch applies the result.  So x (backward: x and dy) is read twice, which memory bounds.  Where
+// leave what each channel gives there, and a launch of a wave a group joins it (or, where it is
+// little, every block that needs it for itself); a further launch applies the result.  So x (backward: x and dy) is read twice, which memory bounds.  Where
 // a block's registers can hold whole groups of a sample they are read once, by one launch.
 //
 // Kernels' times, bf16 (bytes as moved, with the second reading): 128 x 3136 x 64 channels last
-// forward 13.9 + 4.0 (join) + 20.6 us, 154 MB; 32 x 3136 x 256 backward 31.6 + 4.8 + 28.3 us, 257
+// forward 13.6 + 20.3 us, 154 MB; 32 x 3136 x 256 backward 31.6 + 4.8 + 28.3 us, 257
 // MB; in one launch fp32 channels first 64 x 256 x 512 backward 26.6 us, 101 MB, and 4.1 for the
 // weights' gradients.
 #include <algorithm>
@@ -114,7 +114,7 @@ GroupNormArgs args_of(const bl_group_norm_plan_s* p, void* ws) {
   a.part = reinterpret_cast<float*>(at + p->off_part);
   a.sums = reinterpret_cast<float*>(at + p->off_sums);
   a.own = reinterpret_cast<float*>(at + p->off_own);
-  a.batch = d.batch;
+  a.batch = a.own_rows = d.batch;
   a.sites = d.sites;
   a.channels = d.channels;
   a.groups = d.groups;
@@ -220,6 +220,9 @@ extern "C" bl_status_t bl_group_norm_plan_create(bl_group_norm_plan_t* out, cons
     if (wholes >= 1LL << 22 || (wholes < 128 && p->whole_threads[i] > kThreads)) p->whole_threads[i] = 0;
   p->chunk = std::min<long>(p->chunk, d.sites);
   p->chunks = (int)((d.sites + p->chunk - 1) / p->chunk);
+  p->joins[0] = d.layout == BL_CHANNELS_LAST && p->tiles == 1 && d.channels * p->chunks <= kMostJoined &&
+                p->each * p->chunks <= kMostOfGroup;
+  p->joins[1] = p->joins[0] && d.batch * p->chunks <= kMostRows;
   const size_t groups = (size_t)d.batch * d.groups, channels = (size_t)d.batch * d.channels;
   p->off_part = 0;
   p->off_sums = round_up(channels * p->chunks * 8, 16);

@@ -12,6 +12,7 @@ struct bl_group_norm_plan_s {
   int tiles;       // channels last: blocks along channels
   long chunk;      // sites of a block
   int chunks;      // of them
+  bool joins[2];   // channels last, forward and backward: the blocks that apply join the parts themselves
   // a block keeps whole groups of a sample in registers (threads 0: no block can)
   int whole_threads[2], whole_each[2];  // forward and backward: threads, accesses of one
   int whole_lanes;  // channels last: accesses of a site (`tile` channels); first: lanes of a channel
@@ -27,7 +28,8 @@ struct GroupNormArgs {
   float* stats;  // [2][batch][groups] mean, rstd
   float* part;   // [batch][chunks][channels][2]: forward mean and squares, backward sums of dz and dz h
   float* sums;   // backward [batch][groups][2]: means of u and of u h
-  float* own;    // backward [batch][channels][2]: part, summed over a sample
+  float* own;    // backward [own_rows][channels][2]: part, summed over a sample (or not)
+  long own_rows;
   long batch, sites, channels, groups, each;
   long x_stride, y_stride;
   long chunk;
@@ -116,6 +118,13 @@ __device__ __forceinline__ void moments_join(Moments& a, const Moments& b) {
   a.n = n;
 }
 
+// Parts of a sample that blocks which apply join, and of a group.  3 x 605 x 40 fp32 forward (160
+// parts) takes 14.2 us so and 17.6 with a launch that joins, 128 x 3136 x 64 bf16 (256) 34.8 and
+// 37.4; but 32 x 3136 x 256 (4096, which it was tried with) 41.1 and 38.4, 100 x 1024 x 50 (650) 22.4
+// and 20.1.  Backward the weights' gradients are then sums over all samples' chunks: 2002 of them
+// (182 x 7250 x 5 fp32) 39.6 and 31.3.
+constexpr long kMostJoined = 512, kMostOfGroup = 64, kMostRows = 512;
+
 bl_status_t gnorm_last_forward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
 bl_status_t gnorm_last_backward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
 bl_status_t gnorm_first_forward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
@@ -150,7 +159,7 @@ __device__ __forceinline__ void gnorm_weights_block(const GroupNormArgs& a, unsi
   if (c < a.channels) {
     const float* from = a.own + c * 2;
 #pragma unroll 8
-    for (long n = slice; n < a.batch; n += kWeightSlices) {
+    for (long n = slice; n < a.own_rows; n += kWeightSlices) {
       const Pack<float, 2> v = load_pack<float, 2>(from + n * a.channels * 2);
       db += v.v[0];
       dw += v.v[1];

@@ -28,9 +28,9 @@ struct LastPlace {
   int lane, slice, slices;
   bool there;
   template <int V>
-  __device__ __forceinline__ static LastPlace make(const GroupNormArgs& a) {
+  __device__ __forceinline__ static LastPlace make(const GroupNormArgs& a, unsigned block) {
     LastPlace p;
-    const long q = (long)blockIdx.x / a.tiles, tile = (long)blockIdx.x - q * a.tiles;
+    const long q = (long)block / a.tiles, tile = (long)block - q * a.tiles;
     p.n = q / a.chunks;
     p.chunk = q - p.n * a.chunks;
     p.slices = kThreads / a.lanes;
@@ -93,7 +93,7 @@ __device__ __forceinline__ void slices_sum(float (&v)[N], float* red, const Last
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void k_last_part(GroupNormArgs a) {
   __shared__ float red[kThreads * V];
-  const LastPlace p = LastPlace::make<V>(a);
+  const LastPlace p = LastPlace::make<V>(a, blockIdx.x);
   const T* x = static_cast<const T*>(a.x) + p.n * a.x_stride + p.c;
   float n = 0.f, mean[V] = {}, m2[V] = {};
   if (p.there)
@@ -141,30 +141,98 @@ __global__ __launch_bounds__(kThreads) void k_last_part(GroupNormArgs a) {
   for (int j = 0; j < V; ++j) to[2 * j] = sum[j], to[2 * j + 1] = m2[j];
 }
 
+// Two sums over each group's parts in a sample, of one chunk and channel each, by as many lanes of
+// a wave as there are parts: first(part), then second(part, the first sum), and done(group, both).
+// Every thread calls it.
+template <typename Value, typename First, typename Second, typename Done>
+__device__ __forceinline__ void join_parts(const GroupNormArgs& a, long n, First&& first, Second&& second, Done&& done) {
+  const int parts = (int)a.each * a.chunks, each = (int)a.each;
+  int on = 1;
+  while (on < parts) on *= 2;
+  const int lane = threadIdx.x % on, k = lane / each, c = lane - k * each;
+  for (long g0 = 0; g0 < a.groups; g0 += kThreads / on) {
+    const long g = g0 + threadIdx.x / on;
+    const bool there = g < a.groups && lane < parts;
+    Value v;
+    v.load(a, there, there ? a.part + ((n * a.chunks + k) * a.channels + g * each + c) * 2 : a.part,
+           there ? g * each + c : 0, k);
+    const float s1 = wave_sum(first(v), on), s2 = wave_sum(second(v, s1), on);
+    if (there && lane == 0) done(g, s1, s2);
+  }
+}
+// A part's sites (0: there is none), mean and squares about it.
+struct PartMoments {
+  float sites, mean, m2;
+  __device__ __forceinline__ void load(const GroupNormArgs& a, bool there, const float* from, long, int chunk) {
+    const Pack<float, 2> v = load_pack<float, 2>(from);
+    sites = there ? (float)min(a.chunk, a.sites - (long)chunk * a.chunk) : 0.f;
+    mean = there ? v.v[0] : 0.f;
+    m2 = there ? v.v[1] : 0.f;
+  }
+};
+// A part's sums of u = dz w and of u h; every product and sum rounds by itself, so that a group
+// of one value, whose u is its mean, has a gradient of 0.
+template <typename T>
+struct PartSums {
+  float u, uh;
+  __device__ __forceinline__ void load(const GroupNormArgs& a, bool there, const float* from, long c, int) {
+#pragma clang fp contract(off)
+    const Pack<float, 2> v = load_pack<float, 2>(from);
+    const float w = weight_at<T>(a.w, a.wide, c, 1.f);
+    u = there ? v.v[0] * w : 0.f;
+    uh = there ? v.v[1] * w : 0.f;
+  }
+};
+
 // What a thread's channels need: statistics and weights.
 template <typename T, int V>
 struct LastChannels {
   float mean[V], rstd[V], w[V], b[V];
-  __device__ __forceinline__ void load(const GroupNormArgs& a, const LastPlace& p) {
-    const long all = a.batch * a.groups;
+  // stats: of the sample's groups, rstd `all` behind mean
+  __device__ __forceinline__ void load(const GroupNormArgs& a, const LastPlace& p, const float* stats, long all) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const long c = p.there ? p.c + j : 0, q = p.n * a.groups + c / a.each;
-      mean[j] = a.stats[q];
-      rstd[j] = a.stats[all + q];
+      const long c = p.there ? p.c + j : 0, q = c / a.each;
+      mean[j] = stats[q];
+      rstd[j] = stats[all + q];
       w[j] = weight_at<T>(a.w, a.wide, c, 1.f);
       b[j] = weight_at<T>(a.b, a.wide, c, 0.f);
     }
   }
+  __device__ __forceinline__ void load(const GroupNormArgs& a, const LastPlace& p) {
+    load(a, p, a.stats + p.n * a.groups, a.batch * a.groups);
+  }
 };
 
-template <typename T, int V, int ACT>
+// JOINS: the statistics are joined here, by each block for itself (the first of a sample leaves them).
+template <typename T, int V, int ACT, bool JOINS>
 __global__ __launch_bounds__(kThreads) void k_last_apply(GroupNormArgs a) {
-  const LastPlace p = LastPlace::make<V>(a);
+  const LastPlace p = LastPlace::make<V>(a, blockIdx.x);
   const T* x = static_cast<const T*>(a.x) + p.n * a.x_stride + p.c;
   T* y = static_cast<T*>(a.y) + p.n * a.y_stride + p.c;
   LastChannels<T, V> own;
-  own.load(a, p);
+  if constexpr (JOINS) {
+    __shared__ float stats[2 * kMostJoined];
+    const float size = (float)a.sites * (float)a.each;
+    join_parts<PartMoments>(
+        a, p.n, [](const PartMoments& v) { return v.sites * v.mean; },
+        [&](const PartMoments& v, float sum) {
+          const float d = v.mean - sum / size;
+          return fmaf(v.sites * d, d, v.m2);
+        },
+        [&](long g, float sum, float m2) {
+          const float mean = sum / size, rstd = 1.f / sqrtf(m2 / size + a.eps);
+          stats[g] = mean;
+          stats[kMostJoined + g] = rstd;
+          if (p.chunk) return;
+          a.stats[p.n * a.groups + g] = mean;
+          a.stats[(a.batch + p.n) * a.groups + g] = rstd;
+        });
+    __syncthreads();
+    own.load(a, p, stats, kMostJoined);
+  } else {
+    own.load(a, p);
+  }
   if (!p.there) return;
   p.walk<kAhead<T, V>, Held<T, V>>(
       [&](Held<T, V>& to, long site) { to.load(x + site * a.channels, V); },
@@ -199,7 +267,7 @@ struct HeldBoth {
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void k_last_bwd_part(GroupNormArgs a) {
   __shared__ float red[kThreads * 2 * V];
-  const LastPlace p = LastPlace::make<V>(a);
+  const LastPlace p = LastPlace::make<V>(a, blockIdx.x);
   const T* x = static_cast<const T*>(a.x) + p.n * a.x_stride + p.c;
   const T* dy = static_cast<const T*>(a.dy) + p.n * a.y_stride + p.c;
   LastChannels<T, V> own;
@@ -229,24 +297,40 @@ __global__ __launch_bounds__(kThreads) void k_last_bwd_part(GroupNormArgs a) {
   for (int j = 0; j < 2 * V; ++j) to[j] = s[j];
 }
 
-template <typename T, int V, int ACT>
+// (the blocks past the values' own sum the weights' gradients)
+template <typename T, int V, int ACT, bool JOINS>
 __global__ __launch_bounds__(kThreads) void k_last_bwd_apply(GroupNormArgs a, unsigned blocks) {
-  if (blockIdx.x >= blocks) {
-    gnorm_weights_block<T>(a, blockIdx.x - blocks);
+  // (JOINS: these come first, as they have more to sum)
+  const unsigned sums = gridDim.x - blocks, block = JOINS ? blockIdx.x - sums : blockIdx.x;
+  if (block >= blocks) {
+    gnorm_weights_block<T>(a, JOINS ? blockIdx.x : blockIdx.x - blocks);
     return;
   }
-  const LastPlace p = LastPlace::make<V>(a);
+  const LastPlace p = LastPlace::make<V>(a, block);
   const T* x = static_cast<const T*>(a.x) + p.n * a.x_stride + p.c;
   const T* dy = static_cast<const T*>(a.dy) + p.n * a.y_stride + p.c;
   T* dx = static_cast<T*>(a.dx) + p.n * a.x_stride + p.c;
   LastChannels<T, V> own;
   own.load(a, p);
+  const float* means = a.sums + 2 * p.n * a.groups;
+  if constexpr (JOINS) {
+    __shared__ float joined[2 * kMostJoined];
+    const float size = (float)a.sites * (float)a.each;
+    join_parts<PartSums<T>>(
+        a, p.n, [](const PartSums<T>& v) { return v.u; }, [](const PartSums<T>& v, float) { return v.uh; },
+        [&](long g, float u, float uh) {
+          joined[2 * g] = u / size;
+          joined[2 * g + 1] = uh / size;
+        });
+    __syncthreads();
+    means = joined;
+  }
   float c1[V], c2[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const long q = p.n * a.groups + (p.there ? p.c + j : 0) / a.each;
-    c1[j] = a.sums[2 * q];
-    c2[j] = a.sums[2 * q + 1];
+    const long q = (p.there ? p.c + j : 0) / a.each;
+    c1[j] = means[2 * q];
+    c2[j] = means[2 * q + 1];
   }
   if (!p.there) return;
   p.walk<kAheadBoth<T, V>, HeldBoth<T, V>>(
@@ -541,12 +625,14 @@ bl_status_t gnorm_last_forward(const bl_group_norm_plan_s* p, const GroupNormArg
       hipExtLaunchKernelGGL((k_last_part<decltype(t), decltype(v)::value>), grid, block, 0, s, e0, e1, 0, a);
     });
   });
-  if (st == BL_OK) st = gnorm_join_forward(a, s);
+  if (st == BL_OK && !p->joins[0]) st = gnorm_join_forward(a, s);
   if (st != BL_OK) return st;
   return timed_launch("gnorm_fwd", 2.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
     with_act(p->d.act, [&](auto act) {
       dispatch(p, [&](auto t, auto v) {
-        hipExtLaunchKernelGGL((k_last_apply<decltype(t), decltype(v)::value, decltype(act)::value>), grid, block, 0, s,
+        using T = decltype(t);
+        constexpr int V = decltype(v)::value, A = decltype(act)::value;
+        hipExtLaunchKernelGGL((p->joins[0] ? k_last_apply<T, V, A, true> : k_last_apply<T, V, A, false>), grid, block, 0, s,
                               e0, e1, 0, a);
       });
     });
@@ -578,14 +664,17 @@ bl_status_t gnorm_last_backward(const bl_group_norm_plan_s* p, const GroupNormAr
       });
     });
   });
-  if (st == BL_OK) st = gnorm_join_backward(a, p->d.dtype, s);
+  if (st == BL_OK && !p->joins[1]) st = gnorm_join_backward(a, p->d.dtype, s);
   if (st != BL_OK) return st;
-  // (the blocks past the values' own sum the weights' gradients)
+  GroupNormArgs rest = a;
+  if (p->joins[1]) rest.own = a.part, rest.own_rows = a.batch * a.chunks;
   return timed_launch("gnorm_bwd", 3.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
     with_act(p->d.act, [&](auto act) {
       dispatch(p, [&](auto t, auto v) {
-        hipExtLaunchKernelGGL((k_last_bwd_apply<decltype(t), decltype(v)::value, decltype(act)::value>),
-                              dim3(grid.x + gnorm_weights_blocks(a)), block, 0, s, e0, e1, 0, a, grid.x);
+        using T = decltype(t);
+        constexpr int V = decltype(v)::value, A = decltype(act)::value;
+        hipExtLaunchKernelGGL((p->joins[1] ? k_last_bwd_apply<T, V, A, true> : k_last_bwd_apply<T, V, A, false>),
+                              dim3(grid.x + gnorm_weights_blocks(a)), block, 0, s, e0, e1, 0, rest, grid.x);
       });
     });
   });
