@@ -9,8 +9,10 @@
 // only for the first A and for X = (... B2 B1) X, and square products in between, which are
 // symmetric since all are polynomials of A.  Of m by 4 m that is 19 / 32 of the single steps'
 // operations, of squares the same.  But what rounds in A grows by B B where B A B is formed
-// and not from X: a joined run ends before its B's product may exceed 48 (three usual steps;
-// all five lose a digit or two where a gradient has a few strong directions, these none).
+// and not from X: a joined run ends before its B's product may exceed 48 (three usual steps).
+// Where a gradient has a few strong directions, five usual steps of 50 x 128 ... 256 x 640 in fp32
+// are off by 0.9 to 1.8e-6 of the norm one by one, by 2.1 to 3.8e-6 in runs of three and two, by 1.5e-5 to
+// 1e-4 in longer ones: and that only if the square matrices are symmetric to the last bit.
 #include <algorithm>
 #include <cmath>
 #include <new>

@@ -8,7 +8,9 @@
 // last, low low, is below 2^-22) and sums in fp32.  One fp16 part alone leaves errors of 1 %
 // in the result where a gradient has a few strong directions: rounding is noise in all
 // directions, and the steps raise the weak ones by up to 3.44 each.  Symmetric products
-// are taken for tiles on and below the diagonal only and stored twice.
+// are taken on and below the diagonal only and stored twice, in the tiles on it too: what they
+// held of an antisymmetric part would grow tenfold with every joined step (64 x 1100 after five steps:
+// off by 3e-5 of the norm with both halves of those tiles as computed).
 //
 // Bound by the matrix cores where there are many tiles: 1024 x 4096 and squares of 1024, 126 M
 // values, 5.0e12 operations in 6.7 ms (0.65 of what a library's fp16 product of 8192 reaches, 1.15e15
@@ -253,7 +255,8 @@ __global__ __launch_bounds__(MuonShape<SIDE>::kThreads, MuonShape<SIDE>::kBlocks
   char* along = MODE == kApply ? part + w.x : across;
   const size_t along_row = MODE == kApply ? nn : mm;
   const float scale = second ? q.scale2 : q.scale;
-  const bool both = MODE == kApply || p.ti != p.tj, there = wave_there<SIDE>(p);
+  // (on the diagonal the values below it, with what of their blocks of 8 x 8 lies on it read from both sides)
+  const bool diagonal = MODE != kApply && p.ti == p.tj, there = wave_there<SIDE>(p);
 #pragma unroll
   for (int tp = 0; tp < S::kSub; ++tp) {
     if (there)
@@ -272,19 +275,22 @@ __global__ __launch_bounds__(MuonShape<SIDE>::kThreads, MuonShape<SIDE>::kBlocks
 #pragma unroll
           for (int k = 0; k < 4; ++k) v[k] *= scale;
         }
-        hold<4>(across + place, v);
-        if (both)
+        if (!diagonal || row / 8 > col / 8) hold<4>(across + place, v);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) tiled[(row / (S::kSub * 32) * 32 + row % 32 + k) * SIDE + col] = v[k];
+        for (int k = 0; k < 4; ++k) tiled[(row / (S::kSub * 32) * 32 + row % 32 + k) * SIDE + col] = v[k];
       });
-    if (!both) continue;
     __syncthreads();
     for (int i = threadIdx.x; i < S::kGrid * 32 * SIDE / 8; i += S::kThreads) {
       const int r = i / (SIDE / 8), c = i % (SIDE / 8) * 8, row = (r / 32 * S::kSub + tp) * 32 + r % 32;
       if (SIDE > 64 && ((unsigned)row / 64 >= p.p_rows || (unsigned)c / 64 >= p.q_rows)) continue;
+      if (diagonal && row / 8 < c / 8) continue;
+      const bool turned = diagonal && row / 8 == c / 8;
       float v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = tiled[r * SIDE + c + j];
+      for (int j = 0; j < 8; ++j) {
+        const int up = turned ? max(c + j - row, 0) : 0;  // from above the diagonal to below it
+        v[j] = tiled[(r + up) * SIDE + c + j - up];
+      }
       hold<8>(along + held_at((size_t)p.ti * SIDE + row, along_row, p.tj * SIDE + c), v);
     }
     if (tp + 1 < S::kSub) __syncthreads();

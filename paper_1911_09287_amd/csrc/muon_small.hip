@@ -61,9 +61,27 @@ __device__ __forceinline__ f32x4 held(char* slot, int row, int c) {
   for (int j = 0; j < 4; ++j) v[j] = (float)hi.v[j] + (float)lo.v[j];
   return v;
 }
-// This wave's tile of a product of square matrices, over `sum` times 32.  Its lane's four values
-// are rows of a column, and of the symmetric result so are four of a row: hold(slot, column,
-// first row, ...).
+// A symmetric result: a lane's four values are rows r ... r + 3 of column c, and go to its columns r ...
+// r + 3 of row c too.  Values above the diagonal are left out, so that what is held is symmetric to the
+// last bit: an antisymmetric part would grow tenfold with every joined step (50 x 128 after five steps: off
+// by 3e-5 of the norm with both halves as computed, 3e-6 so).
+__device__ __forceinline__ void hold_both(char* slot, int r, int c, const f32x4& v) {
+  if (r >= c) hold(slot, c, r, v);
+  Pack<f16_t, 4> hi, lo;
+  split4(v, hi, lo);
+  const int k = c / 32 * 8 + c % 32 / 8, at = c % 8 * 2;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (r + j < c) continue;
+    *reinterpret_cast<f16_t*>(piece(slot, r + j, k) + at) = hi.v[j];
+    *reinterpret_cast<f16_t*>(piece(slot, r + j, k + 4) + at) = lo.v[j];
+    if (r >= c) continue;
+    const int kr = (r + j) / 32 * 8 + (r + j) % 32 / 8, at_r = (r + j) % 8 * 2;
+    *reinterpret_cast<f16_t*>(piece(slot, c, kr) + at_r) = hi.v[j];
+    *reinterpret_cast<f16_t*>(piece(slot, c, kr + 4) + at_r) = lo.v[j];
+  }
+}
+// This wave's tile of a product of square matrices, over `sum` times 32.
 __device__ __forceinline__ f32x4 square(char* p, char* q, int sum) {
   const int wave = threadIdx.x / kWave;
   f32x4 acc = {};
@@ -156,8 +174,8 @@ __global__ __launch_bounds__(kT) void k_muon_small(MuonList list, MuonSmallSteps
   }
   auto slot = [&](int s) { return lds + s * kSlotBytes; };
   const int tr = wave / 4 * 16, tc = wave % 4 * 16;
-  const int at_row = tc + lane_row(), at_col = tr + lane_quad() * 4;  // of a lane's four values in a slot
-  const bool mine = tr < side && tc < side;
+  const int col = tc + lane_row(), row = tr + lane_quad() * 4;  // of a lane's four values: rows row ... row + 3
+  const bool mine = tr < side && tc <= tr;  // (tiles on and below the diagonal)
   float keep = 1.f, rate = 1.f;
   unsigned key = a.key;
   if (!a.set) {
@@ -186,27 +204,27 @@ __global__ __launch_bounds__(kT) void k_muon_small(MuonList list, MuonSmallSteps
           fragments_at(q, s, fq);
           multiply(fp, fq, acc);
         }
-        hold(slot(kSlotA), at_row, at_col, acc * (kHoldA / (kHoldX * kHoldX)));
+        hold_both(slot(kSlotA), row, col, acc * (kHoldA / (kHoldX * kHoldX)));
       }
       __syncthreads();
     }
     const int b = step.first && !step.last ? kSlotQ0 : kSlotB;
     if (mine) {
-      f32x4 v = square(slot(kSlotA), slot(kSlotA), half) * step.c + held(slot(kSlotA), at_row, at_col) * step.b;
+      f32x4 v = square(slot(kSlotA), slot(kSlotA), half) * step.c + held(slot(kSlotA), col, row) * step.b;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (at_col + j == at_row) v[j] += step.a;
-      hold(slot(b), at_row, at_col, v);
+        if (row + j == col) v[j] += step.a;
+      hold_both(slot(b), row, col, v);
     }
     __syncthreads();
     // the product so far times B, and A B, then B (A B)
     const int next = step.first ? b : product == kSlotQ0 ? kSlotQ1 : kSlotQ0;
     if (mine && !step.first)
-      hold(slot(next), at_row, at_col, square(slot(b), slot(product), half) * (step.hold_q / (step.hold_b * hold_q)));
+      hold_both(slot(next), row, col, square(slot(b), slot(product), half) * (step.hold_q / (step.hold_b * hold_q)));
     if (!step.last) {
-      if (mine) hold(slot(kSlotAB), at_row, at_col, square(slot(b), slot(kSlotA), half) * back);
+      if (mine) hold_both(slot(kSlotAB), row, col, square(slot(b), slot(kSlotA), half) * back);
       __syncthreads();
-      if (mine) hold(slot(kSlotA), at_row, at_col, square(slot(b), slot(kSlotAB), half) * back);
+      if (mine) hold_both(slot(kSlotA), row, col, square(slot(b), slot(kSlotAB), half) * back);
     }
     product = next;
     hold_q = step.hold_q;
