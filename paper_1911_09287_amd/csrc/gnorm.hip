@@ -105,6 +105,17 @@ __global__ __launch_bounds__(kThreads) void k_gnorm_weights(GroupNormArgs a) {
   gnorm_weights_block<T>(a, blockIdx.x);
 }
 
+// Block k + weights' blocks times slab: its channels' sums over a slab.
+__global__ __launch_bounds__(kThreads) void k_gnorm_slabs(GroupNormArgs a, long slab) {
+  const unsigned across = (unsigned)((a.channels + kWave - 1) / kWave), q = blockIdx.x / across;
+  gnorm_rows_sum(a.own, a.channels, q * slab, min(a.own_rows, (q + 1) * slab), blockIdx.x - q * across,
+                 [&](long c, float db, float dw) {
+                   float* to = a.slabs + (q * a.channels + c) * 2;
+                   to[0] = db;
+                   to[1] = dw;
+                 });
+}
+
 unsigned blocks_for(long n, long each) { return (unsigned)((n + each - 1) / each); }
 
 GroupNormArgs args_of(const bl_group_norm_plan_s* p, void* ws) {
@@ -114,6 +125,7 @@ GroupNormArgs args_of(const bl_group_norm_plan_s* p, void* ws) {
   a.part = reinterpret_cast<float*>(at + p->off_part);
   a.sums = reinterpret_cast<float*>(at + p->off_sums);
   a.own = reinterpret_cast<float*>(at + p->off_own);
+  a.slabs = reinterpret_cast<float*>(at + p->off_slabs);
   a.batch = a.own_rows = d.batch;
   a.sites = d.sites;
   a.channels = d.channels;
@@ -157,6 +169,17 @@ bl_status_t gnorm_weights(const GroupNormArgs& a, int dtype, hipStream_t s) {
     if (dtype == BL_F16) hipExtLaunchKernelGGL(k_gnorm_weights<f16_t>, grid, dim3(kThreads), 0, s, e0, e1, 0, a);
     else hipExtLaunchKernelGGL(k_gnorm_weights<bf16_t>, grid, dim3(kThreads), 0, s, e0, e1, 0, a);
   });
+}
+
+bl_status_t gnorm_slabs(const bl_group_norm_plan_s* p, GroupNormArgs& a, hipStream_t s) {
+  if (!p->slabs || (!a.dw && !a.db)) return BL_OK;
+  const bl_status_t st = timed_launch("gnorm_slabs", 8.0 * a.batch * a.channels, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    hipExtLaunchKernelGGL(k_gnorm_slabs, dim3(gnorm_weights_blocks(a) * (unsigned)p->slabs), dim3(kThreads), 0, s, e0, e1, 0,
+                          a, p->slab);
+  });
+  a.own = a.slabs;
+  a.own_rows = p->slabs;
+  return st;
 }
 
 }  // namespace blc
@@ -223,11 +246,17 @@ extern "C" bl_status_t bl_group_norm_plan_create(bl_group_norm_plan_t* out, cons
   p->joins[0] = d.layout == BL_CHANNELS_LAST && p->tiles == 1 && d.channels * p->chunks <= kMostJoined &&
                 p->each * p->chunks <= kMostOfGroup;
   p->joins[1] = p->joins[0] && d.batch * p->chunks <= kMostRows;
+  const long slices = kThreads / gnorm_rows_cols(d.channels);
+  if (!p->joins[1] && d.batch > kMostOwn * slices) {
+    p->slab = std::max<long>(kLeastOwn * slices, (d.batch + kMostSlabs - 1) / kMostSlabs);
+    p->slabs = (d.batch + p->slab - 1) / p->slab;
+  }
   const size_t groups = (size_t)d.batch * d.groups, channels = (size_t)d.batch * d.channels;
   p->off_part = 0;
   p->off_sums = round_up(channels * p->chunks * 8, 16);
   p->off_own = p->off_sums + round_up(groups * 8, 16);
-  p->bytes = d.batch ? p->off_own + channels * 8 : 0;
+  p->off_slabs = p->off_own + round_up(channels * 8, 16);
+  p->bytes = d.batch ? p->off_slabs + (size_t)p->slabs * d.channels * 8 : 0;
   // a launch has fewer than 2^32 threads
   const __int128 blocks = d.layout == BL_CHANNELS_LAST
                               ? (__int128)d.batch * p->chunks * p->tiles

@@ -17,7 +17,8 @@ struct bl_group_norm_plan_s {
   int whole_threads[2], whole_each[2];  // forward and backward: threads, accesses of one
   int whole_lanes;  // channels last: accesses of a site (`tile` channels); first: lanes of a channel
   int whole_tiles;  // channels last: blocks of a sample
-  size_t off_part, off_sums, off_own, bytes;
+  long slab, slabs;  // samples whose sums are added at a time, and such parts (0: all at once)
+  size_t off_part, off_sums, off_own, off_slabs, bytes;
 };
 
 namespace blc {
@@ -30,6 +31,7 @@ struct GroupNormArgs {
   float* sums;   // backward [batch][groups][2]: means of u and of u h
   float* own;    // backward [own_rows][channels][2]: part, summed over a sample (or not)
   long own_rows;
+  float* slabs;  // backward [slabs][channels][2]: own, summed over a slab's samples
   long batch, sites, channels, groups, each;
   long x_stride, y_stride;
   long chunk;
@@ -124,6 +126,10 @@ __device__ __forceinline__ void moments_join(Moments& a, const Moments& b) {
 // and 20.1.  Backward the weights' gradients are then sums over all samples' chunks: 2002 of them
 // (182 x 7250 x 5 fp32) 39.6 and 31.3.
 constexpr long kMostJoined = 512, kMostOfGroup = 64, kMostRows = 512;
+// Rows of samples' sums that a thread adds: of more, slabs are cut, in which it has two trees of 16 at least, and
+// 256 of them at most (64 of a thread that adds them).  Backward, bf16: 600 x 1 x 1024 23.7 us in slabs, 24.7 in one
+// launch, 4000 x 1 x 64 20.1 and 65, 65536 x 1 x 64 139 and 855.
+constexpr long kMostOwn = 128, kLeastOwn = 32, kMostSlabs = 256;
 
 bl_status_t gnorm_last_forward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
 bl_status_t gnorm_last_backward(const bl_group_norm_plan_s* p, const GroupNormArgs& a, hipStream_t s);
@@ -149,42 +155,74 @@ bl_status_t gnorm_join_forward(const GroupNormArgs& a, hipStream_t s);
 bl_status_t gnorm_join_backward(const GroupNormArgs& a, int dtype, hipStream_t s);
 // dw and db from the samples' sums (batch = 0: zeros); as a launch of its own, or by the blocks
 // of another one past its own, of kThreads threads.
-constexpr int kWeightSlices = kThreads / kWave;
-template <typename T>
-__device__ __forceinline__ void gnorm_weights_block(const GroupNormArgs& a, unsigned block) {
-  __shared__ float red[2][kWeightSlices][kWave];
-  const int col = threadIdx.x % kWave, slice = threadIdx.x / kWave;
-  const long c = (long)block * kWave + col;
-  float db = 0.f, dw = 0.f;
-  if (c < a.channels) {
-    const float* from = a.own + c * 2;
-#pragma unroll 8
-    for (long n = slice; n < a.own_rows; n += kWeightSlices) {
-      const Pack<float, 2> v = load_pack<float, 2>(from + n * a.channels * 2);
-      db += v.v[0];
-      dw += v.v[1];
+//
+// Many samples are cut into slabs, whose sums a launch before adds (gnorm_slabs), so that neither the time
+// nor the rounding grows with their number: a thread takes every `slices`th row, sixteen at a time whose loads
+// are in flight together and whose sum is a tree, and the slices are joined in halves.  (One value in 20000
+// rows is off by up to 2 half ulps so; added one after another in four slices by 800.)
+constexpr int kRowsAhead = 16;
+// Channels that a block takes: a power of two, so that few leave more slices of rows.
+__host__ __device__ inline int gnorm_rows_cols(long channels) {
+  int cols = kWave;
+  while (cols > 1 && cols / 2 >= channels) cols /= 2;
+  return cols;
+}
+// Sums over rows [from, to) of the pairs of this block's channels: put(c, first, second), a thread a channel.
+template <typename Put>
+__device__ __forceinline__ void gnorm_rows_sum(const float* own, long channels, long from, long to, unsigned block, Put&& put) {
+  __shared__ float red[2][kThreads / kWave][kWave];
+  const int cols = gnorm_rows_cols(channels);
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int col = threadIdx.x % cols, slice = threadIdx.x / cols, slices = kThreads / cols;
+  const long c = (long)block * kWave + col, at = min(c, channels - 1);
+  float s[2] = {};
+  for (long n = from + slice; n < to; n += kRowsAhead * slices) {
+    float v[2][kRowsAhead];
+#pragma unroll
+    for (int k = 0; k < kRowsAhead; ++k) {  // (the last row again, and not counted)
+      const Pack<float, 2> got = load_pack<float, 2>(own + (min(n + (long)k * slices, to - 1) * channels + at) * 2);
+      v[0][k] = got.v[0], v[1][k] = got.v[1];
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+      for (int k = 0; k < kRowsAhead; ++k) v[j][k] = n + (long)k * slices < to ? v[j][k] : 0.f;
+#pragma unroll
+      for (int half = kRowsAhead / 2; half; half /= 2)
+#pragma unroll
+        for (int k = 0; k < half; ++k) v[j][k] += v[j][k + half];
+      s[j] += v[j][0];
     }
   }
-  red[0][slice][col] = db;
-  red[1][slice][col] = dw;
+  for (int d = cols; d < kWave; d *= 2) s[0] += __shfl_xor(s[0], d), s[1] += __shfl_xor(s[1], d);
+  red[0][wave][lane] = s[0];
+  red[1][wave][lane] = s[1];
   __syncthreads();
-  if (slice || c >= a.channels) return;
-  db = dw = 0.f;
+  if (slice || c >= channels) return;
 #pragma unroll
-  for (int k = 0; k < kWeightSlices; ++k) db += red[0][k][col], dw += red[1][k][col];
-  if (a.dw) {
-    if (a.wide) static_cast<float*>(a.dw)[c] = dw;
-    else static_cast<T*>(a.dw)[c] = (T)dw;
-  }
-  if (a.db) {
-    if (a.wide) static_cast<float*>(a.db)[c] = db;
-    else static_cast<T*>(a.db)[c] = (T)db;
-  }
+  for (int j = 0; j < 2; ++j) s[j] = (red[j][0][col] + red[j][1][col]) + (red[j][2][col] + red[j][3][col]);
+  static_assert(kThreads == 4 * kWave, "the waves above");
+  put(c, s[0], s[1]);
+}
+template <typename T>
+__device__ __forceinline__ void gnorm_weights_block(const GroupNormArgs& a, unsigned block) {
+  gnorm_rows_sum(a.own, a.channels, 0, a.own_rows, block, [&](long c, float db, float dw) {
+    if (a.dw) {
+      if (a.wide) static_cast<float*>(a.dw)[c] = dw;
+      else static_cast<T*>(a.dw)[c] = (T)dw;
+    }
+    if (a.db) {
+      if (a.wide) static_cast<float*>(a.db)[c] = db;
+      else static_cast<T*>(a.db)[c] = (T)db;
+    }
+  });
 }
 inline unsigned gnorm_weights_blocks(const GroupNormArgs& a) {
   return a.dw || a.db ? (unsigned)((a.channels + kWave - 1) / kWave) : 0;
 }
 bl_status_t gnorm_weights(const GroupNormArgs& a, int dtype, hipStream_t s);
+// Where a plan's samples are many: the sums of its slabs, which are a.own's rows from then on.
+bl_status_t gnorm_slabs(const bl_group_norm_plan_s* p, GroupNormArgs& a, hipStream_t s);
 
 // go(act) as a constant.
 template <typename Go>

@@ -418,7 +418,7 @@ bl_status_t gnorm_first_backward(const bl_group_norm_plan_s* p, const GroupNormA
   const dim3 grid = grid_of(a), block(kThreads);
   const double bytes = (double)a.batch * a.sites * a.channels * dtype_bytes(p->d.dtype);
   if (p->whole_threads[1]) {
-    const bl_status_t st = timed_launch("gnorm_bwd", 3.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    bl_status_t st = timed_launch("gnorm_bwd", 3.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
       with_act(p->d.act, [&](auto act) {
         with_each(p->whole_each[1], [&](auto e) {
           dispatch(p, [&](auto t, auto v) {
@@ -429,7 +429,9 @@ bl_status_t gnorm_first_backward(const bl_group_norm_plan_s* p, const GroupNormA
         });
       });
     });
-    return st == BL_OK ? gnorm_weights(a, p->d.dtype, s) : st;
+    GroupNormArgs rest = a;
+    if (st == BL_OK) st = gnorm_slabs(p, rest, s);
+    return st == BL_OK ? gnorm_weights(rest, p->d.dtype, s) : st;
   }
   bl_status_t st = timed_launch("gnorm_bwd_part", 2.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
     with_act(p->d.act, [&](auto act) {
@@ -440,13 +442,15 @@ bl_status_t gnorm_first_backward(const bl_group_norm_plan_s* p, const GroupNormA
     });
   });
   if (st == BL_OK) st = gnorm_join_backward(a, p->d.dtype, s);
+  GroupNormArgs rest = a;
+  if (st == BL_OK) st = gnorm_slabs(p, rest, s);
   if (st != BL_OK) return st;
   // (the blocks past the values' own sum the weights' gradients)
   return timed_launch("gnorm_bwd", 3.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
     with_act(p->d.act, [&](auto act) {
       dispatch(p, [&](auto t, auto v) {
         hipExtLaunchKernelGGL((k_first_bwd_apply<decltype(t), decltype(v)::value, decltype(act)::value>),
-                              dim3(grid.x + gnorm_weights_blocks(a)), block, 0, s, e0, e1, 0, a, grid.x);
+                              dim3(grid.x + gnorm_weights_blocks(a)), block, 0, s, e0, e1, 0, rest, grid.x);
       });
     });
   });

@@ -643,7 +643,7 @@ bl_status_t gnorm_last_backward(const bl_group_norm_plan_s* p, const GroupNormAr
   const dim3 grid((unsigned)(a.batch * a.chunks * a.tiles)), block(kThreads);
   const double bytes = (double)a.batch * a.sites * a.channels * dtype_bytes(p->d.dtype);
   if (p->whole_threads[1]) {
-    const bl_status_t st = timed_launch("gnorm_bwd", 3.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
+    bl_status_t st = timed_launch("gnorm_bwd", 3.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
       with_act(p->d.act, [&](auto act) {
         with_each(p->whole_each[1], [&](auto e) {
           dispatch(p, [&](auto t, auto v) {
@@ -654,7 +654,9 @@ bl_status_t gnorm_last_backward(const bl_group_norm_plan_s* p, const GroupNormAr
         });
       });
     });
-    return st == BL_OK ? gnorm_weights(a, p->d.dtype, s) : st;
+    GroupNormArgs rest = a;
+    if (st == BL_OK) st = gnorm_slabs(p, rest, s);
+    return st == BL_OK ? gnorm_weights(rest, p->d.dtype, s) : st;
   }
   bl_status_t st = timed_launch("gnorm_bwd_part", 2.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
     with_act(p->d.act, [&](auto act) {
@@ -665,9 +667,10 @@ bl_status_t gnorm_last_backward(const bl_group_norm_plan_s* p, const GroupNormAr
     });
   });
   if (st == BL_OK && !p->joins[1]) st = gnorm_join_backward(a, p->d.dtype, s);
-  if (st != BL_OK) return st;
   GroupNormArgs rest = a;
   if (p->joins[1]) rest.own = a.part, rest.own_rows = a.batch * a.chunks;
+  else if (st == BL_OK) st = gnorm_slabs(p, rest, s);
+  if (st != BL_OK) return st;
   return timed_launch("gnorm_bwd", 3.0 * bytes, 0.0, s, [&](hipEvent_t e0, hipEvent_t e1) {
     with_act(p->d.act, [&](auto act) {
       dispatch(p, [&](auto t, auto v) {

@@ -4,8 +4,9 @@ or far values (MI355X).  U = 2^-24; each test says where its tolerance comes fro
 import pytest
 
 from paper_1911_09287_amd import bltrain
+from test_group_norm_gpu import bounds as norm_bounds, inputs as norm_inputs, reference as norm_reference
 from test_muon_gpu import USUAL, gradient
-from test_train_ops_gpu import U, torch  # noqa: F401  (torch: the fixture)
+from test_train_ops_gpu import U, near, tdtype, torch  # noqa: F401  (torch: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +48,35 @@ def test_joined_steps_keep_what_fp32_keeps(torch, shape, runs):  # noqa: F811
     plan.orthogonalize(plan.bind([out], [u.cuda()]), plan.workspace(), eps=1e-30)
     off = (out.double().cpu() - want).norm().item()
     assert off <= 6 * fp32 + U * want.norm().item(), (shape, off, fp32, want.norm().item())
+
+
+# (batch, sites, channels, groups): groups that a block keeps, and in the last two shapes parts of them
+MANY = [(20000, 1, 64, 8), (20000, 3, 24, 3), (100000, 1, 3, 1), (5000, 2, 1030, 10), (513, 4, 70, 7), (700, 2600, 8, 1),
+        (4200, 2600, 8, 1)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("last", [True, False])
+@pytest.mark.parametrize("shape", MANY)
+def test_weight_gradients_of_many_samples(torch, shape, last, dtype):  # noqa: F811
+    # Samples alike: a sum of one value many times, which rounds the same way for long stretches.  The gradients are
+    # those of one sample times their number, and so are the bounds of group norm's own tests, which take 16 U for
+    # every sum: trees of 16 rows (4), at most 16 of them in a slab's slice, six halvings, and the same over slabs.
+    batch, sites, channels, groups = shape
+    x, dy, w, b = norm_inputs(torch, (1, sites, channels, groups), last, dtype, "f32", 31)
+    dy = (dy * 0.1 + 0.3).to(tdtype(torch, dtype))
+    plan = bltrain.GroupNormPlan(batch, sites, channels, groups, channels_last=last, dtype=tdtype(torch, dtype))
+    xs, dys, wd, bd = x.cuda().repeat(batch, 1, 1), dy.cuda().repeat(batch, 1, 1), w.cuda(), b.cuda()
+    y, stats, dx = torch.empty_like(xs), torch.empty(plan.stats_shape(), device="cuda"), torch.full_like(xs, float("nan"))
+    dw, db = (torch.full((channels,), float("nan"), device="cuda") for _ in range(2))
+    ws = plan.workspace()
+    plan.forward(xs, wd, bd, y, stats, ws)
+    ws.fill_(255)
+    plan.backward(dys, xs, wd, bd, stats, dx, dw, db, ws)
+    x, dy, w, b = (v.double() for v in (x, dy, w, b))
+    r = norm_reference(torch, x, w, b, dy, groups, last, None, 1e-5)
+    most = norm_bounds(x, dy, r, groups, last, None, dtype, "f32")
+    assert (dx == dx[:1]).all()
+    near(dx[:1], r["dx"], most["dx"], "dx")
+    near(dw, batch * r["dw"], batch * most["dw"], "dw")
+    near(db, batch * r["db"], batch * most["db"], "db")
