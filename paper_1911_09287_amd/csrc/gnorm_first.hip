@@ -138,6 +138,8 @@ __global__ __launch_bounds__(kThreads) void k_first_bwd_part(GroupNormArgs a) {
       v[k].load(x + t + k * step, p.end - t - k * step);
       g[k].load(dy + t + k * step, p.end - t - k * step);
     }
+    // (these few by themselves first: a chain of all of a long channel's would round too much)
+    float few1 = 0.f, few2 = 0.f;
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       v[k].refresh();
@@ -146,10 +148,12 @@ __global__ __launch_bounds__(kThreads) void k_first_bwd_part(GroupNormArgs a) {
       for (int j = 0; j < V; ++j) {
         // (where there is no value z may be anything)
         const float dz = t + k * step + j < p.end ? act_grad<ACT>(own.z(v[k][j]), g[k][j]) : 0.f;
-        s1 += dz;
-        s2 = t + k * step + j < p.end ? fmaf(dz, own.h(v[k][j]), s2) : s2;
+        few1 += dz;
+        few2 = t + k * step + j < p.end ? fmaf(dz, own.h(v[k][j]), few2) : few2;
       }
     }
+    s1 += few1;
+    s2 += few2;
   }
   s1 = lanes_sum(s1, a.lanes, red[0]);
   s2 = lanes_sum(s2, a.lanes, red[1]);

@@ -19,6 +19,8 @@ template <typename T, int V>
 constexpr int kAhead = V * sizeof(T) >= 16 ? 4 : 8;
 template <typename T, int V>
 constexpr int kAheadBoth = kAhead<T, V> / 2;
+constexpr int kFew = 16;       // turns whose sums are taken by themselves
+constexpr int kMostWholeParts = 16;
 constexpr int kMostParts = 8;  // of a channel's slices, which threads sum side by side
 
 // Where a thread stands: sample, chunk, its first channel and its sites begin + slice, begin +
@@ -272,7 +274,10 @@ __global__ __launch_bounds__(kThreads) void k_last_bwd_part(GroupNormArgs a) {
   const T* dy = static_cast<const T*>(a.dy) + p.n * a.y_stride + p.c;
   LastChannels<T, V> own;
   own.load(a, p);
-  float s[2 * V] = {};
+  // Sums of kFew turns' sites, and of those before: one chain over all of a long sample's would round too much
+  // (512 x 32768 x 64 fp32, one value throughout: db off by 2e-5, and 1e-6 so)
+  float s[2 * V] = {}, before[2 * V] = {};
+  int turn = 0;
   if (p.there)
     p.walk<kAheadBoth<T, V>, HeldBoth<T, V>>(
         [&](HeldBoth<T, V>& to, long site) { to.load(x + site * a.channels, dy + site * a.channels); },
@@ -289,7 +294,12 @@ __global__ __launch_bounds__(kThreads) void k_last_bwd_part(GroupNormArgs a) {
               s[2 * j + 1] = fmaf(dz, h, s[2 * j + 1]);
             }
           }
+          if (++turn % kFew == 0)
+#pragma unroll
+            for (int j = 0; j < 2 * V; ++j) before[j] += s[j], s[j] = 0.f;
         });
+#pragma unroll
+  for (int j = 0; j < 2 * V; ++j) s[j] += before[j];
   slices_sum(s, red, p, a.lanes);
   if (p.slice || !p.there) return;
   float* to = a.part + ((p.n * a.chunks + p.chunk) * a.channels + p.c) * 2;
@@ -504,7 +514,8 @@ __global__ __launch_bounds__(kMostThreads) void k_last_whole_bwd(GroupNormArgs a
     v[e].refresh();
     d[e].refresh();
   }
-  // over the slices: a thread a channel
+  // over the slices: many in a few parts first, then a thread a channel
+  const int parts = min(p.slices, kMostWholeParts);
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     if (k) __syncthreads();
@@ -512,9 +523,18 @@ __global__ __launch_bounds__(kMostThreads) void k_last_whole_bwd(GroupNormArgs a
 #pragma unroll
       for (int j = 0; j < V; ++j) all[p.slice * row + p.c + j] = p.there ? s[k][j] : 0.f;
     __syncthreads();
+    if (p.slices > parts) {
+      // (a part's thread alone reads the place that its sum goes to)
+      for (int i = threadIdx.x; i < parts * row; i += blockDim.x) {
+        float sum = 0.f;
+        for (int at = i; at < p.slices * row; at += parts * row) sum += all[at];
+        all[i] = sum;
+      }
+      __syncthreads();
+    }
     for (int c = threadIdx.x; c < p.width; c += blockDim.x) {
       float sum = 0.f;
-      for (int i = 0; i < p.slices; ++i) sum += all[i * row + c];
+      for (int i = 0; i < parts; ++i) sum += all[i * row + c];
       chan[2 * c + k] = sum;
       a.own[(p.n * a.channels + p.first + c) * 2 + k] = sum;
     }

@@ -80,3 +80,21 @@ def test_weight_gradients_of_many_samples(torch, shape, last, dtype):  # noqa: F
     near(dx[:1], r["dx"], most["dx"], "dx")
     near(dw, batch * r["dw"], batch * most["dw"], "dw")
     near(db, batch * r["db"], batch * most["db"], "db")
+
+
+# (parts of samples that many blocks take, long channels side by side, and a sample's 512 slices of one block)
+@pytest.mark.parametrize("shape,last", [((1024, 3136, 256, 32), True), ((64, 50176, 64, 8), False), ((300, 2048, 4, 1), True)])
+def test_bias_gradients_of_many_sites(torch, shape, last):  # noqa: F811
+    # One gradient at every site: a sum of one value, which rounds the same way for long stretches where it is a
+    # chain.  16 U for a sum in few levels, as group norm's own tests take it, and U for the value itself.
+    batch, sites, channels, groups = shape
+    x, _, w, b = norm_inputs(torch, (1, sites, channels, groups), last, "f32", "f32", 32)
+    plan = bltrain.GroupNormPlan(batch, sites, channels, groups, channels_last=last)
+    xs, wd, bd = x.cuda().repeat(batch, 1, 1), w.cuda(), b.cuda()
+    dys = torch.full_like(xs, 0.3)
+    stats, dw, db = torch.empty(plan.stats_shape(), device="cuda"), torch.empty_like(wd), torch.empty_like(bd)
+    y, ws = torch.empty_like(xs), plan.workspace()
+    plan.forward(xs, wd, bd, y, stats, ws)
+    plan.backward(dys, xs, wd, bd, stats, y, dw, db, ws)
+    want = torch.full((channels,), 0.3).double() * (batch * sites)
+    near(db, want, 17 * U * want)
