@@ -6,7 +6,8 @@ import pytest
 from paper_1911_09287_amd import bltrain
 from test_group_norm_gpu import bounds as norm_bounds, inputs as norm_inputs, reference as norm_reference
 from test_muon_gpu import USUAL, gradient
-from test_train_ops_gpu import U, near, tdtype, torch  # noqa: F401  (torch: the fixture)
+from test_recurrence_gpu import inputs as steps_inputs, reference as steps_reference, run as steps_run
+from test_train_ops_gpu import U, half_ulp, near, tdtype, torch  # noqa: F401  (torch: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -98,3 +99,50 @@ def test_bias_gradients_of_many_sites(torch, shape, last):  # noqa: F811
     plan.backward(dys, xs, wd, bd, stats, y, dw, db, ws)
     want = torch.full((channels,), 0.3).double() * (batch * sites)
     near(db, want, 17 * U * want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("length", [1, 5, 8])
+def test_gates_whose_exponential_overflows(torch, length, dtype):  # noqa: F811
+    # exp(g) is infinite in fp32 for all but the last two, which 3 e^87 stays below the largest number for, and so
+    # is the state from then on
+    gates = torch.tensor([float("inf"), 3.3e38, 89.0, 93.5, 100.0, 127.0, 1000.0, 87.0, 86.5])
+    n = len(gates)
+    gate, x = torch.full((2, length, n), -0.5), torch.ones(2, length, n)
+    gate[:, -1] = gates
+    h0 = torch.ones(2, n, device="cuda")
+    plan = bltrain.RecurrencePlan(2, length, n, gate="exp", dtype=tdtype(torch, dtype))
+    y = torch.full((2, length, n), float("nan"), dtype=tdtype(torch, dtype), device="cuda")
+    last = torch.full_like(h0, float("nan"))
+    plan.forward(gate.to(y.dtype).cuda(), x.to(y.dtype).cuda(), y, plan.workspace(), h0=h0, last=last)
+    h = torch.ones(2, n, dtype=torch.float64)
+    for t in range(length):
+        a = gate[:, t].to(y.dtype).double().exp()
+        h = h * a.masked_fill(a >= 2.0 ** 128, float("inf")) + 1.0
+    assert (last[:, :7] == float("inf")).all() and (y[:, -1, :7] == float("inf")).all()
+    # an exponential of two units, a product and a sum for each step
+    near(last[:, 7:], h[:, 7:], 6 * U * length * h[:, 7:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 7, 20), (2, 300, 20), (1, 6000, 24), (300, 300, 1), (3, 300, 1), (2, 300, 3), (1, 9000, 3)])
+@pytest.mark.parametrize("how", ["grows", "wanders"])
+def test_states_that_grow(torch, how, shape, dtype):  # noqa: F811
+    # gates above 0 whose sum stays below 88 over all steps (in bfloat16 with room for its largest values too): by
+    # 60 steadily, or a few up and down
+    v = steps_inputs(torch, shape, "exp", dtype, 33, False)
+    g = torch.Generator().manual_seed(34)
+    if how == "grows":
+        gate = torch.rand(shape, generator=g) * (120.0 / shape[1])
+    else:
+        gate = torch.randn(shape, generator=g) * min(1.0, 6.0 / shape[1] ** 0.5)
+    v["gate"] = gate.to(tdtype(torch, dtype))
+    sums = v["gate"].double().cumsum(1)
+    assert (sums.amax(1) - sums.amin(1)).max() < 80
+    got = steps_run(torch, shape, "exp", dtype, v)
+    r, most = steps_reference(torch, *(v[k].double() for k in ("gate", "x", "h0", "dy", "dlast")), None, "exp")
+    for name in got:
+        bound = most[name]
+        if name in ("y", "dgate", "dx"):
+            bound = bound + half_ulp(dtype) * (r[name].abs() + bound) + 1e-30
+        near(got[name], r[name], bound, f"{name} {shape} {how}")
