@@ -98,9 +98,10 @@ bl_status_t bl_norm_backward(bl_norm_plan_t plan, const void* dy, const void* x,
  *   mean = sum x / size,   rstd = 1 / sqrt(sum (x - mean)^2 / size + eps)
  *   z = (x - mean) rstd w[c] + b[c],   y = act(z)
  *
- * act: z itself, max(z, 0) or z / (1 + exp(-z)).  x and dx have `dtype` and lie
- * samples x_stride elements apart (0: dense), y and dy likewise with y_stride.
- * w, b, dw, db [channels] have `wdtype`: fp32, or dtype. */
+ * act: z itself, max(z, 0) or z / (1 + exp(-z)), which is taken as 0 where z is below
+ * -87.3 (it would be below 2e-36).  x and dx have `dtype` and lie samples x_stride elements
+ * apart (0: dense), y and dy likewise with y_stride.  w, b, dw, db [channels] have `wdtype`:
+ * fp32, or dtype. */
 #define BL_CHANNELS_LAST 0
 #define BL_CHANNELS_FIRST 1
 

@@ -45,26 +45,39 @@ struct GroupNormArgs {
 __device__ __forceinline__ float norm_z(float x, float mean, float rstd, float w, float b) {
   return fmaf((x - mean) * rstd, w, b);
 }
-// By the hardware's power of two and reciprocal, an ulp each; rounding z log2(e) moves the
-// exponential by |z| ulps more, which z / (1 + exp(-z)) and its slope have at most 0.3 of.  (The
-// library's exponential and division took 30 of 45 instructions a value, and these bound
-// 16-bit passes: 128 x 3136 x 64 bf16 36 us against 22.)
-__device__ __forceinline__ float logistic(float z) {
-  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -0x1.715476p+0f));
+// q = 1 / (1 + exp(-z)) and q (1 - q), its slope, of z that comes from values of type T.  What rounds in z log2(e) moves the
+// exponential by |z| units, which z far below 0 would keep as a relative error: fp32 takes the corrected
+// one.  Of 16 bits a result of 2^-9 or 2^-11 has no sight of it (88 units are 2^-17), and there the power of two and
+// the reciprocal alone do, an ulp each.  (Instructions bound 16-bit passes: 128 x 3136 x 64 bf16 takes 36 us by the
+// library's exponential and division, which are 30 of 45 a value, against 22.)
+template <typename T>
+__device__ __forceinline__ void norm_logistic(float z, float& q, float& slope) {
+  if constexpr (sizeof(T) == 4) {
+    float rest;
+    logistic_of(z, q, rest, slope);
+  } else {
+    q = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -0x1.715476p+0f));
+    slope = fmaf(-q, q, q);
+  }
 }
-template <int ACT>
+template <int ACT, typename T>
 __device__ __forceinline__ float act_of(float z) {
   if (ACT == BL_ACT_RELU) return z > 0.f ? z : z != z ? z : 0.f;
-  if (ACT == BL_ACT_SILU) return z * logistic(z);
+  if (ACT == BL_ACT_SILU) {
+    float q, slope;
+    norm_logistic<T>(z, q, slope);
+    return z * q;
+  }
   return z;
 }
 // dy act'(z)
-template <int ACT>
+template <int ACT, typename T>
 __device__ __forceinline__ float act_grad(float z, float dy) {
   if (ACT == BL_ACT_RELU) return z > 0.f ? dy : z != z ? z : 0.f;
   if (ACT == BL_ACT_SILU) {
-    const float q = logistic(z);
-    return dy * fmaf(z * q, 1.f - q, q);
+    float q, slope;
+    norm_logistic<T>(z, q, slope);
+    return dy * fmaf(z, slope, q);
   }
   return dy;
 }

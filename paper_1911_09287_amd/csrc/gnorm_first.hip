@@ -116,7 +116,7 @@ __global__ __launch_bounds__(kThreads) void k_first_apply(GroupNormArgs a) {
       v[k].refresh();
       Pack<T, V> o;
 #pragma unroll
-      for (int j = 0; j < V; ++j) o.v[j] = (T)act_of<ACT>(own.z(v[k][j]));
+      for (int j = 0; j < V; ++j) o.v[j] = (T)act_of<ACT, T>(own.z(v[k][j]));
       store_part(y + t + k * step, p.end - t - k * step, o);
     }
   }
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(kThreads) void k_first_bwd_part(GroupNormArgs a) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         // (where there is no value z may be anything)
-        const float dz = t + k * step + j < p.end ? act_grad<ACT>(own.z(v[k][j]), g[k][j]) : 0.f;
+        const float dz = t + k * step + j < p.end ? act_grad<ACT, T>(own.z(v[k][j]), g[k][j]) : 0.f;
         few1 += dz;
         few2 = t + k * step + j < p.end ? fmaf(dz, own.h(v[k][j]), few2) : few2;
       }
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kThreads) void k_first_bwd_apply(GroupNormArgs a, u
       Pack<T, V> o;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float dz = act_grad<ACT>(own.z(v[k][j]), g[k][j]);
+        const float dz = act_grad<ACT, T>(own.z(v[k][j]), g[k][j]);
         o.v[j] = (T)norm_grad(dz, own.w, c1, own.h(v[k][j]), c2, own.rstd);
       }
       store_part(dx + t + k * step, p.end - t - k * step, o);
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(kMostThreads) void k_first_whole_fwd(GroupNormArgs 
     const long there = p.at(a, e);
     Pack<T, V> o;
 #pragma unroll
-    for (int j = 0; j < V; ++j) o.v[j] = (T)act_of<ACT>(norm_z(v[e][j], mean, rstd, w[e], b[e]));
+    for (int j = 0; j < V; ++j) o.v[j] = (T)act_of<ACT, T>(norm_z(v[e][j], mean, rstd, w[e], b[e]));
     store_part(y + p.offset(a), there, o);
   }
   if (a.stats && threadIdx.x == 0) {
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(kMostThreads) void k_first_whole_bwd(GroupNormArgs 
     d[e].refresh();
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const float dz = act_grad<ACT>(norm_z(v[e][j], mean, rstd, w[e], b[e]), d[e][j]), h = (v[e][j] - mean) * rstd;
+      const float dz = act_grad<ACT, T>(norm_z(v[e][j], mean, rstd, w[e], b[e]), d[e][j]), h = (v[e][j] - mean) * rstd;
       s1 += j < there ? dz : 0.f;
       s2 = j < there ? fmaf(dz, h, s2) : s2;
     }
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(kMostThreads) void k_first_whole_bwd(GroupNormArgs 
     Pack<T, V> o;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const float dz = act_grad<ACT>(norm_z(v[e][j], mean, rstd, w[e], b[e]), d[e][j]);
+      const float dz = act_grad<ACT, T>(norm_z(v[e][j], mean, rstd, w[e], b[e]), d[e][j]);
       o.v[j] = (T)norm_grad(dz, w[e], c1, (v[e][j] - mean) * rstd, c2, rstd);
     }
     store_part(dx + p.offset(a), there, o);

@@ -245,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void k_last_apply(GroupNormArgs a) {
           Pack<T, V> o;
 #pragma unroll
           for (int j = 0; j < V; ++j)
-            o.v[j] = (T)act_of<ACT>(norm_z(v[k][j], own.mean[j], own.rstd[j], own.w[j], own.b[j]));
+            o.v[j] = (T)act_of<ACT, T>(norm_z(v[k][j], own.mean[j], own.rstd[j], own.w[j], own.b[j]));
           if (k < count) store_pack(y + site * a.channels, o);
         }
       });
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(kThreads) void k_last_bwd_part(GroupNormArgs a) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
               const float h = (at[k].v[j] - own.mean[j]) * own.rstd[j];
-              const float dz = act_grad<ACT>(norm_z(at[k].v[j], own.mean[j], own.rstd[j], own.w[j], own.b[j]), at[k].g[j]);
+              const float dz = act_grad<ACT, T>(norm_z(at[k].v[j], own.mean[j], own.rstd[j], own.w[j], own.b[j]), at[k].g[j]);
               s[2 * j] += dz;
               s[2 * j + 1] = fmaf(dz, h, s[2 * j + 1]);
             }
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(kThreads) void k_last_bwd_apply(GroupNormArgs a, un
           Pack<T, V> o;
 #pragma unroll
           for (int j = 0; j < V; ++j) {
-            const float dz = act_grad<ACT>(norm_z(at[k].v[j], own.mean[j], own.rstd[j], own.w[j], own.b[j]), at[k].g[j]);
+            const float dz = act_grad<ACT, T>(norm_z(at[k].v[j], own.mean[j], own.rstd[j], own.w[j], own.b[j]), at[k].g[j]);
             o.v[j] = (T)norm_grad(dz, own.w[j], c1[j], (at[k].v[j] - own.mean[j]) * own.rstd[j], c2[j], own.rstd[j]);
           }
           if (k < count) store_pack(dx + site * a.channels, o);
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(kMostThreads) void k_last_whole_fwd(GroupNormArgs a
     if (!p.site(a, e, at)) continue;
     Pack<T, V> o;
 #pragma unroll
-    for (int j = 0; j < V; ++j) o.v[j] = (T)act_of<ACT>(norm_z(v[e][j], mean[j], rstd[j], w[j], b[j]));
+    for (int j = 0; j < V; ++j) o.v[j] = (T)act_of<ACT, T>(norm_z(v[e][j], mean[j], rstd[j], w[j], b[j]));
     store_pack(y + at * a.channels, o);
   }
   if (a.stats && p.slice == 0 && p.there)
@@ -507,7 +507,7 @@ __global__ __launch_bounds__(kMostThreads) void k_last_whole_bwd(GroupNormArgs a
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const float h = (v[e][j] - mean[j]) * rstd[j];
-      const float dz = act_grad<ACT>(norm_z(v[e][j], mean[j], rstd[j], w[j], b[j]), d[e][j]);
+      const float dz = act_grad<ACT, T>(norm_z(v[e][j], mean[j], rstd[j], w[j], b[j]), d[e][j]);
       s[0][j] += there ? dz : 0.f;
       s[1][j] = there ? fmaf(dz, h, s[1][j]) : s[1][j];
     }
@@ -572,7 +572,7 @@ __global__ __launch_bounds__(kMostThreads) void k_last_whole_bwd(GroupNormArgs a
     Pack<T, V> o;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const float dz = act_grad<ACT>(norm_z(v[e][j], mean[j], rstd[j], w[j], b[j]), d[e][j]);
+      const float dz = act_grad<ACT, T>(norm_z(v[e][j], mean[j], rstd[j], w[j], b[j]), d[e][j]);
       o.v[j] = (T)norm_grad(dz, w[j], c1[j], (v[e][j] - mean[j]) * rstd[j], c2[j], rstd[j]);
     }
     store_pack(dx + at * a.channels, o);

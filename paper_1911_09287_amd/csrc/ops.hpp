@@ -106,6 +106,29 @@ struct Held {
   }
 };
 
+// ---- exponentials ----------------------------------------------------------------
+// exp(g) by the hardware's power of two, and what g log2(e) and log2(e) itself round, which
+// would be |g| units: within two units of the last place, results below 2^-126 as 0.  (The
+// library's expf takes three times the instructions, and they bound 16-bit passes.)  GROWS:
+// g may be so large that the result is infinite, which has no part that could be corrected;
+// at minus infinity, where r is NaN, it is 0 whatever the correction.
+template <bool GROWS>
+__device__ __forceinline__ float exp_of(float g) {
+  constexpr float kLog2e = 0x1.715476p+0f, kRest = 0x1.4ae0cp-26f, kLn2 = 0x1.62e43p-1f;
+  const float t = g * kLog2e, r = fmaf(g, kLog2e, -t), e = __builtin_amdgcn_exp2f(t);
+  const float x = fmaf(e, __builtin_amdgcn_fmed3f(fmaf(r, kLn2, g * (kRest * kLn2)), -0x1p-10f, 0x1p-10f), e);
+  return GROWS && e == INFINITY ? e : x;
+}
+
+// q = 1 / (1 + exp(-z)), 1 - q and q (1 - q).  exp of -|z| does not overflow, and the smaller of the
+// first two keeps its relative precision, six units.
+__device__ __forceinline__ void logistic_of(float z, float& q, float& rest, float& slope) {
+  const float e = exp_of<false>(-fabsf(z)), big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
+  q = z >= 0.f ? big : small;  // (a NaN: both are)
+  rest = z >= 0.f ? small : big;
+  slope = small * big;
+}
+
 // ---- sums over lanes ------------------------------------------------------------
 // x of the lane that DPP control CTRL names.
 template <int CTRL>

@@ -72,30 +72,15 @@ __device__ __forceinline__ void stretch_apply(const Stretch<N>& s, float (&h)[N]
   for (int j = 0; j < N; ++j) h[j] = RESETS && s.drop ? s.b[j] : fmaf(s.a[j], h[j], s.b[j]);
 }
 
-// exp(g) by the hardware's power of two, and what g log2(e) and log2(e) itself round, which
-// would be |g| units: within two units of the last place, results below 2^-126 as 0.  (The
-// library's expf takes three times the instructions, and they bound 16-bit passes.)  GROWS:
-// g may be so large that the result is infinite, which has no part that could be corrected;
-// at minus infinity, where r is NaN, it is 0 whatever the correction.
-template <bool GROWS>
-__device__ __forceinline__ float exp_of(float g) {
-  constexpr float kLog2e = 0x1.715476p+0f, kRest = 0x1.4ae0cp-26f, kLn2 = 0x1.62e43p-1f;
-  const float t = g * kLog2e, r = fmaf(g, kLog2e, -t), e = __builtin_amdgcn_exp2f(t);
-  const float x = fmaf(e, __builtin_amdgcn_fmed3f(fmaf(r, kLn2, g * (kRest * kLn2)), -0x1p-10f, 0x1p-10f), e);
-  return GROWS && e == INFINITY ? e : x;
-}
-
-// a and 1 - a (exp: 1) of a gate.  sigmoid: exp of -|gate| does not overflow, and the
-// smaller of the two keeps its relative precision.
+// a and 1 - a (exp: 1) of a gate.
 template <int GATE>
 __device__ __forceinline__ void gate_of(float g, float& a, float& rest) {
   if (GATE == BL_GATE_EXP) {
     a = exp_of<true>(g);
     rest = 1.f;
   } else {
-    const float e = exp_of<false>(-fabsf(g)), big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
-    a = g >= 0.f ? big : small;  // (a NaN: both are)
-    rest = g >= 0.f ? small : big;
+    float slope;
+    logistic_of(g, a, rest, slope);
   }
 }
 

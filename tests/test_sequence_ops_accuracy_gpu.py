@@ -146,3 +146,24 @@ def test_states_that_grow(torch, how, shape, dtype):  # noqa: F811
         if name in ("y", "dgate", "dx"):
             bound = bound + half_ulp(dtype) * (r[name].abs() + bound) + 1e-30
         near(got[name], r[name], bound, f"{name} {shape} {how}")
+
+
+@pytest.mark.parametrize("last", [True, False])
+def test_silu_far_below_zero(torch, last):  # noqa: F811
+    # Groups of one value, whose z is the bias to the last bit: the activation and its slope q (1 + z (1 - q)) alone.
+    # q is an exponential of two units (4 U), a sum, a reciprocal of one (2 U) and a product, z q one more: 9 U; the
+    # slope has 9 U of both its terms and three roundings of them.  Where z is below -87.3 both are 0.
+    z = torch.cat([torch.linspace(-87.2, 30.0, 4001), torch.tensor([-90.0, -1000.0, -3e38, 3e37])])
+    n = len(z)
+    plan = bltrain.GroupNormPlan(1, 1, n, n, channels_last=last, act="silu")
+    x = torch.randn(1, n, generator=torch.Generator().manual_seed(35)).cuda()
+    y, dx, stats = torch.full_like(x, float("nan")), torch.full_like(x, float("nan")), torch.empty(2, 1, n, device="cuda")
+    w, b, dw, db = torch.ones(n, device="cuda"), z.cuda(), torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    ws = plan.workspace()
+    plan.forward(x, w, b, y, stats, ws)
+    plan.backward(torch.ones_like(x), x, w, b, stats, dx, dw, db, ws)
+    z = z.double()
+    q = z.sigmoid() * (z > -87.3)
+    near(y[0], z * q, 10 * U * (z * q).abs())
+    near(db, q + z * q * (-z).sigmoid(), 12 * U * (q + (z * q * (-z).sigmoid()).abs()))
+    assert (dx == 0).all() and (dw == 0).all()
