@@ -111,8 +111,7 @@ __global__ __launch_bounds__(kThreads) void k_muon_lay(MuonList list, MuonSlabs 
   double sum = 0.0;
   for (unsigned k = slabs.first[at] + threadIdx.x; k < slabs.first[at + 1]; k += kThreads) sum += a.squares[k];
   sum = block_sum(sum, red);
-  // (what is not finite makes all of the matrix NaN)
-  const double inv = (sum < (double)INFINITY ? 1.0 / (sqrt(sum) + a.eps) : (double)NAN) * kHoldX;
+  const double inv = muon_inverse(sum, a.eps);
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
     gv[k].refresh();

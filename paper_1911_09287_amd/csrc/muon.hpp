@@ -150,6 +150,12 @@ __device__ __forceinline__ unsigned muon_dither(unsigned long long place, unsign
 __device__ __forceinline__ float muon_update_of(float g, float m, float gs, const MuonArgs& a) {
   return !a.momentum ? gs * g : a.nesterov ? fmaf(a.beta, m, gs * g) : m;
 }
+// What u is multiplied by, from the sum of its squares: what is not finite makes all of the matrix NaN, and
+// zeros stay zeros though 1 / eps may be infinite.
+__device__ __forceinline__ double muon_inverse(double sum, double eps) {
+  if (sum == 0.0) return 0.0;
+  return (sum < (double)INFINITY ? 1.0 / (sqrt(sum) + eps) : (double)NAN) * kHoldX;
+}
 // The parameter from its old value and x of X, or x itself (set).
 template <typename P>
 __device__ __forceinline__ P muon_next(float old, float x, unsigned long long place, float keep, float rate, unsigned key,

@@ -130,8 +130,7 @@ __global__ __launch_bounds__(kT) void k_muon_small(MuonList list, MuonSmallSteps
   sum = 0.0;
 #pragma unroll
   for (int w = 0; w < kT / kWave; ++w) sum += red[w];
-  // (what is not finite makes all of the matrix NaN)
-  const double inv = (sum < (double)INFINITY ? 1.0 / (sqrt(sum) + a.eps) : (double)NAN) * kHoldX;
+  const double inv = muon_inverse(sum, a.eps);
   // X [short][n] and its transpose [n][short], padded with zeros to 32 or 64 and 64s.  A thread
   // takes eight rows of the matrix at a column, which lie side by side in one of the two.
   const MuonPlaces w = muon_places(1, it.n);

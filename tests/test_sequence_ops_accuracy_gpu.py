@@ -167,3 +167,17 @@ def test_silu_far_below_zero(torch, last):  # noqa: F811
     near(y[0], z * q, 10 * U * (z * q).abs())
     near(db, q + z * q * (-z).sigmoid(), 12 * U * (q + (z * q * (-z).sigmoid()).abs()))
     assert (dx == 0).all() and (dw == 0).all()
+
+
+@pytest.mark.parametrize("eps", [1e-300, 1e-308, 5e-324])
+def test_zeros_stay_whatever_eps_is(torch, eps):  # noqa: F811
+    # 1 / eps leaves 64 bits; both kernels that lay matrices out, and values beside the smallest there are
+    for shapes in ([(5, 7), (7, 5)], [(70, 90), (5, 7), (7, 5)]):
+        us = [torch.zeros(s) for s in shapes]
+        us[-1] = torch.full(shapes[-1], 2.0 ** -149)
+        plan = bltrain.MuonPlan(shapes)
+        outs = [torch.full(s, float("nan"), device="cuda") for s in shapes]
+        plan.orthogonalize(plan.bind(outs, [u.cuda() for u in us]), plan.workspace(), eps=eps)
+        for out in outs[:-1]:
+            assert (out == 0).all()
+        assert outs[-1].isfinite().all() and (outs[-1] > 0).all()
