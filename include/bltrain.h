@@ -167,7 +167,9 @@ bl_status_t bl_group_norm_backward(bl_group_norm_plan_t plan, const void* dy, co
  * h_before + (what its own steps give).  With exp(gate) above 1 a stretch's product can
  * exceed fp32's range, or h0 times it be NaN, where the single steps' results would
  * not: gates above 0 are for lengths over which their sum stays below 88.  Calls of up to
- * eight steps forward go step by step, and have no such limit.
+ * eight steps forward go step by step, and have no such limit.  What is not
+ * finite stays so up to the next reset, but where single steps keep an infinity it may become
+ * NaN, once a stretch's product has come down to 0.
  *
  * gate, x, dgate and dx have `dtype`; element (o, t, i) lies at o in_outer + t
  * in_step + i (0: dense, in_step = inner and in_outer = length in_step), so that gates
