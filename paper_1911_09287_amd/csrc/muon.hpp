@@ -28,14 +28,14 @@ struct MuonItem {
 
 struct MuonList {
   int count;
-  unsigned first[kMuonList + 1];  // blocks before each matrix's (all ones past the last)
+  unsigned first[kMuonList + 1];  // blocks before each matrix's; past the last one all are the number of blocks
   MuonItem item[kMuonList];
 };
 
 // What the products alone need.
 struct MuonShapes {
   int count;
-  unsigned first[kMuonList + 1];
+  unsigned first[kMuonList + 1];  // (a launch of two products reads a product's number of blocks at its end)
   unsigned off[kMuonList];
   unsigned short m[kMuonList], n[kMuonList];
 };
@@ -181,7 +181,7 @@ bl_status_t muon_small(int param_dtype, int grad_dtype, const MuonList& list, co
                        const MuonArgs& a, double flops, hipStream_t s);
 
 enum MuonMode { kGram, kPoly, kSquare, kApply };
-// side: of the tiles, 64 or 128.
+// side: of the tiles, 64, 128 or 256 (256: not where the result is symmetric).
 bl_status_t muon_product(int mode, int side, const MuonShapes& shapes, unsigned blocks, double flops, const MuonProduct& q,
                          hipStream_t s);
 // The last step's product, and the parameters' update from its tiles.
