@@ -73,16 +73,10 @@ __global__ __launch_bounds__(kThreads) void k_gnorm_join_bwd(GroupNormArgs a) {
   float s1 = 0.f, s2 = 0.f;
   for (unsigned first = 0; first < (unsigned)a.each; first += kWave / on) {
     const unsigned c = first + lane / on;
-    float dz = 0.f, dh = 0.f;
+    float sums[2] = {};
     if (c < (unsigned)a.each)
-#pragma unroll 8
-      for (unsigned k = lane % on; k < (unsigned)a.chunks; k += on) {
-        const Pack<float, 2> v = load_pack<float, 2>(a.part + (((n * a.chunks + k) * a.channels) + g * a.each + c) * 2);
-        dz += v.v[0];
-        dh += v.v[1];
-      }
-    dz = wave_sum(dz, (int)on);
-    dh = wave_sum(dh, (int)on);
+      gnorm_pairs_sum(a.part + (n * a.chunks * a.channels + g * a.each + c) * 2, a.channels * 2, lane % on, a.chunks, on, sums);
+    const float dz = wave_sum(sums[0], (int)on), dh = wave_sum(sums[1], (int)on);
     if (c < (unsigned)a.each && lane % on == 0) {
       const long at = g * a.each + c;
       a.own[(n * a.channels + at) * 2] = dz;

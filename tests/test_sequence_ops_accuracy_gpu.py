@@ -83,8 +83,10 @@ def test_weight_gradients_of_many_samples(torch, shape, last, dtype):  # noqa: F
     near(db, batch * r["db"], batch * most["db"], "db")
 
 
-# (parts of samples that many blocks take, long channels side by side, and a sample's 512 slices of one block)
-@pytest.mark.parametrize("shape,last", [((1024, 3136, 256, 32), True), ((64, 50176, 64, 8), False), ((300, 2048, 4, 1), True)])
+# (parts of samples that many blocks take, long channels side by side, a sample's 512 slices of one block, and
+# one sample's 2048 parts)
+@pytest.mark.parametrize("shape,last", [((1024, 3136, 256, 32), True), ((64, 50176, 64, 8), False), ((300, 2048, 4, 1), True),
+                                        ((1, 1 << 20, 65, 1), True)])
 def test_bias_gradients_of_many_sites(torch, shape, last):  # noqa: F811
     # One gradient at every site: a sum of one value, which rounds the same way for long stretches where it is a
     # chain.  16 U for a sum in few levels, as group norm's own tests take it, and U for the value itself.
