@@ -62,24 +62,21 @@ __device__ __forceinline__ f32x4 held(char* slot, int row, int c) {
   return v;
 }
 // A symmetric result: a lane's four values are rows r ... r + 3 of column c, and go to its columns r ...
-// r + 3 of row c too.  Values above the diagonal are left out, so that what is held is symmetric to the
-// last bit: an antisymmetric part would grow tenfold with every joined step (50 x 128 after five steps: off
-// by 3e-5 of the norm with both halves as computed, 3e-6 so).
+// r + 3 of row c, and those below the diagonal to their own place (after the wave's others, which a tile on
+// the diagonal has stored there), so that what is held is symmetric to the last bit: an antisymmetric part would
+// grow tenfold with every joined step (50 x 128 after five steps: off by 3e-5 of the norm with both halves as
+// computed, 3e-6 so).
 __device__ __forceinline__ void hold_both(char* slot, int r, int c, const f32x4& v) {
-  if (r >= c) hold(slot, c, r, v);
+  hold(slot, c, r, v);
   Pack<f16_t, 4> hi, lo;
   split4(v, hi, lo);
   const int k = c / 32 * 8 + c % 32 / 8, at = c % 8 * 2;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if (r + j < c) continue;
-    *reinterpret_cast<f16_t*>(piece(slot, r + j, k) + at) = hi.v[j];
-    *reinterpret_cast<f16_t*>(piece(slot, r + j, k + 4) + at) = lo.v[j];
-    if (r >= c) continue;
-    const int kr = (r + j) / 32 * 8 + (r + j) % 32 / 8, at_r = (r + j) % 8 * 2;
-    *reinterpret_cast<f16_t*>(piece(slot, c, kr) + at_r) = hi.v[j];
-    *reinterpret_cast<f16_t*>(piece(slot, c, kr + 4) + at_r) = lo.v[j];
-  }
+  for (int j = 0; j < 4; ++j)
+    if (r + j > c) {
+      *reinterpret_cast<f16_t*>(piece(slot, r + j, k) + at) = hi.v[j];
+      *reinterpret_cast<f16_t*>(piece(slot, r + j, k + 4) + at) = lo.v[j];
+    }
 }
 // This wave's tile of a product of square matrices, over `sum` times 32.
 __device__ __forceinline__ f32x4 square(char* p, char* q, int sum) {
