@@ -239,10 +239,10 @@ extern "C" bl_status_t bl_group_norm_plan_create(bl_group_norm_plan_t* out, cons
   p->chunks = (int)((d.sites + p->chunk - 1) / p->chunk);
   p->joins[0] = d.layout == BL_CHANNELS_LAST && p->tiles == 1 && d.channels * p->chunks <= kMostJoined &&
                 p->each * p->chunks <= kMostOfGroup;
-  p->joins[1] = p->joins[0] && d.batch * p->chunks <= kMostRows;
-  const long slices = kThreads / gnorm_rows_cols(d.channels);
-  if (!p->joins[1] && d.batch > kMostOwn * slices) {
-    p->slab = std::max<long>(kLeastOwn * slices, (d.batch + kMostSlabs - 1) / kMostSlabs);
+  const long most_rows = kMostOwn * (kThreads / gnorm_rows_cols(d.channels));
+  p->joins[1] = p->joins[0] && d.batch * p->chunks <= most_rows;
+  if (!p->joins[1] && d.batch > most_rows) {
+    p->slab = std::max<long>(most_rows / (kMostOwn / kLeastOwn), (d.batch + kMostSlabs - 1) / kMostSlabs);
     p->slabs = (d.batch + p->slab - 1) / p->slab;
   }
   const size_t groups = (size_t)d.batch * d.groups, channels = (size_t)d.batch * d.channels;

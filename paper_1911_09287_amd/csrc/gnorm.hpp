@@ -136,9 +136,9 @@ __device__ __forceinline__ void moments_join(Moments& a, const Moments& b) {
 // Parts of a sample that blocks which apply join, and of a group.  3 x 605 x 40 fp32 forward (160
 // parts) takes 14.2 us so and 17.6 with a launch that joins, 128 x 3136 x 64 bf16 (256) 34.8 and
 // 37.4; but 32 x 3136 x 256 (4096, which it was tried with) 41.1 and 38.4, 100 x 1024 x 50 (650) 22.4
-// and 20.1.  Backward the weights' gradients are then sums over all samples' chunks: 2002 of them
-// (182 x 7250 x 5 fp32) 39.6 and 31.3.
-constexpr long kMostJoined = 512, kMostOfGroup = 64, kMostRows = 512;
+// and 20.1.  Backward the weights' gradients are then sums over all samples' chunks, if a thread has no more
+// of these than kMostOwn: 63 each of 182 x 7250 x 5 fp32 28.1 us and 31.9, of 600 x 2600 x 8 (38) 55.7 and 59.1.
+constexpr long kMostJoined = 512, kMostOfGroup = 64;
 // Rows of samples' sums that a thread adds: of more, slabs are cut, in which it has two trees of 16 at least, and
 // 256 of them at most (64 of a thread that adds them).  Backward, bf16: 600 x 1 x 1024 23.7 us in slabs, 24.7 in one
 // launch, 4000 x 1 x 64 20.1 and 65, 65536 x 1 x 64 139 and 855.
