@@ -75,7 +75,8 @@ __global__ __launch_bounds__(kThreads) void k_gnorm_join_bwd(GroupNormArgs a) {
     const unsigned c = first + lane / on;
     float sums[2] = {};
     if (c < (unsigned)a.each)
-      gnorm_pairs_sum(a.part + (n * a.chunks * a.channels + g * a.each + c) * 2, a.channels * 2, lane % on, a.chunks, on, sums);
+      gnorm_pairs_sum(a.part + (n * a.chunks * a.channels + g * a.each + c) * 2, a.channels * 2, lane % on, a.chunks, on,
+                      a.chunks, sums);
     const float dz = wave_sum(sums[0], (int)on), dh = wave_sum(sums[1], (int)on);
     if (c < (unsigned)a.each && lane % on == 0) {
       const long at = g * a.each + c;
