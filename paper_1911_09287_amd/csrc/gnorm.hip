@@ -7,8 +7,8 @@
 // a block's registers can hold whole groups of a sample they are read once, by one launch.
 //
 // Kernels' times, bf16 (bytes as moved, with the second reading): 128 x 3136 x 64 channels last
-// forward 13.6 + 20.3 us, 154 MB; 32 x 3136 x 256 backward 31.6 + 4.8 + 28.3 us, 257
-// MB; in one launch fp32 channels first 64 x 256 x 512 backward 26.6 us, 101 MB, and 4.1 for the
+// forward 13.7 + 20.3 us, 154 MB; 32 x 3136 x 256 backward 31.2 + 4.9 + 28.4 us, 257
+// MB; in one launch fp32 channels first 64 x 256 x 512 backward 27.8 us, 101 MB, and 4.5 for the
 // weights' gradients.
 #include <algorithm>
 #include <cmath>

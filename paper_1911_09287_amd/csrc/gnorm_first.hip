@@ -202,7 +202,7 @@ __global__ __launch_bounds__(kThreads) void k_first_bwd_apply(GroupNormArgs a, u
 // A block keeps a group of a sample: each channel's sites on `lanes` lanes of a wave, so that
 // a thread has accesses k of the channels pass rows + its row (entry e = pass per + k of E).
 // x (and dy) are read once, and no sums cross blocks but the weights' gradients.  (64 x 256 x 512
-// fp32 backward: 26.6 us, 3.8 TB/s, in three launches over 90.)
+// fp32 backward: 27.8 us, 3.6 TB/s, in three launches over 90.)
 template <int V>
 struct WholePlace {
   long n, g, c, site;  // of an entry: its channel in the group and its first site

@@ -13,7 +13,7 @@
 // off by 3e-5 of the norm with both halves of those tiles as computed).
 //
 // Bound by the matrix cores where there are many tiles: 1024 x 4096 and squares of 1024, 126 M
-// values, 5.0e12 operations in 6.7 ms (0.65 of what a library's fp16 product of 8192 reaches, 1.15e15
+// values, 5.0e12 operations in 7.0 ms (0.62 of what a library's fp16 product of 8192 reaches, 1.15e15
 // a second); with the 200 tiles of a residual network's grams by their fetch, 64 KB a compute
 // unit in 1.25 us.
 #include "muon.hpp"
